@@ -63,7 +63,8 @@ enum mpt_status {
     MPT_E_WORKSPACE = -6, /* workspace missing, misaligned or too small */
     MPT_E_STATE = -7,     /* context call out of order (e.g. a solve before a build) */
     MPT_E_DEVICE = -8,    /* HIP runtime error (detail in mpt_last_error) */
-    MPT_E_INTERNAL = -9   /* internal error (e.g. a host allocation failed) */
+    MPT_E_INTERNAL = -9,  /* internal error (e.g. a host allocation failed) */
+    MPT_E_PAGES = -10     /* a page call asks for more pages than are free */
 };
 
 /* Bytes of device workspace that every entry point below needs for an
@@ -458,6 +459,206 @@ int mpt_pinned_assemble(int m, int64_t nnz, const int64_t *req_off, const int32_
                         int t, const int32_t *dmap, int n_distinct, const int64_t *free_off,
                         const int32_t *free_layout, int32_t *seqs, void *workspace,
                         size_t workspace_bytes, void *stream);
+
+/*
+ * ---- Serving a layout: a paged key/value cache ----
+ *
+ * The prompts of a layout share prefixes (the nodes of its trie). These calls
+ * hold the keys and values of those prefixes in pages that several sequences
+ * refer to, so that a request forked off a cached prefix computes only the
+ * tokens that the trie cost bills for it.
+ *
+ * Token t of the sequence in slot s lies in page table[s * max_pages + t /
+ * page_size], at slot t % page_size of that page. ref[p] counts the
+ * references to page p from the sequences' tables; bit p % 64 of
+ * free_bits[p / 64] is set iff ref[p] = 0 (bits past n_pages are 0). A page
+ * taken by a call is the lowest-numbered free one, so tables do not depend on
+ * how the device schedules work. Table entries past a sequence's last page
+ * mean nothing and are not touched.
+ *
+ * The caller owns every array and fills in the descriptor; mpt_kv_reset
+ * empties the tables. A row (layer, page, slot, head) holds head_dim
+ * consecutive elements. Strides are in elements and multiples of 8, bases
+ * are 16-byte aligned, head_dim is a multiple of 8; the other orders of the
+ * dimensions are free (heads inside or outside the slots, layers or keys and
+ * values interleaved). Rows must not overlap.
+ *
+ * Errors in device data: a call that finds one changes nothing in tables and
+ * pages and ORs MPT_KV_* bits into *status, where they stay until
+ * mpt_kv_status reads them. The page calls take a nullable HOST output; with
+ * it they synchronise `stream` and return the error of this call
+ * (MPT_E_RANGE, MPT_E_DUP, MPT_E_STATE or MPT_E_PAGES). Without it, and in
+ * mpt_kv_append, mpt_kv_attention and mpt_kv_merge, nothing synchronises, and
+ * the calls can be captured into a graph. Page ids outside [0, n_pages) and
+ * slots outside [0, max_seqs) are never followed.
+ * Calls on one cache must be ordered by the caller (one stream, or events).
+ */
+#define MPT_KV_BF16 0
+#define MPT_KV_F16 1
+#define MPT_KV_F32 2              /* outputs and merged parts only */
+#define MPT_KV_MAX_DIM 256
+#define MPT_KV_MAX_PAGE_SIZE 1024
+#define MPT_KV_MAX_PAGES (1 << 26)
+#define MPT_KV_MAX_PARTS 16
+
+#define MPT_KV_BAD_SLOT 1u        /* a slot outside [0, max_seqs), or offsets that are no CSR */
+#define MPT_KV_BAD_LENGTH 2u      /* a length outside its range */
+#define MPT_KV_BAD_PAGE 4u        /* a page id outside [0, n_pages) or without references */
+#define MPT_KV_DUPLICATE 8u       /* a slot or page listed twice */
+#define MPT_KV_NOT_EMPTY 16u      /* a fork into a slot that holds tokens */
+#define MPT_KV_NO_PAGES 32u       /* more pages asked for than are free */
+#define MPT_KV_SHARED 64u         /* an append into a page of several sequences */
+
+typedef struct mpt_kv_cache {
+    void *k, *v;                  /* device: keys and values */
+    int64_t k_stride[4];          /* elements from one layer, page, slot, head to the next */
+    int64_t v_stride[4];
+    int32_t *table;               /* device [max_seqs * max_pages]: page ids */
+    int32_t *length;              /* device [max_seqs]: tokens per sequence (0: an empty slot) */
+    int32_t *ref;                 /* device [n_pages] */
+    uint64_t *free_bits;          /* device [(n_pages + 63) / 64] */
+    uint32_t *status;             /* device: MPT_KV_* bits */
+    int dtype;                    /* MPT_KV_BF16 or MPT_KV_F16 */
+    int n_layers, n_pages;
+    int page_size;                /* a power of two, 1 .. MPT_KV_MAX_PAGE_SIZE */
+    int n_heads, head_dim;        /* key/value heads; a multiple of 8, 8 .. MPT_KV_MAX_DIM */
+    int max_seqs, max_pages;      /* max_pages * page_size <= 2^30 */
+} mpt_kv_cache;
+
+/* Empties the cache: every page free, every length 0, status 0. Does not
+ * synchronise. */
+int mpt_kv_reset(const mpt_kv_cache *cache, void *stream);
+
+/* *bits (HOST) = the cache's status bits, which are then cleared.
+ * Synchronises `stream`. */
+int mpt_kv_status(const mpt_kv_cache *cache, uint32_t *bits, void *stream);
+
+/* Bytes of device workspace (256-byte aligned) for the page calls: 8 n_pages
+ * + 12 max_seqs and less than 4 KiB (0 for a descriptor that is not valid). */
+size_t mpt_kv_workspace_bytes(const mpt_kv_cache *cache);
+
+/*
+ * Forks: for each i < n the empty slot dst[i] becomes a sequence of
+ * new_len[i] tokens whose first keep[i] are those of src[i]. The
+ * keep / page_size full pages are shared; then come fresh pages, taken in the
+ * order of the list, and the keep % page_size tokens of a last partial page
+ * are copied into the first of them (all layers). src[i] = -1 with keep[i] = 0
+ * shares nothing. Sources are read as they were before the call.
+ *   src, dst, keep, new_len [n]  device; dst distinct and empty; 0 <= keep[i]
+ *                                <= length[src[i]], keep[i] <= new_len[i]
+ *   free_pages                   HOST out, nullable: free pages afterwards
+ * All or nothing.
+ */
+int mpt_kv_fork(const mpt_kv_cache *cache, int n, const int32_t *src, const int32_t *dst,
+                const int32_t *keep, const int32_t *new_len, int64_t *free_pages,
+                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Grows sequences to new_len[i] >= length[seqs[i]] tokens with fresh pages,
+ * as mpt_kv_fork takes them. A partial last page that other sequences refer
+ * to (left by mpt_kv_free with a keep) is first replaced by a copy.
+ *   seqs, new_len [n]  device; seqs distinct
+ */
+int mpt_kv_extend(const mpt_kv_cache *cache, int n, const int32_t *seqs, const int32_t *new_len,
+                  int64_t *free_pages, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Cuts sequences to keep[i] <= length[seqs[i]] tokens (keep NULL: to none).
+ * Pages past the last kept token lose a reference and are free without any.
+ *   seqs, keep [n]  device; seqs distinct; empty ones are allowed
+ */
+int mpt_kv_free(const mpt_kv_cache *cache, int n, const int32_t *seqs, const int32_t *keep,
+                int64_t *free_pages, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Moves pages so that the n_live pages in use are 0 .. n_live - 1: the used
+ * pages from n_live on, in ascending order, go to the free ones below, in
+ * ascending order. Tables, references and contents (all layers) move along.
+ *   live_pages  HOST out, nullable: n_live
+ */
+int mpt_kv_compact(const mpt_kv_cache *cache, int64_t *live_pages,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Copies the contents of page src[i] to page dst[i] (all layers), i < n.
+ * No page may be in both lists or twice in dst. Tables stay as they are.
+ *   checked  HOST out, nullable: pages copied (n, or 0 after an error)
+ */
+int mpt_kv_copy(const mpt_kv_cache *cache, int n, const int32_t *src, const int32_t *dst,
+                int64_t *checked, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Writes new keys and values of one layer: entry i < n has the tokens
+ * q_off[i] .. q_off[i+1] - 1 of k_new and v_new, the newest of the sequence in
+ * slot seqs[i] (which mpt_kv_fork or mpt_kv_extend has made long enough):
+ * they go to positions length - (q_off[i+1] - q_off[i]) .. length - 1.
+ *   seqs [n]             device; distinct
+ *   q_off [n+1]          device; q_off[0] = 0, non-decreasing, q_off[n] = n_tokens
+ *   k_new, v_new         device, the cache's type, [n_tokens, n_heads,
+ *                        head_dim]; strides in elements, multiples of 8;
+ *                        16-byte aligned
+ * Tokens before position 0, in bad slots or pages, or in pages that other
+ * sequences refer to are not written (and set status bits).
+ */
+int mpt_kv_append(const mpt_kv_cache *cache, int layer, int n, const int32_t *seqs,
+                  const int32_t *q_off, int64_t n_tokens, const void *k_new,
+                  int64_t k_token_stride, int64_t k_head_stride, const void *v_new,
+                  int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/* Bytes of device workspace (256-byte aligned) for mpt_kv_attention of up to
+ * n_tokens tokens with n_q_heads query heads (0 for sizes out of range). */
+size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_t n_tokens,
+                                        int n_q_heads);
+
+/*
+ * Attention of new tokens over the cache, one layer. Entry i < n has the
+ * queries q_off[i] .. q_off[i+1] - 1, the newest n_i tokens of the sequence
+ * in slot seqs[i] of length L: query j stands at position p = L - n_i + j.
+ * Query head h reads key head h / (n_q_heads / n_heads). Token t is visible
+ * iff kv_begin[i] <= t < L, t <= p if causal, and t > p - window if
+ * window > 0. With s_t = scale q.k_t, or softcap tanh(scale q.k_t / softcap)
+ * if softcap > 0, over the visible t:
+ *     lse = log sum exp(s_t),   out = sum exp(s_t - lse) v_t.
+ * Rows that see no token (or only scores of minus infinity) get out = 0 and
+ * lse = minus infinity. What lies in tokens that a row does not see, NaN and
+ * infinities included, has no effect on it. Decoding is a chunk of one token;
+ * a prefix that several sequences share is one slot with all of their queries
+ * and causal = 0, joined with their own parts (kv_begin) by mpt_kv_merge.
+ *   seqs [n]       device; a slot may be listed several times
+ *   q_off [n+1]    device; q_off[0] = 0, non-decreasing, q_off[n] = n_tokens
+ *   q, out         device [n_tokens, n_q_heads, head_dim]; strides in
+ *                  elements, multiples of 8; 16-byte aligned. q has the
+ *                  cache's type, out that type or MPT_KV_F32 (out_dtype)
+ *   lse            device out, nullable: float [n_tokens * n_q_heads],
+ *                  natural logarithms
+ *   kv_begin [n]   device, nullable (0): first visible token
+ * Scores, statistics and sums are held in 32 bits; the weights exp(s_t - max)
+ * are rounded to the cache's type for the product with the values.
+ */
+int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, const int32_t *seqs,
+                     const int32_t *q_off, int64_t n_tokens, int n_q_heads, const void *q,
+                     int64_t q_token_stride, int64_t q_head_stride, void *out,
+                     int64_t out_token_stride, int64_t out_head_stride, int out_dtype, float *lse,
+                     const int32_t *kv_begin, int causal, int window, float softcap, float scale,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Joins attention over disjoint parts of a context: for each row r < rows
+ *     lse = log sum_p exp(lse_p),   out = sum_p exp(lse_p - lse) out_p,
+ * which is attention over all parts together. Parts whose lse is minus
+ * infinity are not read; without any other, out = 0 and lse = minus infinity.
+ *   n_parts         1 .. MPT_KV_MAX_PARTS
+ *   parts, part_lse HOST arrays [n_parts] of device pointers: [rows, dim]
+ *                   (contiguous, 16-byte aligned, MPT_KV_* part_dtype) and
+ *                   float [rows]
+ *   dim             a multiple of 8, 8 .. MPT_KV_MAX_DIM
+ *   out [rows, dim] device, contiguous, 16-byte aligned, out_dtype; may be
+ *                   one of the parts if the types are equal
+ *   lse [rows]      device out, nullable; may be one of part_lse
+ */
+int mpt_kv_merge(int n_parts, int64_t rows, int dim, const void *const *parts,
+                 const float *const *part_lse, int part_dtype, void *out, int out_dtype, float *lse,
+                 void *stream);
 
 /* Static text for a status code. */
 const char *mpt_status_string(int status);

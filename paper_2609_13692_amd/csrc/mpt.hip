@@ -3551,6 +3551,7 @@ extern "C" const char *mpt_status_string(int status) {
         case MPT_E_STATE: return "call out of order for the context's state";
         case MPT_E_DEVICE: return "HIP runtime error";
         case MPT_E_INTERNAL: return "internal error";
+        case MPT_E_PAGES: return "not enough free pages";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,231 @@
+"""The paged key/value cache of include/mpt.h: pages that the sequences of a
+layout share, appends, attention of new tokens over the pages, and the join of
+attention over parts of a context.
+
+As :mod:`.mpt` this only marshals arguments: every step runs in the HIP kernels
+of ``libmpt.so``. Calls enqueue on the current stream (or ``stream``) and
+synchronise only where ``check=True`` asks for a host result. Lists of slots,
+lengths and pages are int32 device tensors.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from .mpt import KvDescriptor, MptError, _check, _stream, load
+
+BF16, F16, F32 = 0, 1, 2
+_KIND = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+MAX_PARTS = 16
+STATUS_BITS = {1: "slot", 2: "length", 4: "page", 8: "duplicate", 16: "not empty", 32: "no pages", 64: "shared page"}
+
+
+def _list(t, n, name, device):
+    """Address of a contiguous int32 device tensor of at least n elements."""
+    if t.dtype != torch.int32:
+        raise TypeError(f"{name} must be torch.int32, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < n:
+        raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
+    return t.data_ptr()
+
+
+class KvCache:
+    """Keys and values of many sequences in pages that they may share.
+
+    ``k`` and ``v`` are [layers, pages, slots per page, heads, dim] tensors
+    (bfloat16 or float16) of any strides that are multiples of 8 elements, the
+    last one 1; ``table`` [slots, pages of a sequence], ``length`` [slots],
+    ``ref`` [pages] and ``status`` [1] are int32, ``free_bits`` int64, one bit
+    per page: together the state described at ``mpt_kv_cache``.
+    :meth:`create` allocates and empties one.
+
+    The cache holds the workspaces of its calls, which grow as needed; calls
+    on one cache must be ordered (one stream, or events between streams).
+    """
+
+    def __init__(self, k, v, table, length, ref, free_bits, status):
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be [layers, pages, slots, heads, dim] of one shape and type")
+        if k.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"k and v must be bfloat16 or float16, got {k.dtype}")
+        if not k.is_cuda:
+            raise ValueError("k must be a device tensor")
+        if k.stride(4) != 1 or v.stride(4) != 1:
+            raise ValueError("the elements of a row must be contiguous")
+        layers, pages, size, heads, dim = k.shape
+        for name, t, dtype, n in (("ref", ref, torch.int32, pages), ("free_bits", free_bits, torch.int64, -(-pages // 64)),
+                                  ("status", status, torch.int32, 1), ("length", length, torch.int32, 1),
+                                  ("table", table, torch.int32, 1), ("v", v, v.dtype, 0)):
+            if t.dtype != dtype or t.device != k.device or t.numel() < n or (name != "v" and not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on {k.device}")
+        if table.dim() != 2 or table.shape[0] != length.numel():
+            raise ValueError("table must be [slots, pages of a sequence], length [slots]")
+        self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
+        self.free_bits, self.status = free_bits, status
+        self.device, self.dtype, self.page_size, self.n_heads, self.head_dim = k.device, k.dtype, size, heads, dim
+        self.max_seqs = table.shape[0]
+        d = KvDescriptor()
+        d.k, d.v = k.data_ptr(), v.data_ptr()
+        d.k_stride[:], d.v_stride[:] = k.stride()[:4], v.stride()[:4]
+        d.table, d.length, d.ref = table.data_ptr(), length.data_ptr(), ref.data_ptr()
+        d.free_bits, d.status = free_bits.data_ptr(), status.data_ptr()
+        d.dtype, d.n_layers, d.n_pages, d.page_size = _KIND[k.dtype], layers, pages, size
+        d.n_heads, d.head_dim, d.max_seqs, d.max_pages = heads, dim, table.shape[0], table.shape[1]
+        self._d = d
+        self._p = ctypes.addressof(d)
+        self._lib = load()
+        n = self._lib.mpt_kv_workspace_bytes(self._p)
+        if n == 0:
+            raise MptError(-1, "mpt_kv_workspace_bytes", self._lib.mpt_last_error().decode())
+        self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self._at_ws, self._at_sizes = None, {}
+
+    @classmethod
+    def create(cls, n_layers, n_pages, page_size, n_heads, head_dim, max_seqs, max_len, dtype=torch.bfloat16,
+               device="cuda", heads_first=False):
+        """An empty cache; ``heads_first`` puts a page's heads outside its slots."""
+        shape = (n_layers, n_pages) + ((n_heads, page_size) if heads_first else (page_size, n_heads)) + (head_dim,)
+        # zeros: a page is copied whole, tokens that were never written included
+        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        if heads_first:
+            k, v = k.transpose(2, 3), v.transpose(2, 3)
+        i32 = dict(dtype=torch.int32, device=device)
+        c = cls(k, v, torch.full((max_seqs, max(1, -(-max_len // page_size))), -1, **i32), torch.zeros(max_seqs, **i32),
+                torch.zeros(n_pages, **i32), torch.zeros(-(-n_pages // 64), dtype=torch.int64, device=device),
+                torch.zeros(1, **i32))
+        c.reset()
+        return c
+
+    def reset(self, stream=None):
+        _check(self._lib.mpt_kv_reset(self._p, _stream(stream)), "mpt_kv_reset")
+
+    def take_status(self, stream=None) -> list[str]:
+        """What calls have found wrong in device data since the last look."""
+        bits = ctypes.c_uint32(0)
+        _check(self._lib.mpt_kv_status(self._p, ctypes.addressof(bits), _stream(stream)), "mpt_kv_status")
+        return [name for bit, name in STATUS_BITS.items() if bits.value & bit]
+
+    def _pages(self, name, lists, check, stream, counted=True):
+        f = getattr(self._lib, "mpt_kv_" + name)
+        out = ctypes.c_int64(0)
+        n = next((t.numel() for t in lists if t is not None), 0)
+        args = [None if t is None else _list(t, n, name + " list", self.device) for t in lists]
+        rc = f(self._p, *((n,) if counted else ()), *args, ctypes.addressof(out) if check else None,
+               self._ws.data_ptr(), self._ws.numel(), _stream(stream))
+        _check(rc, "mpt_kv_" + name)
+        return int(out.value) if check else None
+
+    def fork(self, src, dst, keep, new_len, check=False, stream=None):
+        """Empty slots dst become sequences of new_len tokens sharing the first
+        keep with src (-1: none). With check, waits and returns the number of
+        free pages left, or raises."""
+        return self._pages("fork", (src, dst, keep, new_len), check, stream)
+
+    def extend(self, seqs, new_len, check=False, stream=None):
+        """Grows sequences to new_len tokens."""
+        return self._pages("extend", (seqs, new_len), check, stream)
+
+    def free(self, seqs, keep=None, check=False, stream=None):
+        """Cuts sequences to keep tokens (None: to none)."""
+        return self._pages("free", (seqs, keep), check, stream)
+
+    def compact(self, check=False, stream=None):
+        """Moves the pages in use to the lowest numbers; with check returns
+        how many they are."""
+        return self._pages("compact", (), check, stream, counted=False)
+
+    def copy(self, src, dst, check=False, stream=None):
+        """Copies page contents (all layers)."""
+        return self._pages("copy", (src, dst), check, stream)
+
+    def _rows(self, t, heads, name, dtype):
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.dtype != dtype:
+            raise ValueError(f"{name} must be [tokens, {heads}, {self.head_dim}] of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if t.device != self.device or t.stride(2) != 1:
+            raise ValueError(f"{name} must be on {self.device}, with contiguous rows")
+        return t.data_ptr(), t.stride(0), t.stride(1)
+
+    def append(self, layer, k_new, v_new, q_off, seqs, stream=None):
+        """Writes the newest tokens' keys and values of one layer; q_off [n + 1]
+        cuts the tokens into the sequences in seqs [n]."""
+        n, tokens = seqs.numel(), k_new.shape[0]
+        if v_new.shape[0] != tokens:
+            raise ValueError("k_new and v_new must have one row per token")
+        rc = self._lib.mpt_kv_append(self._p, layer, n, _list(seqs, n, "seqs", self.device),
+                                     _list(q_off, n + 1, "q_off", self.device), tokens,
+                                     *self._rows(k_new, self.n_heads, "k_new", self.dtype),
+                                     *self._rows(v_new, self.n_heads, "v_new", self.dtype), _stream(stream))
+        if rc:
+            _check(rc, "mpt_kv_append")
+
+    def attend(self, layer, q, q_off, seqs, causal=True, window=0, softcap=0.0, scale=None, kv_begin=None, out=None,
+               lse=None, out_dtype=None, stream=None):
+        """(out, lse) of the newest tokens' queries over their sequences (see
+        mpt_kv_attention). scale defaults to 1 / sqrt(dim)."""
+        n, tokens, heads = seqs.numel(), q.shape[0], q.shape[1]
+        if out is None:
+            out = torch.empty((tokens, heads, self.head_dim), dtype=out_dtype or self.dtype, device=self.device)
+        elif out.shape[0] != tokens or (out_dtype or out.dtype) != out.dtype:
+            raise ValueError("out must have one row per token, of out_dtype")
+        if lse is None:
+            lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device)
+        elif lse.dtype != torch.float32 or lse.device != self.device or lse.shape != (tokens, heads) or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous float32 [tokens, heads] device tensor")
+        key = (n, tokens, heads)
+        need = self._at_sizes.get(key)
+        if need is None:
+            need = self._lib.mpt_kv_attention_workspace_bytes(self._p, n, tokens, heads)
+            if len(self._at_sizes) < 4096:
+                self._at_sizes[key] = need
+        if need and (self._at_ws is None or self._at_ws.numel() < need):
+            self._at_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        ws = self._at_ws
+        rc = self._lib.mpt_kv_attention(
+            self._p, layer, n, _list(seqs, n, "seqs", self.device), _list(q_off, n + 1, "q_off", self.device), tokens,
+            heads, *self._rows(q, heads, "q", self.dtype), *self._rows(out, heads, "out", out.dtype),
+            _KIND.get(out.dtype, -1), lse.data_ptr(),
+            None if kv_begin is None else _list(kv_begin, n, "kv_begin", self.device), 1 if causal else 0, window, softcap,
+            1.0 / math.sqrt(self.head_dim) if scale is None else scale, ws.data_ptr() if ws is not None else None,
+            ws.numel() if ws is not None else 0, _stream(stream))
+        if rc:
+            _check(rc, "mpt_kv_attention")
+        return out, lse
+
+
+def merge(parts, lses, out_dtype=None, out=None, lse=None, stream=None):
+    """(out, lse) of attention over disjoint parts of a context: parts are
+    [..., dim] tensors of one shape and type, lses float32 [...] (see
+    mpt_kv_merge)."""
+    if len(parts) != len(lses) or not 1 <= len(parts) <= MAX_PARTS:
+        raise ValueError(f"needs 1 .. {MAX_PARTS} parts, each with its lse")
+    first = parts[0]
+    if first.dtype not in _KIND:
+        raise TypeError(f"parts must be bfloat16, float16 or float32, got {first.dtype}")
+    shape, device = first.shape, first.device
+    for p, l in zip(parts, lses):
+        if p.shape != shape or p.dtype != first.dtype or p.device != device or not p.is_contiguous() or not p.is_cuda:
+            raise ValueError("parts must be contiguous device tensors of one shape and type")
+        if l.shape != shape[:-1] or l.dtype != torch.float32 or l.device != device or not l.is_contiguous():
+            raise ValueError("lses must be contiguous float32 device tensors of the parts' shape without the last dimension")
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype or first.dtype, device=device)
+    elif out.shape != shape or out.device != device or not out.is_contiguous() or out.dtype not in _KIND or \
+            (out_dtype or out.dtype) != out.dtype:
+        raise ValueError("out must be a contiguous device tensor of the parts' shape and out_dtype")
+    if lse is None:
+        lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+    elif lse.shape != shape[:-1] or lse.dtype != torch.float32 or lse.device != device or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 device tensor")
+    n = len(parts)
+    rc = load().mpt_kv_merge(n, lse.numel(), shape[-1], (ctypes.c_void_p * n)(*[p.data_ptr() for p in parts]),
+                             (ctypes.c_void_p * n)(*[l.data_ptr() for l in lses]), _KIND[first.dtype], out.data_ptr(),
+                             _KIND.get(out.dtype, -1), lse.data_ptr(), _stream(stream))
+    if rc:
+        _check(rc, "mpt_kv_merge")
+    return out, lse

@@ -32,7 +32,7 @@ MPT_NOALLOC_MAX_M = 20
 _STATUS = {
     0: "MPT_OK", -1: "MPT_E_INVALID", -2: "MPT_E_RANGE", -3: "MPT_E_DUP",
     -4: "MPT_E_WEIGHT", -5: "MPT_E_OVERFLOW", -6: "MPT_E_WORKSPACE", -7: "MPT_E_STATE",
-    -8: "MPT_E_DEVICE", -9: "MPT_E_INTERNAL",
+    -8: "MPT_E_DEVICE", -9: "MPT_E_INTERNAL", -10: "MPT_E_PAGES",
 }
 EXPORTED = ("mpt_workspace_bytes", "mpt_build_weights", "mpt_solve_exact", "mpt_extract_orders",
             "mpt_status_string", "mpt_last_error", "mpt_profile_begin", "mpt_profile_end",
@@ -42,7 +42,9 @@ EXPORTED = ("mpt_workspace_bytes", "mpt_build_weights", "mpt_solve_exact", "mpt_
             "mpt_pinned_assemble", "mpt_create", "mpt_destroy", "mpt_set_option", "mpt_ctx_workspace_bytes",
             "mpt_set_workspace", "mpt_ctx_build_weights", "mpt_ctx_solve_exact", "mpt_ctx_extract_orders",
             "mpt_copy_table", "mpt_table_device", "mpt_solve_exact_noalloc", "mpt_ctx_optimum",
-            "mpt_profile_begin_prefix")
+            "mpt_profile_begin_prefix", "mpt_kv_reset", "mpt_kv_status", "mpt_kv_workspace_bytes", "mpt_kv_fork",
+            "mpt_kv_extend", "mpt_kv_free", "mpt_kv_compact", "mpt_kv_copy", "mpt_kv_append",
+            "mpt_kv_attention_workspace_bytes", "mpt_kv_attention", "mpt_kv_merge")
 
 
 class MptError(RuntimeError):
@@ -55,6 +57,16 @@ class MptError(RuntimeError):
 class ProfileRow(ctypes.Structure):
     _fields_ = [("kernel", ctypes.c_char * 48), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double), ("work", ctypes.c_double)]
+
+
+class KvDescriptor(ctypes.Structure):
+    """mpt_kv_cache (see include/mpt.h); :class:`.kv.KvCache` fills it in."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 4),
+                ("v_stride", ctypes.c_int64 * 4), ("table", ctypes.c_void_p), ("length", ctypes.c_void_p),
+                ("ref", ctypes.c_void_p), ("free_bits", ctypes.c_void_p), ("status", ctypes.c_void_p),
+                ("dtype", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("n_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("max_seqs", ctypes.c_int), ("max_pages", ctypes.c_int)]
 
 
 _lib = None
@@ -134,6 +146,21 @@ def load() -> ctypes.CDLL:
     lib.mpt_copy_table.restype = i32
     lib.mpt_table_device.argtypes = [P, i32, ctypes.POINTER(P), ctypes.POINTER(sz)]
     lib.mpt_table_device.restype = i32
+    f32 = ctypes.c_float
+    for name, args in (("reset", [P, P]), ("status", [P, P, P]),
+                       ("fork", [P, i32, P, P, P, P, P, P, sz, P]), ("extend", [P, i32, P, P, P, P, sz, P]),
+                       ("free", [P, i32, P, P, P, P, sz, P]), ("compact", [P, P, P, sz, P]),
+                       ("copy", [P, i32, P, P, P, P, sz, P]),
+                       ("append", [P, i32, i32, P, P, i64, P, i64, i64, P, i64, i64, P]),
+                       ("attention", [P, i32, i32, P, P, i64, i32, P, i64, i64, P, i64, i64, i32, P, P, i32, i32, f32,
+                                      f32, P, sz, P]),
+                       ("merge", [i32, i64, i32, P, P, i32, P, i32, P, P])):
+        f = getattr(lib, "mpt_kv_" + name)
+        f.argtypes, f.restype = args, i32
+    lib.mpt_kv_workspace_bytes.argtypes = [P]
+    lib.mpt_kv_workspace_bytes.restype = sz
+    lib.mpt_kv_attention_workspace_bytes.argtypes = [P, i32, i64, i32]
+    lib.mpt_kv_attention_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
