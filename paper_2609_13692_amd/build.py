@@ -11,7 +11,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SRCS = [os.path.join(CSRC, f) for f in ("mpt.hip", "ctx.hip", "greedy.hip", "layout.hip", "pinned.hip")]
-KV_SRCS = [os.path.join(CSRC, f) for f in ("kv.hip", "attention.hip")]
+KV_SRCS = [os.path.join(CSRC, f) for f in ("attention_wide.hip", "attention_narrow.hip", "attention.hip", "kv.hip")]
 LIB = os.path.join(PKG, "libmpt.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -31,7 +31,7 @@ def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
     with tempfile.TemporaryDirectory() as d:
         jobs, objects = [], []
-        for srcs, flags in ((SRCS, SOLVER), (KV_SRCS, [])):
+        for srcs, flags in ((KV_SRCS, []), (SRCS, SOLVER)):
             for src in srcs:
                 obj = os.path.join(d, os.path.basename(src) + ".o")
                 objects.append(obj)
@@ -40,7 +40,7 @@ def build(verbose: bool = False) -> str:
                 "-L", "/opt/rocm/lib", "-lrocprofiler-sdk-roctx", "-Wl,-rpath,/opt/rocm/lib"]
         if verbose:
             print("\n".join(" ".join(c) for c in (*jobs, link)), flush=True)
-        with ThreadPoolExecutor(4) as pool:
+        with ThreadPoolExecutor(8) as pool:
             list(pool.map(subprocess.check_call, jobs))
         subprocess.check_call(link)
     os.replace(tmp, LIB)

@@ -1,0 +1,332 @@
+// Shared by the two attention kernels: their arguments, how the work of a
+// ragged batch is cut over workgroups, and the matrix instructions.
+//
+// Rows. The queries of an entry that read one key head are n tokens x G heads
+// = n G rows (row r: token r / G, head r % G), cut into tiles of M rows. A
+// tile reads the keys [lo, hi) that any of its rows sees, in steps of BN
+// tokens: its units.
+//
+// Cut. All units of all tiles, in the order entry, key head, tile, step, are
+// one line of U units. Worker w takes [w U / W, (w + 1) U / W): the same
+// amount of work each whatever the lengths, with at most two tiles of its own
+// cut (its first and its last). Lengths are on the device, so every workgroup
+// finds its part itself, from sums over the entries. A tile that one worker
+// holds alone is finished by it; of the others each worker leaves the
+// unnormalised sums in the workspace, and a second launch joins them in the
+// order of the workers, so results do not depend on scheduling.
+#pragma once
+
+#include "kv.h"
+
+namespace mptkv {
+
+struct Attn {
+    mpt_kv_cache c;
+    int layer, n, n_tokens, heads, group, units;     // units: 16-byte pieces of a row
+    const int32_t *seqs, *q_off, *kv_begin;
+    const char *q;
+    char *out;
+    int64_t q_token, q_head, out_token, out_head;
+    float *lse;
+    int out_f32, causal, window, flip;
+    float factor;                                     // |scale| log2(e), or |scale| / softcap
+    float cap;                                        // softcap log2(e)
+    uint32_t k_page, k_slot, v_page, v_slot;          // strides in 16-byte units
+    const char *k, *v;                                // of the layer
+    int64_t k_head, v_head;                           // bytes
+    int workers;
+    struct Part *parts;                               // [workers]
+    float *sums;                                      // [workers][2][tile rows * (padded dim + 2)]
+};
+
+// What a worker's first tile is, if it is the second worker of that tile:
+// the join's work list.
+struct Part {
+    int count, entry, head, tile;                     // count: workers of the tile (0: nothing to join)
+    int q0, n;                                        // the entry's first token and tokens
+};
+
+constexpr int kEntries = 256;                         // entries whose sizes are held at a time
+constexpr int kMaxEntries = kEntries * kEntries;
+
+struct Entries {
+    int q0[kEntries], n[kEntries], len[kEntries], begin[kEntries], slot[kEntries];
+    int64_t steps[kEntries];                          // units of one key head
+    int64_t chunk[kEntries];                          // units of each 256 entries, all heads
+    int64_t wave[4];
+};
+
+struct Range {
+    int lo, hi, first, count;                         // visible tokens; first step and steps (at least 1)
+};
+
+template <int M, int BN>
+__device__ inline Range tile_range(const Attn &a, int n, int len, int begin, int tile) {
+    const int rows = n * a.group, r0 = tile * M, r1 = min(r0 + M, rows) - 1;
+    Range g;
+    const int p0 = len - n + r0 / a.group, p1 = len - n + r1 / a.group;
+    g.hi = max(0, a.causal ? min(len, p1 + 1) : len);
+    g.lo = a.window ? max(begin, p0 + 1 - a.window) : begin;
+    if (g.hi <= g.lo) g.lo = g.hi = 0;
+    g.first = g.lo / BN;
+    g.count = max(1, (g.hi + BN - 1) / BN - g.first);
+    return g;
+}
+
+template <int M>
+__device__ inline int tiles_of(const Attn &a, int n) {
+    return (n * a.group + M - 1) / M;
+}
+
+// Sizes of entries base .. base + 255; returns their units (all heads).
+template <int M, int BN>
+__device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = base + tid;
+    const mpt_kv_cache &c = a.c;
+    int n = 0, len = 0, begin = 0, q0 = 0, slot = -1;
+    if (i < a.n) {
+        q0 = a.q_off[i];
+        const int q1 = a.q_off[i + 1];
+        slot = a.seqs[i];
+        const bool csr = q0 >= 0 && q0 <= q1 && q1 <= a.n_tokens;
+        const bool ok = slot >= 0 && slot < c.max_seqs;
+        if (csr) n = q1 - q0;
+        if (ok) len = max(0, min(c.length[slot], c.max_pages * c.page_size));
+        if (a.kv_begin) begin = max(0, a.kv_begin[i]);
+        if (blockIdx.x == 0 && !(csr && ok)) flag(c, MPT_KV_BAD_SLOT);
+        if (!ok) slot = 0;
+    }
+    const int tiles = tiles_of<M>(a, n);
+    int64_t steps = 0;
+    if (tiles <= 8)
+        for (int t = 0; t < tiles; ++t) steps += tile_range<M, BN>(a, n, len, begin, t).count;
+    // long entries: the lanes of a wave take the tiles
+    for (uint64_t todo = __ballot(tiles > 8); todo; todo &= todo - 1) {
+        const int src = __ffsll((unsigned long long)todo) - 1;
+        const int n2 = __shfl(n, src), len2 = __shfl(len, src), begin2 = __shfl(begin, src);
+        int64_t x = 0;
+        for (int t = lane; t < tiles_of<M>(a, n2); t += 64) x += tile_range<M, BN>(a, n2, len2, begin2, t).count;
+        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+        if (lane == src) steps = x;
+    }
+    s.q0[tid] = q0, s.n[tid] = n, s.len[tid] = len, s.begin[tid] = begin, s.slot[tid] = slot, s.steps[tid] = steps;
+    int64_t sum = steps;
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    __syncthreads();
+    if (lane == 0) s.wave[wave] = sum;
+    __syncthreads();
+    return (s.wave[0] + s.wave[1] + s.wave[2] + s.wave[3]) * c.n_heads;
+}
+
+// A workgroup's walk over its units.
+template <int M, int BN>
+struct Walk {
+    int64_t total, at, end;           // units: all, this worker's next, its end
+    int64_t before;                   // units before the current entry
+    int worker, workers, base, e;     // entries base .. are loaded, e is the current one
+    int head, tile;
+    int64_t tile_at;                  // units before the current tile
+
+    __device__ static int64_t cut(int64_t total, int w, int workers) { return total * w / workers; }
+    // the worker that holds unit u
+    __device__ static int owner(int64_t u, int64_t total, int workers) {
+        return (int)(((u + 1) * workers - 1) / total);
+    }
+
+    // False if this workgroup has no work. least: units that are worth a worker.
+    __device__ bool begin(const Attn &a, Entries &s, int least) {
+        const int tid = threadIdx.x;
+        total = 0;
+        for (base = 0; base < a.n; base += kEntries) {
+            const int64_t x = load_entries<M, BN>(a, s, base);
+            if (tid == 0) s.chunk[base / kEntries] = x;
+            total += x;
+        }
+        workers = (int)min((int64_t)a.workers, max((int64_t)1, total / least));
+        // neighbours, which read the same keys, on one XCD (the grid is a
+        // multiple of 8: every number below it is one workgroup's)
+        const int per = (workers + 7) / 8, bid = blockIdx.x;
+        worker = (bid >> 3) < per ? (bid & 7) * per + (bid >> 3) : bid;
+        if (tid == 0) a.parts[worker].count = 0;
+        if (total == 0 || worker >= workers) return false;
+        at = cut(total, worker, workers);
+        end = cut(total, worker + 1, workers);
+        __syncthreads();
+        before = 0;
+        int k = 0;
+        while (before + s.chunk[k] <= at) before += s.chunk[k++];
+        if (a.n > kEntries) {
+            __syncthreads();
+            load_entries<M, BN>(a, s, k * kEntries);
+        }
+        base = k * kEntries;
+        // the entry, by the lanes of each wave: 64 at a time
+        const int lane = tid & 63;
+        e = 0;
+        for (;;) {
+            int64_t x = s.steps[e + lane] * a.c.n_heads, y = x;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int64_t z = __shfl_up(y, d);
+                if (lane >= d) y += z;
+            }
+            const uint64_t past = __ballot(before + y > at);
+            if (past) {
+                const int k2 = __ffsll((unsigned long long)past) - 1;
+                before += __shfl(y - x, k2);
+                e += k2;
+                break;
+            }
+            before += __shfl(y, 63);
+            e += 64;
+        }
+        const int64_t in = at - before, steps = s.steps[e];
+        head = (int)(in / steps);
+        find_tile(a, s, in - head * steps);
+        return true;
+    }
+
+    // The tile that holds the given step of a head of the current entry.
+    __device__ void find_tile(const Attn &a, const Entries &s, int64_t step) {
+        const int lane = threadIdx.x & 63, tiles = tiles_of<M>(a, s.n[e]);
+        int64_t sum = 0;
+        for (tile = 0;; tile += 64) {
+            const int64_t x = tile + lane < tiles ? tile_range<M, BN>(a, s.n[e], s.len[e], s.begin[e], tile + lane).count : 0;
+            int64_t y = x;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int64_t z = __shfl_up(y, d);
+                if (lane >= d) y += z;
+            }
+            const uint64_t past = __ballot(sum + y > step);
+            if (past) {
+                const int k = __ffsll((unsigned long long)past) - 1;
+                tile += k;
+                tile_at = before + head * s.steps[e] + sum + __shfl(y - x, k);
+                return;
+            }
+            sum += __shfl(y, 63);
+        }
+    }
+
+    // To the next tile, after all units of the current one.
+    __device__ void next(const Attn &a, Entries &s) {
+        tile_at = at;
+        if (++tile < tiles_of<M>(a, s.n[e])) return;
+        tile = 0;
+        if (++head < a.c.n_heads) return;
+        head = 0;
+        before = at;
+        do {
+            if (++e == kEntries) {
+                __syncthreads();
+                base += kEntries;
+                load_entries<M, BN>(a, s, base);
+                e = 0;
+            }
+        } while (s.n[e] == 0);
+    }
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <class T> struct Type;
+template <> struct Type<__bf16> {
+    using x8 = bf16x8;
+    static constexpr int kExponent = 0x7f80;
+    __device__ static f32x16 mfma32(s16x8 x, s16x8 y, f32x16 z) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
+    }
+    __device__ static f32x4 mfma16(s16x8 x, s16x8 y, f32x4 z) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
+    }
+};
+template <> struct Type<_Float16> {
+    using x8 = f16x8;
+    static constexpr int kExponent = 0x7c00;
+    __device__ static f32x16 mfma32(s16x8 x, s16x8 y, f32x16 z) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), z, 0, 0, 0);
+    }
+    __device__ static f32x4 mfma16(s16x8 x, s16x8 y, f32x4 z) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), z, 0, 0, 0);
+    }
+};
+
+// 16 bytes of zeros in memory: what is read in place of tokens outside a
+// tile's range, of pages that do not exist and of dimensions past head_dim.
+// Rows of zeros take part in every product without a trace; the stale
+// contents of a page may be NaN, and 0 x NaN is none.
+static __device__ const uint4 kZeros[4] = {};
+
+__device__ inline void load_lds16(const char *from, char *lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+}
+
+// Bytes from a layer's and head's first row to that of a token: strides are
+// counted in 16 bytes, so that 32-bit factors reach 64 GiB per page.
+__device__ inline uint64_t row_at(uint32_t page, uint32_t slot, uint32_t page_stride, uint32_t slot_stride) {
+    return ((uint64_t)page * page_stride + (uint64_t)slot * slot_stride) << 4;
+}
+
+// Four elements of one column from four rows: the lanes of 16 exchange what
+// they read, lane i of them getting column i.
+__device__ inline s16x4 read_column4(const char *lds) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)lds);
+}
+
+// Positions in log2 units of a score x = q.k: x |scale| log2(e), or with a
+// cap c log2(e) tanh(x |scale| / c). tanh z = 1 - 2 / (1 + e^2z); below 1/4,
+// where that cancels, its series to z^9 (relative error 1e-8).
+template <bool CAP>
+__device__ inline float score(const Attn &a, float x) {
+    if constexpr (!CAP) return x * a.factor;
+    const float z = x * a.factor, y = z * z;
+    const float e = __builtin_amdgcn_exp2f(2.885390081777927f * z);
+    const float big = 1.0f - 2.0f / (1.0f + e);
+    const float small = z * (1.0f + y * (-0.333333333f + y * (0.133333333f + y * (-0.053968254f + y * 0.021869489f))));
+    return a.cap * (fabsf(z) < 0.25f ? small : big);
+}
+
+template <class T>
+__device__ inline bool finite16(short x) {
+    return (x & Type<T>::kExponent) != Type<T>::kExponent;
+}
+
+// By value: __builtin_bit_cast of an element of a vector takes its first one.
+template <class T>
+__device__ inline float value16(short x) {
+    return (float)__builtin_bit_cast(T, x);
+}
+
+// Whether any of 8 elements is an infinity or NaN.
+template <class T>
+__device__ inline uint32_t odd8(s16x8 x) {
+    const uint4 u = __builtin_bit_cast(uint4, x);
+    constexpr uint32_t kE = Type<T>::kExponent * 0x10001u, kOne = (0x8000u - Type<T>::kExponent) * 0x10001u;
+    return (((u.x & kE) + kOne) | ((u.y & kE) + kOne) | ((u.z & kE) + kOne) | ((u.w & kE) + kOne)) & 0x80008000u;
+}
+
+template <class T>
+__device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
+    if (a.out_f32) {
+        *(f32x4 *)(a.out + 4 * at) = x;
+    } else {
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        t4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = (T)x[i];
+        *(t4 *)(a.out + 2 * at) = y;
+    }
+}
+
+inline int pad_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+
+// Launch of one kernel for the sizes of a call; false if the launch failed.
+void launch_wide(const Attn &a, int blocks32, hipStream_t s);
+void launch_narrow(const Attn &a, hipStream_t s);
+
+}  // namespace mptkv
