@@ -39,6 +39,12 @@ struct Attn {
     float *sums;                                      // [workers][2][tile rows * (padded dim + 2)]
 };
 
+// A value that is the same in all lanes, in scalar registers.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
 // What a worker's first tile is, if it is the second worker of that tile:
 // the join's work list.
 struct Part {
@@ -136,12 +142,13 @@ struct Walk {
     // False if this workgroup has no work. least: units that are worth a worker.
     __device__ bool begin(const Attn &a, Entries &s, int least) {
         const int tid = threadIdx.x;
-        total = 0;
+        int64_t sum = 0;
         for (base = 0; base < a.n; base += kEntries) {
             const int64_t x = load_entries<M, BN>(a, s, base);
             if (tid == 0) s.chunk[base / kEntries] = x;
-            total += x;
+            sum += x;
         }
+        total = uniform(sum);
         workers = (int)min((int64_t)a.workers, max((int64_t)1, total / least));
         // neighbours, which read the same keys, on one XCD (the grid is a
         // multiple of 8: every number below it is one workgroup's)
@@ -149,12 +156,12 @@ struct Walk {
         worker = (bid >> 3) < per ? (bid & 7) * per + (bid >> 3) : bid;
         if (tid == 0) a.parts[worker].count = 0;
         if (total == 0 || worker >= workers) return false;
-        at = cut(total, worker, workers);
-        end = cut(total, worker + 1, workers);
+        at = uniform(cut(total, worker, workers));
+        end = uniform(cut(total, worker + 1, workers));
         __syncthreads();
         before = 0;
         int k = 0;
-        while (before + s.chunk[k] <= at) before += s.chunk[k++];
+        while (before + uniform(s.chunk[k]) <= at) before += uniform(s.chunk[k++]);
         if (a.n > kEntries) {
             __syncthreads();
             load_entries<M, BN>(a, s, k * kEntries);
@@ -172,14 +179,14 @@ struct Walk {
             const uint64_t past = __ballot(before + y > at);
             if (past) {
                 const int k2 = __ffsll((unsigned long long)past) - 1;
-                before += __shfl(y - x, k2);
+                before += uniform(__shfl(y - x, k2));
                 e += k2;
                 break;
             }
-            before += __shfl(y, 63);
+            before += uniform(__shfl(y, 63));
             e += 64;
         }
-        const int64_t in = at - before, steps = s.steps[e];
+        const int64_t in = at - before, steps = uniform(s.steps[e]);
         head = (int)(in / steps);
         find_tile(a, s, in - head * steps);
         return true;
@@ -200,17 +207,17 @@ struct Walk {
             if (past) {
                 const int k = __ffsll((unsigned long long)past) - 1;
                 tile += k;
-                tile_at = before + head * s.steps[e] + sum + __shfl(y - x, k);
+                tile_at = before + head * uniform(s.steps[e]) + sum + uniform(__shfl(y - x, k));
                 return;
             }
-            sum += __shfl(y, 63);
+            sum += uniform(__shfl(y, 63));
         }
     }
 
     // To the next tile, after all units of the current one.
     __device__ void next(const Attn &a, Entries &s) {
         tile_at = at;
-        if (++tile < tiles_of<M>(a, s.n[e])) return;
+        if (++tile < tiles_of<M>(a, uniform(s.n[e]))) return;
         tile = 0;
         if (++head < a.c.n_heads) return;
         head = 0;
@@ -222,7 +229,7 @@ struct Walk {
                 load_entries<M, BN>(a, s, base);
                 e = 0;
             }
-        } while (s.n[e] == 0);
+        } while (uniform(s.n[e]) == 0);
     }
 };
 
@@ -230,6 +237,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -255,15 +263,43 @@ template <> struct Type<_Float16> {
     }
 };
 
-// 16 bytes of zeros in memory: what is read in place of tokens outside a
-// tile's range, of pages that do not exist and of dimensions past head_dim.
-// Rows of zeros take part in every product without a trace; the stale
-// contents of a page may be NaN, and 0 x NaN is none.
-static __device__ const uint4 kZeros[4] = {};
+// A row of zeros in memory: what is read in place of tokens outside a tile's
+// range, of pages that do not exist and of dimensions past head_dim. Rows of
+// zeros take part in every product without a trace; the stale contents of a
+// page may be NaN, and 0 x NaN is none.
+static __device__ const uint4 kZeros[MPT_KV_MAX_DIM / 8] = {};
 
-__device__ inline void load_lds16(const char *from, char *lds) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                     (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+// from, or zeros; a select that is not turned into branches around two loads.
+__device__ inline const char *or_zeros(bool there, const char *from) {
+    uint64_t p = (uint64_t)(there ? from : (const char *)kZeros);
+    asm("" : "+v"(p));
+    return (const char *)p;
+}
+
+// x, as a value that may differ from one pass of a loop to the next: addresses
+// formed from it are formed anew instead of being kept in registers.
+__device__ inline int renewed(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+template <class V>
+__device__ inline V load(const char *from) {
+    return *(const __attribute__((address_space(1))) V *)(uint64_t)from;
+}
+
+// 16 bytes per lane from memory to LDS, lane i at lds + 16 i, without a stop
+// in registers. The instruction is written out because the compiler takes any
+// later LDS read for one of its result and would wait for the loads of the
+// next tile there; who uses it waits (arrived) before the barrier that lets
+// the tile be read.
+__device__ inline void load_lds16(const char *from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory");
+}
+__device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ inline uint32_t lds_address(const void *p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
 }
 
 // Bytes from a layer's and head's first row to that of a token: strides are

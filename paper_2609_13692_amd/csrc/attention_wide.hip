@@ -17,12 +17,10 @@
 
 namespace mptkv {
 
-template <class T, int DP, int NB, bool CAP>
+template <int DP>
 struct Wide {
-    static constexpr int M = 128 * NB, BN = DP == 256 ? 32 : 64;
-    static constexpr int MT = BN / 32, KK = DP / 16, DT = DP / 32, ROW = 2 * DP, CH = DP / 8;
-    static constexpr int kTile = BN * ROW, kLoads = kTile / 4096;     // 16-byte loads per thread and tile
-
+    static constexpr int BN = 64, KK = DP / 16, DT = DP / 32, ROW = 2 * DP, CH = DP / 8;
+    static constexpr int kTile = BN * ROW, kLoads = kTile / 4096;     // 16-byte loads per thread, of keys or values
     static constexpr int kStride = 256 / CH;                          // tokens between a thread's loads
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight
@@ -35,141 +33,157 @@ struct Wide {
 
 template <class T, int DP, int NB, bool CAP>
 __global__ __launch_bounds__(256, NB == 2 || DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
-    using W = Wide<T, DP, NB, CAP>;
-    constexpr int M = W::M, BN = W::BN, MT = W::MT, KK = W::KK, DT = W::DT, ROW = W::ROW, CH = W::CH, L = W::kLoads;
+    using W = Wide<DP>;
+    constexpr int M = 128 * NB, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, CH = W::CH, L = W::kLoads, TILE = W::kTile;
     __shared__ Entries ent;
-    __shared__ __attribute__((aligned(1024))) char k0[W::kTile], v0[W::kTile], k1[W::kTile], v1[W::kTile];
+    __shared__ __attribute__((aligned(1024))) char keys[2 * TILE], values[2 * TILE];
     const mpt_kv_cache &c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
     const int shift = 31 - __clz(c.page_size);
+    const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_address(keys) + wave * 1024);
+    const uint32_t v_lds = __builtin_amdgcn_readfirstlane(lds_address(values) + wave * 1024);
+    // the thread's tokens of a tile, its pieces of their rows
+    const int own = tid / CH, kp = (tid % CH) ^ W::k_swizzle(own), vp = (tid % CH) ^ W::v_swizzle(own);
+    const bool k_in = kp < a.units, v_in = vp < a.units;
+    // where a lane reads its operands: rows of 32 tokens of keys, 8 of values
+    const int k_row = col * ROW, k_flip = half ^ W::k_swizzle(col);
+    const int v_of = 4 * half + (lane & 15) / 4;
+    const int v_row = v_of * ROW + (lane & 1) * 8, v_flip = (((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ W::v_swizzle(v_of);
 
     Walk<M, BN> walk;
     if (!walk.begin(a, ent, 4)) return;
 
     while (walk.at < walk.end) {
-        const int e = walk.e, n = ent.n[e], len = ent.len[e], q0 = ent.q0[e], slot = ent.slot[e];
-        const Range range = tile_range<M, BN>(a, n, len, ent.begin[e], walk.tile);
-        const int64_t from = walk.at - walk.tile_at;
-        const int first = range.first + (int)from;
-        const int last = range.first + (int)min((int64_t)range.count, from + (walk.end - walk.at));
-        const int head = walk.head, rows = n * a.group, row_base = walk.tile * M + wave * 32 * NB;
-        const int32_t *table = c.table + (int64_t)slot * c.max_pages;
+        const int e = uniform(walk.e), n = uniform(ent.n[e]), len = uniform(ent.len[e]), q0 = uniform(ent.q0[e]);
+        const int begin = uniform(ent.begin[e]), head = uniform(walk.head), tile = uniform(walk.tile);
+        const Range range = tile_range<M, BN>(a, n, len, begin, tile);
+        const int from = uniform((int)(walk.at - walk.tile_at)), first = range.first + from;
+        const int last = uniform(range.first + (int)min((int64_t)range.count, from + (walk.end - walk.at)));
+        const int rows = n * a.group, row_base = tile * M + wave * 32 * NB;
+        const int32_t *table = c.table + (int64_t)uniform(ent.slot[e]) * c.max_pages;
         const bool active = row_base < rows;
 
-        // queries of the wave's blocks: operand pieces, and what each may see
+        // queries of the wave's blocks as operands, and what each may see
         s16x8 qf[NB][KK];
         int see_lo[NB], see_hi[NB], wave_lo = 0, wave_hi = 1 << 30;
-        int64_t out_at[NB];
-        int64_t lse_at[NB];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const int r = row_base + nb * 32 + col, rr = min(r, rows - 1), j = rr / a.group, hq = rr - j * a.group;
+            const int r = row_base + nb * 32 + col, rr = min(r, rows - 1), j = rr / a.group;
             const int p = len - n + j;
             see_hi[nb] = a.causal ? min(len, p + 1) : len;
-            see_lo[nb] = a.window ? max(ent.begin[e], p + 1 - a.window) : ent.begin[e];
-            const int64_t token = q0 + j, h = (int64_t)head * a.group + hq;
-            out_at[nb] = r < rows ? token * a.out_token + h * a.out_head : -1;
-            lse_at[nb] = token * a.heads + h;
-            const char *q = a.q + 2 * (token * a.q_token + h * a.q_head);
+            see_lo[nb] = a.window ? max(begin, p + 1 - a.window) : begin;
+            const char *q = a.q + 2 * ((int64_t)(q0 + j) * a.q_token + ((int64_t)head * a.group + rr - j * a.group) * a.q_head);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
                 const int piece = 2 * kk + half;
-                uint4 x = *(const uint4 *)(r < rows && piece < a.units ? q + 16 * piece : (const char *)kZeros);
-                if (a.flip) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
+                u32x4 x = mptkv::load<u32x4>(or_zeros(r < rows && piece < a.units, q + 16 * piece));
+                if (a.flip) x ^= 0x80008000u;
                 qf[nb][kk] = __builtin_bit_cast(s16x8, x);
             }
             int lo = see_lo[nb], hi = see_hi[nb];
             for (int d = 1; d < 32; d <<= 1) lo = max(lo, __shfl_xor(lo, d)), hi = min(hi, __shfl_xor(hi, d));
             wave_lo = max(wave_lo, lo), wave_hi = min(wave_hi, hi);
         }
+        wave_lo = __builtin_amdgcn_readfirstlane(wave_lo), wave_hi = __builtin_amdgcn_readfirstlane(wave_hi);
         // tokens that all rows of the tile see
-        int tile_lo, tile_hi;
-        {
-            const int ra = walk.tile * M, rb = min(ra + M, rows) - 1;
-            const int pa = len - n + ra / a.group, pb = len - n + rb / a.group;
-            tile_hi = a.causal ? min(len, pa + 1) : len;
-            tile_lo = a.window ? max(ent.begin[e], pb + 1 - a.window) : ent.begin[e];
-        }
-        f32x16 o[NB][DT];
+        const int pa = len - n + tile * M / a.group, pb = len - n + (min(tile * M + M, rows) - 1) / a.group;
+        const int tile_hi = a.causal ? min(len, pa + 1) : len, tile_lo = a.window ? max(begin, pb + 1 - a.window) : begin;
+
+        f32x16 o[NB][DT], s[NB];
+        s16x8 pf[NB][2];
         float m[NB], l[NB];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             m[nb] = -INFINITY, l[nb] = 0;
+            pf[nb][0] = pf[nb][1] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[nb][dt][r] = 0;
         }
 
-        // the thread's tokens of a step, its piece of their rows, their pages
-        const int own = tid / CH;
-        const int kp = (tid % CH) ^ W::k_swizzle(own), vp = (tid % CH) ^ W::v_swizzle(own);
+        // pages of the thread's tokens of a tile, and the tile's loads
         const char *kh = a.k + head * a.k_head + 16 * kp, *vh = a.v + head * a.v_head + 16 * vp;
-        const bool k_in = kp < a.units, v_in = vp < a.units;
-        int page[L];
-        auto find_pages = [&](int step) {
+        auto find_pages = [&](int step, int (&page)[L]) {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 const int t = step * BN + i * W::kStride + own;
                 page[i] = t >= range.lo && t < range.hi ? table[t >> shift] : -1;
             }
         };
-        auto load = [&](int step, char *kb, char *vb) {
+        auto load = [&](int step, const int (&page)[L], const char *rows0, bool in, uint32_t page_stride, uint32_t slot_stride, uint32_t lds) {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 const int t = step * BN + i * W::kStride + own;
                 const bool there = (unsigned)page[i] < (unsigned)c.n_pages;
                 if (!there && t >= range.lo && t < range.hi) flag(c, MPT_KV_BAD_PAGE);
-                const uint32_t slot = t & (c.page_size - 1);
-                load_lds16(there && k_in ? kh + row_at(page[i], slot, a.k_page, a.k_slot) : (const char *)kZeros, kb + (i * 4 + wave) * 1024);
-                load_lds16(there && v_in ? vh + row_at(page[i], slot, a.v_page, a.v_slot) : (const char *)kZeros, vb + (i * 4 + wave) * 1024);
+                load_lds16(or_zeros(there && in, rows0 + row_at(page[i], t & (c.page_size - 1), page_stride, slot_stride)), lds + i * 4096);
             }
         };
-        // scores and weights of a step
-        s16x8 pf[NB][MT * 2];
-        auto weigh = [&](int step, const char *kb) {
-            const int t0 = step * BN;
-            f32x16 s[MT][NB];
-            const int k_row = col * ROW, k_flip = half ^ W::k_swizzle(col);
+        // S' = K Q' of 32 tokens
+        auto multiply = [&](const char *kb) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[nb][r] = 0;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                const s16x8 kf = *(const s16x8 *)(kb + k_row + (((2 * kk) ^ k_flip) << 4));
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb] = Type<T>::mfma32(kf, qf[nb][kk], s[nb]);
+            }
+        };
+        // O' += V' P' of 32 tokens
+        auto add = [&](const char *vb) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const char *p = vb + g * 16 * ROW + v_row + (((dt * 4) ^ v_flip) << 4);
+                    const s16x4 x = read_column4(p), y = read_column4(p + 8 * ROW);
+                    const s16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) o[nb][dt] = Type<T>::mfma32(vf, pf[nb][g], o[nb][dt]);
+                }
+        };
+        // One step of 32 tokens from t0: products with the values of the step
+        // before beside this step's maximum, scores of the next step beside
+        // this step's weights.
+        auto step32 = [&](int t0, const char *k_next, const char *v_before) {
+            f32x16 x[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                x[nb] = s[nb];
+                if constexpr (CAP) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[nb][r] = score<true>(a, x[nb][r]);
+                }
+            }
+            if (t0 < wave_lo || t0 + 32 > wave_hi) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[mt][nb][r] = 0;
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    const s16x8 kf = *(const s16x8 *)(kb + mt * 32 * ROW + k_row + (((2 * kk) ^ k_flip) << 4));
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) s[mt][nb] = Type<T>::mfma32(kf, qf[nb][kk], s[mt][nb]);
-                }
+                    for (int r = 0; r < 16; ++r) {
+                        const int t = t0 + 4 * half + 8 * (r / 4) + r % 4;
+                        if (!(t >= see_lo[nb] && t < see_hi[nb])) x[nb][r] = -INFINITY;
+                    }
             }
-            // tokens that some row of the wave does not see
-            const bool masked = t0 < wave_lo || t0 + BN > wave_hi;
+            add(v_before);
+            float top[NB];
+            bool up = false;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
+                top[nb] = x[nb][0];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int r = 1; r < 16; ++r) top[nb] = fmaxf(top[nb], x[nb][r]);
+                if constexpr (!CAP) top[nb] = fmaxf(top[nb] * a.factor, -INFINITY);
+                up |= top[nb] > m[nb] + 8.0f;
+            }
+            if (__any(up)) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[mt][nb][r] = score<CAP>(a, s[mt][nb][r]);
-                if (masked) {
-                    const int t1 = t0 + 4 * half;
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int t = t1 + mt * 32 + 8 * (r / 4) + r % 4;
-                            if (!(t >= see_lo[nb] && t < see_hi[nb])) s[mt][nb][r] = -INFINITY;
-                        }
-                }
-                float top = -INFINITY;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[mt][nb][r]);
-                if (__any(top > m[nb] + 8.0f)) {
-                    top = fmaxf(top, __shfl_xor(top, 32));
-                    const float now = fmaxf(m[nb], top), keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[nb] - now);
+                for (int nb = 0; nb < NB; ++nb) {
+                    const float now = fmaxf(m[nb], fmaxf(top[nb], __shfl_xor(top[nb], 32)));
+                    const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[nb] - now);
                     m[nb] = now;
                     l[nb] *= keep;
 #pragma unroll
@@ -177,90 +191,115 @@ __global__ __launch_bounds__(256, NB == 2 || DP == 256 ? 1 : 2) void k_kv_wide(A
 #pragma unroll
                         for (int r = 0; r < 16; ++r) o[nb][dt][r] *= keep;
                 }
+            }
+            multiply(k_next);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
                 const float base = m[nb] == -INFINITY ? 0.0f : m[nb];
                 typename Type<T>::x8 p;
+                float sum[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float x = __builtin_amdgcn_exp2f(s[mt][nb][r] - base);
-                        l[nb] += x;
-                        p[r % 8] = (T)x;
-                        if (r % 8 == 7) pf[nb][mt * 2 + r / 8] = __builtin_bit_cast(s16x8, p);
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const float w = __builtin_amdgcn_exp2f(CAP ? x[nb][r] - base : __builtin_fmaf(x[nb][r], a.factor, -base));
+                    sum[r % 4] += w;
+                    p[r % 8] = (T)w;
+                    if (r % 8 == 7) pf[nb][r / 8] = __builtin_bit_cast(s16x8, p);
+                }
+                l[nb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             }
         };
-        // O' += V' P'
-        auto add = [&](const char *vb) {
-            const int row = 4 * half + (lane & 15) / 4;
-            const int v_row = row * ROW + (lane & 1) * 8, v_piece = ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
+        // Infinities and NaN in values of 32 tokens: a weight of zero does not
+        // cancel them in a row that does not see them. Rows that do see them
+        // get them added here, in memory, which costs the products no
+        // registers; then they are zeros for the product.
+        float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (from == 0)) * (M * (DP + 2)) + wave * NB * 32 * DP;
+        auto put_sums = [&]() {
 #pragma unroll
-            for (int g = 0; g < MT * 2; ++g)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const char *p = vb + g * 16 * ROW + v_row + (((dt * 4 + v_piece) ^ W::v_swizzle(row)) << 4);
-                    const s16x4 x = read_column4(p), y = read_column4(p + 8 * ROW);
-                    const s16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) o[nb][dt] = Type<T>::mfma32(vf, pf[nb][g], o[nb][dt]);
-                }
+                    for (int r = 0; r < 16; r += 4)
+                        *(f32x4 *)(sums + (((nb * DT + dt) * 4 + r / 4) * 64 + lane) * 4) =
+                            f32x4{o[nb][dt][r], o[nb][dt][r + 1], o[nb][dt][r + 2], o[nb][dt][r + 3]};
         };
-        // Infinities and NaN in values: a weight of zero does not cancel them
-        // in a row that does not see them. Rows that do see them get them
-        // added here; then they are zeros for the product.
-        auto odd_values = [&](int step, char *vb) {
+        auto odd_values = [&](int t0, char *vb) {
             uint32_t odd = 0;
 #pragma unroll 1
-            for (int x = tid; x < BN * CH; x += 256) odd |= odd8<T>(*(const s16x8 *)(vb + 16 * x));
+            for (int x = tid; x < 32 * CH; x += 256) odd |= odd8<T>(*(const s16x8 *)(vb + 16 * x));
             if (!__syncthreads_or(odd != 0)) return;
+            put_sums();
 #pragma unroll 1
-            for (int token = 0; token < BN; ++token)
+            for (int token = 0; token < 32; ++token)
+#pragma unroll 1
+                for (int x = 0; x < NB * DT * 4; ++x) {
+                    const int nb = x / (DT * 4), d = (x % (DT * 4)) * 8 + 4 * half, t = t0 + token;
+                    const s16x4 y = *(const s16x4 *)(vb + token * ROW + (((d / 8) ^ W::v_swizzle(token)) << 4) + (d % 8) * 2);
+                    const bool seen = t >= (nb ? see_lo[NB - 1] : see_lo[0]) && t < (nb ? see_hi[NB - 1] : see_hi[0]);
+                    float *p = sums + (x * 64 + lane) * 4;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (seen && !finite16<T>(y[i])) p[i] += value16<T>(y[i]);
+                }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                     for (int r = 0; r < 16; r += 4) {
-                        const int d = dt * 32 + 2 * r + 4 * half;
-                        const s16x4 x = *(const s16x4 *)(vb + token * ROW + (((d / 8) ^ W::v_swizzle(token)) << 4) + (d % 8) * 2);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float y = finite16<T>(x[i]) ? 0.0f : value16<T>(x[i]);
-#pragma unroll
-                            for (int nb = 0; nb < NB; ++nb)
-                                if (step * BN + token >= see_lo[nb] && step * BN + token < see_hi[nb]) o[nb][dt][r + i] += y;
-                        }
+                        const f32x4 y = *(const f32x4 *)(sums + (((nb * DT + dt) * 4 + r / 4) * 64 + lane) * 4);
+                        o[nb][dt][r] = y[0], o[nb][dt][r + 1] = y[1], o[nb][dt][r + 2] = y[2], o[nb][dt][r + 3] = y[3];
                     }
             __syncthreads();
 #pragma unroll 1
-            for (int x = tid; x < BN * CH * 8; x += 256) {
+            for (int x = tid; x < 32 * CH * 8; x += 256) {
                 short *p = (short *)vb + x;
                 if (!finite16<T>(*p)) *p = 0;
             }
             __syncthreads();
         };
-        auto compute = [&](int step, const char *kb, char *vb) {
-            if (active) weigh(step, kb);
-            if (step * BN < tile_lo || step * BN + BN > tile_hi) odd_values(step, vb);
-            if (active) add(vb);
-        };
+        auto partly_seen = [&](int t0) { return t0 < tile_lo || t0 + 32 > tile_hi; };
 
-        __syncthreads();                       // the previous tile's last products have read their buffers
-        find_pages(first);
-        load(first, k0, v0);
-        find_pages(first + 1);
-        for (int step = first; step < last; step += 2) {
+        // Tile i's keys are needed from the second half of tile i - 1 on, its
+        // values until the first half of tile i + 1: one barrier a tile, in
+        // its middle, and loads half a tile to a tile and a half ahead.
+        __syncthreads();                       // the previous rows' products have read their buffers
+        int page[L], ahead[L];
+        find_pages(first, page);
+        find_pages(first + 1, ahead);
+        load(first, page, kh, k_in, a.k_page, a.k_slot, k_lds);
+#pragma unroll
+        for (int i = 0; i < L; ++i) *(uint4 *)(values + TILE + (i * 256 + tid) * 16) = uint4{0, 0, 0, 0};   // "before"
+        arrived();
+        __syncthreads();
+        load(first, page, vh, v_in, a.v_page, a.v_slot, v_lds);
+        load(first + 1, ahead, kh, k_in, a.k_page, a.k_slot, k_lds + TILE);
+#pragma unroll
+        for (int i = 0; i < L; ++i) page[i] = ahead[i];
+        find_pages(first + 2, ahead);
+        if (active) multiply(keys);
+        for (int step = first; step < last; ++step) {
+            const int b = (step - first) & 1, t0 = step * BN;
+            char *k_now = keys + b * TILE, *k_next = keys + (b ^ 1) * TILE, *v_now = values + b * TILE, *v_before = values + (b ^ 1) * TILE;
+            if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, v_before + 32 * ROW);
+            if (active) step32(t0, k_now + 32 * ROW, v_before + 32 * ROW);
+            arrived();
             __syncthreads();
             if (step + 1 < last) {
-                load(step + 1, k1, v1);
-                find_pages(step + 2);
+                load(step + 1, page, vh, v_in, a.v_page, a.v_slot, v_lds + (b ^ 1) * TILE);
+                load(step + 2, ahead, kh, k_in, a.k_page, a.k_slot, k_lds + b * TILE);
+#pragma unroll
+                for (int i = 0; i < L; ++i) page[i] = ahead[i];
+                find_pages(step + 3, ahead);
             }
-            compute(step, k0, v0);
-            if (step + 1 >= last) break;
-            __syncthreads();
-            if (step + 2 < last) {
-                load(step + 2, k0, v0);
-                find_pages(step + 3);
-            }
-            compute(step + 1, k1, v1);
+            if (partly_seen(t0)) odd_values(t0, v_now);
+            if (active) step32(t0 + 32, k_next, v_now);
+        }
+        {
+            char *v_last = values + ((last - 1 - first) & 1) * TILE + 32 * ROW;
+            const int t0 = last * BN - 32;
+            if (partly_seen(t0)) odd_values(t0, v_last);
+            if (active) add(v_last);
         }
 
         const bool starts = from == 0, ends = last == range.first + range.count;
@@ -270,44 +309,39 @@ __global__ __launch_bounds__(256, NB == 2 || DP == 256 ? 1 : 2) void k_kv_wide(A
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     const float sum = l[nb] + __shfl_xor(l[nb], 32), scale = sum == 0 ? 0.0f : 1.0f / sum;
-                    if (out_at[nb] < 0) continue;
+                    const int r = row_base + nb * 32 + col, j = r / a.group;
+                    if (r >= rows) continue;
+                    const int64_t token = q0 + j, hq = (int64_t)head * a.group + r - j * a.group;
+                    const int64_t to = token * a.out_token + hq * a.out_head;
                     if (a.lse && half == 0)
-                        a.lse[lse_at[nb]] = sum == 0 ? -INFINITY : 0.693147180559945f * (m[nb] + __builtin_amdgcn_logf(sum));
+                        a.lse[token * a.heads + hq] = sum == 0 ? -INFINITY : 0.693147180559945f * (m[nb] + __builtin_amdgcn_logf(sum));
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                        for (int r = 0; r < 16; r += 4) {
-                            const int d = dt * 32 + 2 * r + 4 * half;
+                        for (int x = 0; x < 16; x += 4) {
+                            const int d = dt * 32 + 2 * x + 4 * half;
                             if (d < 8 * a.units)
-                                store4<T>(a, out_at[nb] + d, f32x4{o[nb][dt][r] * scale, o[nb][dt][r + 1] * scale,
-                                                                   o[nb][dt][r + 2] * scale, o[nb][dt][r + 3] * scale});
+                                store4<T>(a, to + d, f32x4{o[nb][dt][x] * scale, o[nb][dt][x + 1] * scale,
+                                                           o[nb][dt][x + 2] * scale, o[nb][dt][x + 3] * scale});
                         }
                 }
             }
         } else {
             // unnormalised sums, in the order of the registers
-            float *sums = a.sums + ((int64_t)walk.worker * 2 + (starts ? 1 : 0)) * (M * (DP + 2));
             if (active) {
+                put_sums();
+                float *st = sums - wave * NB * 32 * DP + M * DP + wave * NB * 64;
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    const int block = wave * NB + nb;
-                    float *p = sums + block * 32 * DP;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                        for (int r = 0; r < 16; r += 4)
-                            *(f32x4 *)(p + ((dt * 4 + r / 4) * 64 + lane) * 4) =
-                                f32x4{o[nb][dt][r], o[nb][dt][r + 1], o[nb][dt][r + 2], o[nb][dt][r + 3]};
                     const float sum = l[nb] + __shfl_xor(l[nb], 32);
-                    float *st = sums + M * DP + block * 64;
-                    st[lane] = half ? sum : m[nb];
+                    st[nb * 64 + lane] = half ? sum : m[nb];
                 }
             }
             if (!starts && tid == 0) {
                 const int64_t t0 = walk.tile_at;
                 const int w0 = Walk<M, BN>::owner(t0, walk.total, walk.workers);
                 const int w1 = Walk<M, BN>::owner(t0 + range.count - 1, walk.total, walk.workers);
-                if (w0 + 1 == walk.worker) a.parts[walk.worker] = Part{w1 - w0 + 1, e + walk.base, head, walk.tile, q0, n};
+                if (w0 + 1 == walk.worker) a.parts[walk.worker] = Part{w1 - w0 + 1, e + walk.base, head, tile, q0, n};
             }
         }
         if (ends && walk.at < walk.end) walk.next(a, ent);
