@@ -362,7 +362,7 @@ __device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
 inline int pad_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 // Launch of one kernel for the sizes of a call; false if the launch failed.
-void launch_wide(const Attn &a, int blocks32, hipStream_t s);
+void launch_wide(const Attn &a, hipStream_t s);
 void launch_narrow(const Attn &a, hipStream_t s);
 
 }  // namespace mptkv

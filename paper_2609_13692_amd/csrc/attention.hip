@@ -11,16 +11,15 @@ using mptlib::fail;
 
 // Which kernel, and how many workers: what the card holds at once.
 struct Choice {
-    int blocks32;            // 32-row blocks per wave of the wide kernel; 0: the narrow kernel
+    bool wide;
     int workers, rows;       // workgroups, rows of a tile
 };
 
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
-    if (rows <= 16) return {0, dim == 256 ? 512 : 768, 16};
-    if (rows <= 128 || dim == 256) return {1, dim == 256 ? 256 : 512, 128};
-    return {2, 256, 256};
+    if (rows <= 16) return {false, dim == 256 ? 512 : 768, 16};
+    return {true, dim == 256 ? 256 : 512, 128};
 }
 
 static size_t attention_bytes(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
@@ -85,8 +84,9 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
         a.factor = softcap > 0 ? std::fabs(scale) / softcap : std::fabs(scale) * log2e;
         a.cap = softcap * log2e;
         for (int i = 1; i < 3; ++i)
-            if (cache->k_stride[i] / 8 > UINT32_MAX || cache->v_stride[i] / 8 > UINT32_MAX)
-                return fail(MPT_E_INVALID, "cache: a stride of 64 GiB or more");
+            if (cache->k_stride[i] / 8 * (i == 2 ? cache->page_size : 1) > UINT32_MAX ||
+                cache->v_stride[i] / 8 * (i == 2 ? cache->page_size : 1) > UINT32_MAX)
+                return fail(MPT_E_INVALID, "cache: a page, or the stride of pages, of 64 GiB or more");
         a.k_page = (uint32_t)(cache->k_stride[1] / 8), a.k_slot = (uint32_t)(cache->k_stride[2] / 8);
         a.v_page = (uint32_t)(cache->v_stride[1] / 8), a.v_slot = (uint32_t)(cache->v_stride[2] / 8);
         a.k = (const char *)cache->k + 2 * layer * cache->k_stride[0];
@@ -95,8 +95,8 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
         a.workers = ch.workers;
         a.parts = (Part *)workspace;
         a.sums = (float *)((char *)workspace + mptlib::align256(sizeof(Part) * ch.workers));
-        if (ch.blocks32)
-            launch_wide(a, ch.blocks32, s);
+        if (ch.wide)
+            launch_wide(a, s);
         else
             launch_narrow(a, s);
         MPT_HIP_TRY(hipGetLastError());
