@@ -87,10 +87,11 @@ __device__ inline int tiles_of(const Attn &a, int n) {
 // Sizes of entries base .. base + 255; returns their units (all heads).
 template <int M, int BN>
 __device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = base + tid;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = base + tid;   // a thread each
+    const bool mine = tid < kEntries;
     const mpt_kv_cache &c = a.c;
-    int n = 0, len = 0, begin = 0, q0 = 0, slot = -1;
-    if (i < a.n) {
+    int n = 0, len = 0, begin = 0, q0 = 0, slot = 0;
+    if (mine && i < a.n) {
         q0 = a.q_off[i];
         const int q1 = a.q_off[i + 1];
         slot = a.seqs[i];
@@ -115,11 +116,11 @@ __device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
         for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
         if (lane == src) steps = x;
     }
-    s.q0[tid] = q0, s.n[tid] = n, s.len[tid] = len, s.begin[tid] = begin, s.slot[tid] = slot, s.steps[tid] = steps;
+    if (mine) s.q0[tid] = q0, s.n[tid] = n, s.len[tid] = len, s.begin[tid] = begin, s.slot[tid] = slot, s.steps[tid] = steps;
     int64_t sum = steps;
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
     __syncthreads();
-    if (lane == 0) s.wave[wave] = sum;
+    if (mine && lane == 0) s.wave[wave] = sum;
     __syncthreads();
     return (s.wave[0] + s.wave[1] + s.wave[2] + s.wave[3]) * c.n_heads;
 }
@@ -362,7 +363,7 @@ __device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
 inline int pad_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 // Launch of one kernel for the sizes of a call; false if the launch failed.
-void launch_wide(const Attn &a, hipStream_t s);
+void launch_wide(const Attn &a, int waves, hipStream_t s);
 void launch_narrow(const Attn &a, hipStream_t s);
 
 }  // namespace mptkv

@@ -11,15 +11,16 @@ using mptlib::fail;
 
 // Which kernel, and how many workers: what the card holds at once.
 struct Choice {
-    bool wide;
+    int waves;               // of a workgroup of the wide kernel, 32 rows each; 0: the narrow kernel
     int workers, rows;       // workgroups, rows of a tile
 };
 
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
-    if (rows <= 16) return {false, dim == 256 ? 512 : 768, 16};
-    return {true, dim == 256 ? 256 : 512, 128};
+    if (rows <= 16) return {0, dim == 256 ? 512 : 768, 16};
+    if (rows <= 128 || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
+    return {8, 256, 256};
 }
 
 static size_t attention_bytes(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
@@ -95,8 +96,8 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
         a.workers = ch.workers;
         a.parts = (Part *)workspace;
         a.sums = (float *)((char *)workspace + mptlib::align256(sizeof(Part) * ch.workers));
-        if (ch.wide)
-            launch_wide(a, s);
+        if (ch.waves)
+            launch_wide(a, ch.waves, s);
         else
             launch_narrow(a, s);
         MPT_HIP_TRY(hipGetLastError());

@@ -19,11 +19,15 @@
 
 namespace mptkv {
 
-template <int DP>
+// Lambdas whose bodies the compiler would rather call, with every register
+// that they touch put into memory.
+#define INLINE __attribute__((always_inline))
+
+template <int DP, int WAVES>
 struct Wide {
-    static constexpr int BN = 64, KK = DP / 16, DT = DP / 32, ROW = 2 * DP, CH = DP / 8;
-    static constexpr int kTile = BN * ROW, kLoads = kTile / 4096;     // 16-byte loads per thread, of keys or values
-    static constexpr int kStride = 256 / CH;                          // tokens between a thread's loads
+    static constexpr int kThreads = 64 * WAVES, BN = 64, KK = DP / 16, DT = DP / 32, ROW = 2 * DP, CH = DP / 8;
+    static constexpr int kTile = BN * ROW, kLoads = kTile / (16 * kThreads);   // 16-byte loads per thread, of keys or values
+    static constexpr int kStride = kThreads / CH;                          // tokens between a thread's loads
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight
     // tokens' pieces, values so that four tokens' 64 bytes, fall on all banks;
@@ -33,10 +37,10 @@ struct Wide {
     __device__ static int v_swizzle(int token) { return DP == 64 ? 4 * ((token >> 1) & 1) : 4 * (token & 3); }
 };
 
-template <class T, int DP, bool CAP>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
-    using W = Wide<DP>;
-    constexpr int M = 128, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, CH = W::CH, L = W::kLoads, TILE = W::kTile;
+template <class T, int DP, int WAVES, bool CAP>
+__global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
+    using W = Wide<DP, WAVES>;
+    constexpr int M = 32 * WAVES, THREADS = W::kThreads, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, CH = W::CH, L = W::kLoads, TILE = W::kTile;
     __shared__ Entries ent;
     __shared__ __attribute__((aligned(1024))) char keys[2 * TILE], values[2 * TILE];
     const mpt_kv_cache &c = a.c;
@@ -104,7 +108,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
         // The pages of the thread's tokens of a tile (of some token of the
         // range for those outside it, whose loads take zeros).
         const char *kh = a.k + head * a.k_head + 16 * kp, *vh = a.v + head * a.v_head + 16 * vp;
-        auto find_pages = [&](int step, int (&page)[L]) {
+        auto find_pages = [&](int step, int (&page)[L]) INLINE {
             if (step * BN >= range.lo && step * BN + BN <= range.hi) {
 #pragma unroll
                 for (int i = 0; i < L; ++i) page[i] = table[(step * BN + i * W::kStride + own) >> shift];
@@ -114,29 +118,29 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
                     page[i] = table[max(0, max(range.lo, min(range.hi - 1, step * BN + i * W::kStride + own))) >> shift];
             }
         };
-        auto load = [&](int step, const int (&page)[L], const char *rows0, bool in, const uint32_t (&slot)[L], uint32_t page_stride, uint32_t slot_stride, uint32_t lds) {
+        auto load = [&](int step, const int (&page)[L], const char *rows0, bool in, const uint32_t (&slot)[L], uint32_t page_stride, uint32_t slot_stride, uint32_t lds) INLINE {
             const char *tile0 = rows0 + ((uint64_t)((uint32_t)(step * BN) & (c.page_size - 1)) * slot_stride << 4);
-            auto all = [&](auto seen) {
+            auto all = [&](auto seen) INLINE {
 #pragma unroll
                 for (int i = 0; i < L; ++i) {
                     const bool there = (unsigned)page[i] < (unsigned)c.n_pages, see = seen(i);
                     lost |= see && !there;
                     const uint64_t u = (uint64_t)(uint32_t)page[i] * page_stride + slot[i];
-                    load_lds16(or_zeros(see && there && in, tile0 + (u << 4)), lds + i * 4096);
+                    load_lds16(or_zeros(see && there && in, tile0 + (u << 4)), lds + i * 16 * THREADS);
                 }
             };
             if (step * BN >= range.lo && step * BN + BN <= range.hi)
-                all([](int) { return true; });
+                all([](int) INLINE { return true; });
             else
-                all([&](int i) { return (unsigned)(step * BN + i * W::kStride + own - range.lo) < (unsigned)(range.hi - range.lo); });
+                all([&](int i) INLINE { return (unsigned)(step * BN + i * W::kStride + own - range.lo) < (unsigned)(range.hi - range.lo); });
         };
         // The products of a step, in groups that the compiler keeps in order:
         // an operand from LDS (read two groups ahead), its product, and beside
         // it a share of the step's other work.
         // S' = K Q' of 32 tokens
-        auto multiply = [&](const char *kb, auto beside) {
+        auto multiply = [&](const char *kb, auto beside) INLINE {
             s16x8 kf[3];
-            auto read = [&](int kk) { kf[kk % 3] = *(const s16x8 *)(kb + k_row + (((2 * kk) ^ k_flip) << 4)); };
+            auto read = [&](int kk) INLINE { kf[kk % 3] = *(const s16x8 *)(kb + k_row + (((2 * kk) ^ k_flip) << 4)); };
             read(0);
             read(1);
 #pragma unroll
@@ -148,9 +152,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
             }
         };
         // O' += V' P' of 32 tokens
-        auto add = [&](const char *vb, auto beside) {
+        auto add = [&](const char *vb, auto beside) INLINE {
             s16x8 vf[3];
-            auto read = [&](int i) {
+            auto read = [&](int i) INLINE {
                 const char *x = vb + (i / DT) * 16 * ROW + v_row + (((i % DT * 4) ^ v_flip) << 4);
                 const s16x4 y = read_column4(x), z = read_column4(x + 8 * ROW);
                 vf[i % 3] = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -165,11 +169,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        auto nothing = [](int) {};
+        auto nothing = [](int) INLINE {};
         // One step of 32 tokens from t0: products with the values of the step
         // before beside this step's maximum, scores of the next step beside
         // this step's weights.
-        auto step32 = [&](int t0, const char *k_next, const char *v_before) {
+        auto step32 = [&](int t0, const char *k_next, const char *v_before) INLINE {
             f32x16 x = s;
             if constexpr (CAP) {
 #pragma unroll
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
                 }
             }
             float top = -INFINITY;
-            add(v_before, [&](int i) {
+            add(v_before, [&](int i) INLINE {
                 constexpr int E = 8 / DT;
 #pragma unroll
                 for (int y = i * E; y < i * E + E; ++y) top = fmaxf(top, x[y]);
@@ -201,7 +205,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
             }
             const float base = m == -INFINITY ? 0.0f : m;
             typename Type<T>::x8 w8;
-            multiply(k_next, [&](int i) {
+            multiply(k_next, [&](int i) INLINE {
                 constexpr int E = 16 / KK;
 #pragma unroll
                 for (int r = i * E; r < i * E + E; ++r) {
@@ -217,17 +221,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
         // get them added here, in memory, which costs the products no
         // registers; then they are zeros for the product.
         float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (from == 0)) * (M * (DP + 2)) + wave * 32 * DP;
-        auto put_sums = [&]() {
+        auto put_sums = [&]() INLINE {
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4)
                     *(f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4) = f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]};
         };
-        auto odd_values = [&](int t0, char *vb) {
+        auto odd_values = [&](int t0, char *vb) INLINE {
             uint32_t odd = 0;
 #pragma unroll 1
-            for (int x = tid; x < 32 * CH; x += 256) odd |= odd8<T>(*(const s16x8 *)(vb + 16 * x));
+            for (int x = tid; x < 32 * CH; x += THREADS) odd |= odd8<T>(*(const s16x8 *)(vb + 16 * x));
             if (!__syncthreads_or(odd != 0)) return;
             put_sums();
 #pragma unroll 1
@@ -251,13 +255,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
                 }
             __syncthreads();
 #pragma unroll 1
-            for (int x = tid; x < 32 * CH * 8; x += 256) {
+            for (int x = tid; x < 32 * CH * 8; x += THREADS) {
                 short *y = (short *)vb + x;
                 if (!finite16<T>(*y)) *y = 0;
             }
             __syncthreads();
         };
-        auto partly_seen = [&](int t0) { return t0 < tile_lo || t0 + 32 > tile_hi; };
+        auto partly_seen = [&](int t0) INLINE { return t0 < tile_lo || t0 + 32 > tile_hi; };
 
         // Tile i's keys are needed from the second half of tile i - 1 on, its
         // values until the first half of tile i + 1: one barrier a tile, in
@@ -269,7 +273,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
         find_pages(first + 1, pages1);
         load(first, pages0, kh, k_in, k_slot, a.k_page, a.k_slot, k_lds);
 #pragma unroll
-        for (int i = 0; i < L; ++i) *(uint4 *)(values + TILE + (i * 256 + tid) * 16) = uint4{0, 0, 0, 0};   // "before"
+        for (int i = 0; i < L; ++i) *(uint4 *)(values + TILE + (i * THREADS + tid) * 16) = uint4{0, 0, 0, 0};   // "before"
         arrived();
         __syncthreads();
         load(first, pages0, vh, v_in, v_slot, a.v_page, a.v_slot, v_lds);
@@ -278,7 +282,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
         if (active) multiply(keys, nothing);
         // the pages of tile step + 1 and of step + 2; those of step + 3 take
         // the place of the first
-        auto one_tile = [&](int step, int (&next)[L], int (&after)[L], auto odd_tile) {
+        auto one_tile = [&](int step, int (&next)[L], int (&after)[L], auto odd_tile) INLINE {
             constexpr int B = decltype(odd_tile)::value;
             const int t0 = step * BN;
             if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, values + (1 - B) * TILE + 32 * ROW);
@@ -344,9 +348,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
 
 // Joins the parts of a tile: workgroup (w, block of 32 rows); the waves share
 // the dimensions.
-template <class T, int DP>
+template <class T, int DP, int WAVES>
 __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
-    constexpr int M = 128, DT = DP / 32;
+    constexpr int M = 32 * WAVES, DT = DP / 32;
     const int w = blockIdx.x, block = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const Part part = a.parts[w];
     if (part.count == 0) return;
@@ -386,30 +390,35 @@ __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
             }
 }
 
-template <class T, int DP>
+template <class T, int DP, int WAVES>
 static void launch(const Attn &a, hipStream_t s) {
     {
         mptlib::LaunchScope scope("k_kv_wide", (double)a.n_tokens * a.heads, s);
         if (a.cap != 0)
-            k_kv_wide<T, DP, true><<<a.workers, 256, 0, s>>>(a);
+            k_kv_wide<T, DP, WAVES, true><<<a.workers, 64 * WAVES, 0, s>>>(a);
         else
-            k_kv_wide<T, DP, false><<<a.workers, 256, 0, s>>>(a);
+            k_kv_wide<T, DP, WAVES, false><<<a.workers, 64 * WAVES, 0, s>>>(a);
     }
     mptlib::LaunchScope scope("k_kv_join_wide", a.workers, s);
-    k_kv_join_wide<T, DP><<<dim3(a.workers, 4), 256, 0, s>>>(a);
+    k_kv_join_wide<T, DP, WAVES><<<dim3(a.workers, WAVES), 256, 0, s>>>(a);
 }
 
 template <class T>
-static void launch_dim(const Attn &a, hipStream_t s) {
+static void launch_dim(const Attn &a, int waves, hipStream_t s) {
     const int dim = pad_dim(8 * a.units);
-    dim == 64 ? launch<T, 64>(a, s) : dim == 128 ? launch<T, 128>(a, s) : launch<T, 256>(a, s);
+    if (dim == 64)
+        waves == 8 ? launch<T, 64, 8>(a, s) : launch<T, 64, 4>(a, s);
+    else if (dim == 128)
+        waves == 8 ? launch<T, 128, 8>(a, s) : launch<T, 128, 4>(a, s);
+    else
+        launch<T, 256, 4>(a, s);
 }
 
-void launch_wide(const Attn &a, hipStream_t s) {
+void launch_wide(const Attn &a, int waves, hipStream_t s) {
     if (a.c.dtype == MPT_KV_BF16)
-        launch_dim<__bf16>(a, s);
+        launch_dim<__bf16>(a, waves, s);
     else
-        launch_dim<_Float16>(a, s);
+        launch_dim<_Float16>(a, waves, s);
 }
 
 }  // namespace mptkv
