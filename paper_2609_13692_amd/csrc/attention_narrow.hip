@@ -4,11 +4,14 @@
 //
 // The work is one pass over keys and values: 2 x 2 D bytes a token against
 // 16 x 4 D flops, a few hundredths of what the matrix cores could do, so a
-// wave only has to keep loads in flight. Keys go from memory to registers as
-// they are the operand of S' = K Q' (16x16x32); values go through registers to
-// the wave's own LDS, which transposes them into the operand of O' += V' P'.
-// The loads of the next step are issued when the registers of this one are
-// free, before its weights and products. No barrier until the tile's end.
+// wave only has to keep loads in flight. Loads take whole rows (neighbouring
+// lanes neighbouring bytes: read as the operand of a product needs them, 16
+// rows at a time, keys cost the address units four times the lookups and held
+// the kernel at 3.8 TB/s); the wave's own LDS then hands out keys as the operand of
+// S' = K Q' (16x16x32) and values, transposed, as that of O' += V' P'. A step
+// begins with its keys and values going to LDS and the next step's loads, which
+// then have all of its products and weights to arrive. No barrier until the
+// tile's end.
 
 #include "attention.h"
 
@@ -17,23 +20,24 @@ namespace mptkv {
 template <int DP>
 struct Narrow {
     static constexpr int M = 16, BN = 128, KK = DP / 32, DT = DP / 16, ROW = 2 * DP, CH = DP / 8;
-    static constexpr int kTile = 32 * ROW, L = kTile / 1024;           // a wave's values of a step; loads of 1 KiB
+    static constexpr int kTile = 32 * ROW, L = kTile / 1024;           // a wave's keys of a step; loads of 1 KiB
+    static constexpr int kShift = DP == 64 ? 3 : DP == 128 ? 4 : 5;    // log2 CH
 
-    // Eight tokens' 32 bytes fall on all banks.
+    // Eight tokens' 32 bytes, and their 16 bytes, fall on different banks.
     __device__ static int swizzle(int token) { return DP == 64 ? 2 * ((token >> 1) & 3) : 2 * (token & 7); }
 };
 
 template <class T, int DP, bool CAP, bool PAD>
-__global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void k_kv_narrow(Attn a) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
     using N = Narrow<DP>;
     constexpr int M = N::M, BN = N::BN, KK = N::KK, DT = N::DT, ROW = N::ROW, CH = N::CH, L = N::L;
     __shared__ Entries ent;
-    __shared__ __attribute__((aligned(1024))) char values[4 * N::kTile];
+    __shared__ __attribute__((aligned(1024))) char tiles[4 * 2 * N::kTile];
     __shared__ float stat[4][2][16];
     const mpt_kv_cache &c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
     const int shift = 31 - __clz(c.page_size);
-    char *vw = values + wave * N::kTile;
+    char *kw = tiles + wave * 2 * N::kTile, *vw = kw + N::kTile;      // the wave's keys and values
 
     Walk<M, BN> walk;
     if (!walk.begin(a, ent, 1)) return;
@@ -78,37 +82,29 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void k_kv_narrow(Attn a) {
             return t >= range.lo && t < range.hi ? table[t >> shift] : -1;
         };
         const char *kh = a.k + head * a.k_head, *vh = a.v + head * a.v_head;
-        s16x8 kf[2][KK];
-        u32x4 vr[L];
-        auto load = [&](int step, int pages) {
-            const int t0 = step * BN + wave * 32, ln = renewed(lane);
+        u32x4 kr[L], vr[L];
+        auto load = [&](int step, int pages) __attribute__((always_inline)) {
+            const int t0 = step * BN + wave * 32, ln = renewed(lane), piece = ln & (CH - 1);
             if ((unsigned)pages >= (unsigned)c.n_pages) {
                 if (t0 + (ln & 31) >= range.lo && t0 + (ln & 31) < range.hi) flag(c, MPT_KV_BAD_PAGE);
                 pages = -1;
             }
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-                const int t = mt * 16 + (ln & 15), q = ln >> 4, page = __shfl(pages, t);
-                const uint64_t at = row_at(page, (t0 + t) & (c.page_size - 1), a.k_page, a.k_slot);
-                if constexpr (PAD) {                               // past head_dim: the row's last piece, then zeros
-                    const char *x = or_zeros(page >= 0, kh + at);
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        const int piece = 4 * kk + q;
-                        const s16x8 y = mptkv::load<s16x8>(x + 16 * min(piece, a.units - 1));
-                        kf[mt][kk] = piece < a.units ? y : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-                    }
-                } else {
-                    const char *x = or_zeros(page >= 0, kh + at + 16 * q);
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) kf[mt][kk] = mptkv::load<s16x8>(x + 64 * kk);
-                }
-            }
+            const char *kx = kh + 16 * piece, *vx = vh + 16 * piece;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                const int t = i * (64 / CH) + (ln >> (DP == 64 ? 3 : DP == 128 ? 4 : 5)), piece = ln & (CH - 1), page = __shfl(pages, t);
-                const char *x = vh + row_at(page, (t0 + t) & (c.page_size - 1), a.v_page, a.v_slot) + 16 * piece;
-                vr[i] = mptkv::load<u32x4>(or_zeros(page >= 0 && (!PAD || piece < a.units), x));
+                const int t = i * (64 / CH) + (ln >> N::kShift), page = __shfl(pages, t);
+                const uint32_t slot = (t0 + t) & (c.page_size - 1);
+                const bool there = page >= 0 && (!PAD || piece < a.units);
+                kr[i] = mptkv::load<u32x4>(or_zeros(there, kx + row_at(page, slot, a.k_page, a.k_slot)));
+                vr[i] = mptkv::load<u32x4>(or_zeros(there, vx + row_at(page, slot, a.v_page, a.v_slot)));
+            }
+        };
+        auto put = [&](const u32x4 (&x)[L], char *to) __attribute__((always_inline)) {
+            const int ln = renewed(lane);
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int t = i * (64 / CH) + (ln >> N::kShift);
+                *(u32x4 *)(to + t * ROW + (((ln & (CH - 1)) ^ N::swizzle(t)) << 4)) = x[i];
             }
         };
 
@@ -117,7 +113,23 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void k_kv_narrow(Attn a) {
         pages = find_page(first + 1);
         for (int step = first; step < last; ++step) {
             const int t0 = step * BN + wave * 32, ln = renewed(lane);
+            put(kr, kw);
+            put(vr, vw);
+            if (step + 1 < last) {
+                load(step + 1, pages);
+                pages = find_page(step + 2);
+            }
+            if (t0 >= range.hi || t0 + 32 <= range.lo) continue;   // nothing for this wave
             float s[8];
+            s16x8 kf[2][KK];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    const int t = mt * 16 + (ln & 15);
+                    kf[mt][kk] = *(const s16x8 *)(kw + t * ROW + (((4 * kk + (ln >> 4)) ^ N::swizzle(t)) << 4));
+                }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
                 f32x4 x = {0, 0, 0, 0};
@@ -126,16 +138,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void k_kv_narrow(Attn a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[mt * 4 + i] = x[i];
             }
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const int t = i * (64 / CH) + (ln >> (DP == 64 ? 3 : DP == 128 ? 4 : 5));
-                *(u32x4 *)(vw + t * ROW + (((ln & (CH - 1)) ^ N::swizzle(t)) << 4)) = vr[i];
-            }
-            if (step + 1 < last) {
-                load(step + 1, pages);
-                pages = find_page(step + 2);
-            }
-            if (t0 >= range.hi || t0 + 32 <= range.lo) continue;   // nothing for this wave
             const bool masked = t0 < all_lo || t0 + 32 > all_hi;
             float top = -INFINITY;
 #pragma unroll
@@ -191,12 +193,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void k_kv_narrow(Attn a) {
                 }
             }
             const int row = ln >> 2;                               // 4 quad + col / 4
+            s16x8 vf[DT];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const char *q = vw + row * ROW + (((dt * 2 + (ln & 3) / 2) ^ N::swizzle(row)) << 4) + (ln & 1) * 8;
                 const s16x4 x = read_column4(q), y = read_column4(q + 16 * ROW);
-                o[dt] = Type<T>::mfma16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), pf, o[dt]);
+                vf[dt] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
             }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = Type<T>::mfma16(vf[dt], pf, o[dt]);
         }
 
         // the waves' parts: each in its own LDS, DT vectors of 1 KiB
@@ -224,7 +230,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void k_kv_narrow(Attn a) {
             const int dt = k * 4 + wave;
             f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) x += f[w] * *(const f32x4 *)(values + w * N::kTile + dt * 1024 + lane * 16);
+            for (int w = 0; w < 4; ++w) x += f[w] * *(const f32x4 *)(tiles + (2 * w + 1) * N::kTile + dt * 1024 + lane * 16);
             x *= scale;
             if (starts && ends) {
                 const int d = dt * 16 + 4 * quad;
