@@ -39,12 +39,6 @@ struct Attn {
     float *sums;                                      // [workers][2][tile rows * (padded dim + 2)]
 };
 
-// A value that is the same in all lanes, in scalar registers.
-__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ inline int64_t uniform(int64_t x) {
-    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
-}
-
 // What a worker's first tile is, if it is the second worker of that tile:
 // the join's work list.
 struct Part {
@@ -79,6 +73,13 @@ __device__ inline Range tile_range(const Attn &a, int n, int len, int begin, int
     return g;
 }
 
+// Tokens [lo, hi) that all rows first .. last of an entry see.
+__device__ inline void seen_by_all(const Attn &a, int n, int len, int begin, int first, int last, int &lo, int &hi) {
+    const int p0 = len - n + first / a.group, p1 = len - n + last / a.group;
+    hi = a.causal ? min(len, p0 + 1) : len;
+    lo = a.window ? max(begin, p1 + 1 - a.window) : begin;
+}
+
 template <int M>
 __device__ inline int tiles_of(const Attn &a, int n) {
     return (n * a.group + M - 1) / M;
@@ -110,15 +111,15 @@ __device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
     // long entries: the lanes of a wave take the tiles
     for (uint64_t todo = __ballot(tiles > 8); todo; todo &= todo - 1) {
         const int src = __ffsll((unsigned long long)todo) - 1;
-        const int n2 = __shfl(n, src), len2 = __shfl(len, src), begin2 = __shfl(begin, src);
+        const int n2 = __builtin_amdgcn_readlane(n, src), len2 = __builtin_amdgcn_readlane(len, src);
+        const int begin2 = __builtin_amdgcn_readlane(begin, src);
         int64_t x = 0;
         for (int t = lane; t < tiles_of<M>(a, n2); t += 64) x += tile_range<M, BN>(a, n2, len2, begin2, t).count;
-        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+        x = of_lane(wave_sums(x), 63);
         if (lane == src) steps = x;
     }
     if (mine) s.q0[tid] = q0, s.n[tid] = n, s.len[tid] = len, s.begin[tid] = begin, s.slot[tid] = slot, s.steps[tid] = steps;
-    int64_t sum = steps;
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    const int64_t sum = of_lane(wave_sums(steps), 63);
     __syncthreads();
     if (mine && lane == 0) s.wave[wave] = sum;
     __syncthreads();
@@ -172,19 +173,15 @@ struct Walk {
         const int lane = tid & 63;
         e = 0;
         for (;;) {
-            int64_t x = s.steps[e + lane] * a.c.n_heads, y = x;
-            for (int d = 1; d < 64; d <<= 1) {
-                const int64_t z = __shfl_up(y, d);
-                if (lane >= d) y += z;
-            }
+            const int64_t x = s.steps[e + lane] * a.c.n_heads, y = wave_sums(x);
             const uint64_t past = __ballot(before + y > at);
             if (past) {
                 const int k2 = __ffsll((unsigned long long)past) - 1;
-                before += uniform(__shfl(y - x, k2));
+                before += of_lane(y - x, k2);
                 e += k2;
                 break;
             }
-            before += uniform(__shfl(y, 63));
+            before += of_lane(y, 63);
             e += 64;
         }
         const int64_t in = at - before, steps = uniform(s.steps[e]);
@@ -199,19 +196,15 @@ struct Walk {
         int64_t sum = 0;
         for (tile = 0;; tile += 64) {
             const int64_t x = tile + lane < tiles ? tile_range<M, BN>(a, s.n[e], s.len[e], s.begin[e], tile + lane).count : 0;
-            int64_t y = x;
-            for (int d = 1; d < 64; d <<= 1) {
-                const int64_t z = __shfl_up(y, d);
-                if (lane >= d) y += z;
-            }
+            const int64_t y = wave_sums(x);
             const uint64_t past = __ballot(sum + y > step);
             if (past) {
                 const int k = __ffsll((unsigned long long)past) - 1;
                 tile += k;
-                tile_at = before + head * uniform(s.steps[e]) + sum + uniform(__shfl(y - x, k));
+                tile_at = before + head * uniform(s.steps[e]) + sum + of_lane(y - x, k);
                 return;
             }
-            sum += uniform(__shfl(y, 63));
+            sum += of_lane(y, 63);
         }
     }
 

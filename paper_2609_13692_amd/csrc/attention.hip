@@ -18,7 +18,7 @@ struct Choice {
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
-    if (rows <= 16) return {0, dim == 256 ? 256 : 512, 16};
+    if (rows <= 16) return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
     if (rows <= 128 || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
     return {8, 256, 256};
 }

@@ -55,9 +55,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
         const int see_hi = a.causal ? min(len, p + 1) : len;
         const int see_lo = a.window ? max(begin, p + 1 - a.window) : begin;
         const int64_t token = q0 + j, hh = (int64_t)head * a.group + hq;
-        int all_lo = see_lo, all_hi = see_hi;
-        for (int d = 1; d < 16; d <<= 1) all_lo = max(all_lo, __shfl_xor(all_lo, d)), all_hi = min(all_hi, __shfl_xor(all_hi, d));
-        all_lo = uniform(all_lo), all_hi = uniform(all_hi);
+        int all_lo, all_hi;
+        seen_by_all(a, n, len, begin, tile * M, min(tile * M + M, rows) - 1, all_lo, all_hi);
         s16x8 qf[KK];
         {
             const char *q = a.q + 2 * (token * a.q_token + hh * a.q_head);
@@ -255,39 +254,71 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
     }
 }
 
-// Joins the parts of a tile, as k_kv_join_wide: workgroup w, the waves share
-// the dimensions.
+// Joins the parts of a tile: workgroup (w, 16 dimensions). The waves share the
+// parts, four at a time in flight (one after the other, their latencies would
+// add up to more than the attention of a short context).
 template <class T, int DP>
 __global__ __launch_bounds__(256) void k_kv_join_narrow(Attn a) {
-    constexpr int M = 16, DT = DP / 16, K = DT / 4;
-    const int w = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
+    constexpr int M = 16;
+    __shared__ float stat[4][2][16];
+    __shared__ f32x4 other[4][64];
+    const int w = blockIdx.x, dt = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
     const Part part = a.parts[w];
     if (part.count == 0) return;
+    // part i: worker w - 1 + i; the first one's second slot, the others' first
     auto sums = [&](int i) { return a.sums + ((int64_t)(w - 1 + i) * 2 + (i == 0)) * (M * (DP + 2)); };
-    float m = -INFINITY;
-    for (int i = 0; i < part.count; ++i) m = fmaxf(m, sums(i)[M * DP + col]);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0;
-    f32x4 o[K] = {};
-    for (int i = 0; i < part.count; ++i) {
-        const float *p = sums(i);
-        const float f = __builtin_amdgcn_exp2f(p[M * DP + col] - base);
-        l += p[M * DP + 16 + col] * f;
+    float m = -INFINITY, l = 0;
+    f32x4 o = {0, 0, 0, 0};
+    for (int i = wave; i < part.count; i += 16) {
+        float pm[4], pl[4];
+        f32x4 po[4];
 #pragma unroll
-        for (int k = 0; k < K; ++k) o[k] += f * *(const f32x4 *)(p + ((k * 4 + wave) * 64 + lane) * 4);
+        for (int k = 0; k < 4; ++k) {
+            const bool there = i + 4 * k < part.count;
+            const float *p = sums(there ? i + 4 * k : i);
+            pm[k] = there ? p[M * DP + col] : -INFINITY;
+            pl[k] = p[M * DP + 16 + col];
+            po[k] = *(const f32x4 *)(p + (dt * 64 + lane) * 4);
+        }
+        float now = m;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) now = fmaxf(now, pm[k]);
+        const float base = now == -INFINITY ? 0.0f : now, keep = __builtin_amdgcn_exp2f(m - base);
+        l *= keep;
+        o *= keep;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = __builtin_amdgcn_exp2f(pm[k] - base);
+            if (i + 4 * k < part.count) {
+                l += f * pl[k];
+                o += f * po[k];
+            }
+        }
+        m = now;
+    }
+    if (quad == 0) stat[wave][0][col] = m, stat[wave][1][col] = l;
+    other[wave][lane] = o;
+    __syncthreads();
+    if (wave) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, stat[k][0][col]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    l = 0;
+    o = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float f = __builtin_amdgcn_exp2f(stat[k][0][col] - base);
+        l += f * stat[k][1][col];
+        o += f * other[k][lane];
     }
     const int rows = part.n * a.group, r = part.tile * M + col;
     if (r >= rows) return;
-    const int j = r / a.group;
+    const int j = r / a.group, d = dt * 16 + 4 * quad;
     const int64_t token = part.q0 + j, h = (int64_t)part.head * a.group + r - j * a.group;
-    const float scale = l == 0 ? 0.0f : 1.0f / l;
-    if (a.lse && wave == 0 && quad == 0)
-        a.lse[token * a.heads + h] = l == 0 ? -INFINITY : 0.693147180559945f * (m + __builtin_amdgcn_logf(l));
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int d = (k * 4 + wave) * 16 + 4 * quad;
-        if (d < 8 * a.units) store4<T>(a, token * a.out_token + h * a.out_head + d, o[k] * scale);
-    }
+    if (a.lse && dt == 0 && quad == 0)
+        a.lse[token * a.heads + h] = l == 0 ? -INFINITY : 0.693147180559945f * (top + __builtin_amdgcn_logf(l));
+    if (d < 8 * a.units) store4<T>(a, token * a.out_token + h * a.out_head + d, o * (l == 0 ? 0.0f : 1.0f / l));
 }
 
 template <class T, int DP>
@@ -300,7 +331,7 @@ static void launch(const Attn &a, hipStream_t s) {
         kernel<<<a.workers, 256, 0, s>>>(a);
     }
     mptlib::LaunchScope scope("k_kv_join_narrow", a.workers, s);
-    k_kv_join_narrow<T, DP><<<a.workers, 256, 0, s>>>(a);
+    k_kv_join_narrow<T, DP><<<dim3(a.workers, (a.units + 1) / 2), 256, 0, s>>>(a);
 }
 
 template <class T>

@@ -89,12 +89,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             if (a.flip) x ^= 0x80008000u;
             qf[kk] = __builtin_bit_cast(s16x8, x);
         }
-        int wave_lo = see_lo, wave_hi = see_hi;                       // tokens that all rows of the wave see
-        for (int d = 1; d < 32; d <<= 1) wave_lo = max(wave_lo, __shfl_xor(wave_lo, d)), wave_hi = min(wave_hi, __shfl_xor(wave_hi, d));
-        wave_lo = uniform(wave_lo), wave_hi = uniform(wave_hi);
-        // ... all rows of the tile
-        const int pa = len - n + tile * M / a.group, pb = len - n + (min(tile * M + M, rows) - 1) / a.group;
-        const int tile_hi = a.causal ? min(len, pa + 1) : len, tile_lo = a.window ? max(begin, pb + 1 - a.window) : begin;
+        // tokens that all rows of the wave, and of the tile, see
+        int wave_lo, wave_hi, tile_lo, tile_hi;
+        seen_by_all(a, n, len, begin, min(row_base, rows - 1), min(row_base + 31, rows - 1), wave_lo, wave_hi);
+        seen_by_all(a, n, len, begin, tile * M, min(tile * M + M, rows) - 1, tile_lo, tile_hi);
 
         f32x16 o[DT], s;
         s16x8 pf[2];
@@ -358,21 +356,43 @@ __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
     if (part.tile * M + block * 32 >= rows) return;
     // part i: worker w - 1 + i; the first one's second slot, the others' first
     auto sums = [&](int i) { return a.sums + ((int64_t)(w - 1 + i) * 2 + (i == 0)) * (M * (DP + 2)); };
-    float m = -INFINITY;
-    for (int i = 0; i < part.count; ++i) m = fmaxf(m, sums(i)[M * DP + block * 64 + (lane & 31)]);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0;
+    float m = -INFINITY, l = 0;
     f32x4 o[(DT + 3) / 4][4] = {};
-    for (int i = 0; i < part.count; ++i) {
-        const float *p = sums(i), *st = p + M * DP + block * 64 + (lane & 31);
-        const float f = __builtin_amdgcn_exp2f(st[0] - base);
-        l += st[32] * f;
+    for (int i = 0; i < part.count; i += 2) {
+        float pm[2], pl[2];
+        f32x4 po[2][(DT + 3) / 4][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const bool there = i + u < part.count;
+            const float *p = sums(there ? i + u : i), *st = p + M * DP + block * 64 + (lane & 31);
+            pm[u] = there ? st[0] : -INFINITY;
+            pl[u] = st[32];
+#pragma unroll
+            for (int k = 0; k < (DT + 3) / 4; ++k)
+                if (wave + 4 * k < DT)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        po[u][k][x] = *(const f32x4 *)(p + block * 32 * DP + (((wave + 4 * k) * 4 + x) * 64 + lane) * 4);
+        }
+        const float now = fmaxf(m, fmaxf(pm[0], pm[1])), base = now == -INFINITY ? 0.0f : now;
+        const float keep = __builtin_amdgcn_exp2f(m - base);
+        l *= keep;
 #pragma unroll
         for (int k = 0; k < (DT + 3) / 4; ++k)
-            if (wave + 4 * k < DT)
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    o[k][x] += f * *(const f32x4 *)(p + block * 32 * DP + (((wave + 4 * k) * 4 + x) * 64 + lane) * 4);
+            for (int x = 0; x < 4; ++x) o[k][x] *= keep;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (i + u >= part.count) break;
+            const float f = __builtin_amdgcn_exp2f(pm[u] - base);
+            l += f * pl[u];
+#pragma unroll
+            for (int k = 0; k < (DT + 3) / 4; ++k)
+                if (wave + 4 * k < DT)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[k][x] += f * po[u][k][x];
+        }
+        m = now;
     }
     if (r >= rows) return;
     const int j = r / a.group;

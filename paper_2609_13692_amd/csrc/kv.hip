@@ -50,11 +50,7 @@ static Plan plan_at(const mpt_kv_cache &c, void *ws) {
 // Exclusive sum over the workgroup's 1024 threads; *total is the whole sum.
 __device__ inline int64_t block_scan(int64_t v, int64_t *total, int64_t *lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    const int64_t x = wave_sums(v);
     if (lane == 63) lds[wave] = x;
     __syncthreads();
     int64_t before = 0, all = 0;
