@@ -290,7 +290,17 @@ __device__ inline V load(const char *from) {
 __device__ inline void load_lds16(const char *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory");
 }
-__device__ inline void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// The same with 4 bytes per lane.
+__device__ inline void load_lds4(const void *from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory");
+}
+// Waits until at most N of the wave's later loads are on their way: loads
+// arrive in order, so all before those N have.
+template <int N>
+__device__ inline void arrived() {
+    static_assert(N >= 0 && N < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 __device__ inline uint32_t lds_address(const void *p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
@@ -316,7 +326,7 @@ __device__ inline float score(const Attn &a, float x) {
     if constexpr (!CAP) return x * a.factor;
     const float z = x * a.factor, y = z * z;
     const float e = __builtin_amdgcn_exp2f(2.885390081777927f * z);
-    const float big = 1.0f - 2.0f / (1.0f + e);
+    const float big = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e);
     const float small = z * (1.0f + y * (-0.333333333f + y * (0.133333333f + y * (-0.053968254f + y * 0.021869489f))));
     return a.cap * (fabsf(z) < 0.25f ? small : big);
 }

@@ -6,16 +6,14 @@
 // query are values of its own two lanes, and the weights, rounded, are the
 // second operand of O' += V' P' as they lie (the tokens of a product may come
 // in any order if both operands agree on it). Keys and values go from memory
-// to LDS directly, one tile of 64 tokens (32 at 256 dimensions) ahead of the
-// products; values are read back by the transposing LDS loads.
+// to LDS directly, one to three tiles of 64 tokens ahead of the products;
+// values are read back by the transposing LDS loads.
 //
 // The maximum that weights are taken against is moved only when a score
 // exceeds it by 2^8: products with weights up to 256 are as exact, and the
 // sums are rescaled a few times per row instead of at every step.
 
 #include "attention.h"
-
-#include <type_traits>
 
 namespace mptkv {
 
@@ -27,7 +25,13 @@ template <int DP, int WAVES>
 struct Wide {
     static constexpr int kThreads = 64 * WAVES, BN = 64, KK = DP / 16, DT = DP / 32, ROW = 2 * DP, CH = DP / 8;
     static constexpr int kTile = BN * ROW, kLoads = kTile / (16 * kThreads);   // 16-byte loads per thread, of keys or values
-    static constexpr int kStride = kThreads / CH;                          // tokens between a thread's loads
+    static constexpr int kStride = kThreads / CH;                       // tokens between a thread's loads
+    // Tiles of keys (and of values) in LDS: two where two workgroups share a
+    // CU or rows are long, else four. Page ids are fetched for twice as many.
+    static constexpr int S = WAVES == 8 ? 4 : 2, IDS = 2 * S;
+    // Operands read from LDS ahead of their products: with one wave to a SIMD
+    // nothing else covers the latency.
+    static constexpr int kAhead = DP == 256 ? 6 : 2;
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight
     // tokens' pieces, values so that four tokens' 64 bytes, fall on all banks;
@@ -41,12 +45,15 @@ template <class T, int DP, int WAVES, bool CAP>
 __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
     using W = Wide<DP, WAVES>;
     constexpr int M = 32 * WAVES, THREADS = W::kThreads, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, CH = W::CH, L = W::kLoads, TILE = W::kTile;
+    constexpr int S = W::S, IDS = W::IDS, AHEAD = W::kAhead;
     __shared__ Entries ent;
-    __shared__ __attribute__((aligned(1024))) char keys[2 * TILE], values[2 * TILE];
+    __shared__ __attribute__((aligned(1024))) char keys[S * TILE], values[S * TILE];
+    __shared__ __attribute__((aligned(256))) int ids[WAVES * IDS * BN];       // each wave its own
     const mpt_kv_cache &c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
     const int shift = 31 - __clz(c.page_size);
     const uint32_t k_lds = uniform((int)(lds_address(keys) + wave * 1024)), v_lds = uniform((int)(lds_address(values) + wave * 1024));
+    const uint32_t id_lds = uniform((int)(lds_address(ids) + wave * IDS * BN * 4));
     // the thread's tokens of a tile are kStride apart from `own` on; its pieces
     // of their rows; the rows' places in a page whose slots are counted from
     // the tile's first (a tile is a part of a page, or pages are of the tile)
@@ -103,28 +110,24 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[dt][r] = 0;
 
-        // The pages of the thread's tokens of a tile (of some token of the
-        // range for those outside it, whose loads take zeros).
+        // The pages of a tile's tokens (of some token of the range for those
+        // outside it, whose loads take zeros), and its keys or values.
         const char *kh = a.k + head * a.k_head + 16 * kp, *vh = a.v + head * a.v_head + 16 * vp;
-        auto find_pages = [&](int step, int (&page)[L]) INLINE {
-            if (step * BN >= range.lo && step * BN + BN <= range.hi) {
-#pragma unroll
-                for (int i = 0; i < L; ++i) page[i] = table[(step * BN + i * W::kStride + own) >> shift];
-            } else {
-#pragma unroll
-                for (int i = 0; i < L; ++i)
-                    page[i] = table[max(0, max(range.lo, min(range.hi - 1, step * BN + i * W::kStride + own))) >> shift];
-            }
+        auto fetch_ids = [&](int step) INLINE {
+            const int t = max(0, max(range.lo, min(range.hi - 1, step * BN + lane)));
+            load_lds4(table + (t >> shift), id_lds + (step & (IDS - 1)) * BN * 4);
         };
-        auto load = [&](int step, const int (&page)[L], const char *rows0, bool in, const uint32_t (&slot)[L], uint32_t page_stride, uint32_t slot_stride, uint32_t lds) INLINE {
+        auto load = [&](int step, const char *rows0, bool in, const uint32_t (&slot)[L], uint32_t page_stride, uint32_t slot_stride, uint32_t lds) INLINE {
             const char *tile0 = rows0 + ((uint64_t)((uint32_t)(step * BN) & (c.page_size - 1)) * slot_stride << 4);
+            const int *page = ids + (wave * IDS + (step & (IDS - 1))) * BN + own;
             auto all = [&](auto seen) INLINE {
 #pragma unroll
                 for (int i = 0; i < L; ++i) {
-                    const bool there = (unsigned)page[i] < (unsigned)c.n_pages, see = seen(i);
+                    const int id = page[i * W::kStride];
+                    const bool there = (unsigned)id < (unsigned)c.n_pages, see = seen(i);
                     lost |= see && !there;
-                    const uint64_t u = (uint64_t)(uint32_t)page[i] * page_stride + slot[i];
-                    load_lds16(or_zeros(see && there && in, tile0 + (u << 4)), lds + i * 16 * THREADS);
+                    const uint64_t u = (uint64_t)(uint32_t)id * page_stride + slot[i];
+                    load_lds16(or_zeros(see && there && in, tile0 + (u << 4)), lds + (step & (S - 1)) * TILE + i * 16 * THREADS);
                 }
             };
             if (step * BN >= range.lo && step * BN + BN <= range.hi)
@@ -132,37 +135,39 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             else
                 all([&](int i) INLINE { return (unsigned)(step * BN + i * W::kStride + own - range.lo) < (unsigned)(range.hi - range.lo); });
         };
+        auto load_keys = [&](int step) INLINE { load(step, kh, k_in, k_slot, a.k_page, a.k_slot, k_lds); };
+        auto load_values = [&](int step) INLINE { load(step, vh, v_in, v_slot, a.v_page, a.v_slot, v_lds); };
         // The products of a step, in groups that the compiler keeps in order:
-        // an operand from LDS (read two groups ahead), its product, and beside
+        // an operand from LDS (read some groups ahead), its product, and beside
         // it a share of the step's other work.
         // S' = K Q' of 32 tokens
         auto multiply = [&](const char *kb, auto beside) INLINE {
-            s16x8 kf[3];
-            auto read = [&](int kk) INLINE { kf[kk % 3] = *(const s16x8 *)(kb + k_row + (((2 * kk) ^ k_flip) << 4)); };
-            read(0);
-            read(1);
+            s16x8 kf[AHEAD + 1];
+            auto read = [&](int kk) INLINE { kf[kk % (AHEAD + 1)] = *(const s16x8 *)(kb + k_row + (((2 * kk) ^ k_flip) << 4)); };
+#pragma unroll
+            for (int kk = 0; kk < AHEAD; ++kk) read(kk);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                if (kk + 2 < KK) read(kk + 2);
-                s = Type<T>::mfma32(kf[kk % 3], qf[kk], kk ? s : f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
+                if (kk + AHEAD < KK) read(kk + AHEAD);
+                s = Type<T>::mfma32(kf[kk % (AHEAD + 1)], qf[kk], kk ? s : f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
                 beside(kk);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
         // O' += V' P' of 32 tokens
         auto add = [&](const char *vb, auto beside) INLINE {
-            s16x8 vf[3];
+            s16x8 vf[AHEAD + 1];
             auto read = [&](int i) INLINE {
                 const char *x = vb + (i / DT) * 16 * ROW + v_row + (((i % DT * 4) ^ v_flip) << 4);
                 const s16x4 y = read_column4(x), z = read_column4(x + 8 * ROW);
-                vf[i % 3] = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
+                vf[i % (AHEAD + 1)] = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
             };
-            read(0);
-            read(1);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read(i);
 #pragma unroll
             for (int i = 0; i < 2 * DT; ++i) {
-                if (i + 2 < 2 * DT) read(i + 2);
-                o[i % DT] = Type<T>::mfma32(vf[i % 3], pf[i / DT], o[i % DT]);
+                if (i + AHEAD < 2 * DT) read(i + AHEAD);
+                o[i % DT] = Type<T>::mfma32(vf[i % (AHEAD + 1)], pf[i / DT], o[i % DT]);
                 beside(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -251,6 +256,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                     const f32x4 y = *(const f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4);
                     o[dt][r] = y[0], o[dt][r + 1] = y[1], o[dt][r + 2] = y[2], o[dt][r + 3] = y[3];
                 }
+            // the wait for these loads here: where the paths meet it would
+            // hold up every step for all loads to LDS
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) asm volatile("" : "+v"(o[dt]));
             __syncthreads();
 #pragma unroll 1
             for (int x = tid; x < 32 * CH * 8; x += THREADS) {
@@ -263,46 +272,53 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
 
         // Tile i's keys are needed from the second half of tile i - 1 on, its
         // values until the first half of tile i + 1: one barrier a tile, in
-        // its middle, and loads half a tile to a tile and a half ahead. pages0
-        // and pages1: of the even and odd tiles from `first`.
+        // its middle. Turn i, after that of tile i, fetches the page ids of
+        // tile i + 2 S - 1, the values of i + S - 1 and the keys of i + S: PER
+        // loads a wave. Turns first - S .. first - 1 come before the loop.
+        constexpr int PER = 2 * L + 1;
         __syncthreads();                       // the previous rows' products have read their buffers
-        int pages0[L], pages1[L];
-        find_pages(first, pages0);
-        find_pages(first + 1, pages1);
-        load(first, pages0, kh, k_in, k_slot, a.k_page, a.k_slot, k_lds);
 #pragma unroll
-        for (int i = 0; i < L; ++i) *(uint4 *)(values + TILE + (i * THREADS + tid) * 16) = uint4{0, 0, 0, 0};   // "before"
-        arrived();
+        for (int i = 0; i < S; ++i) fetch_ids(first + i);
+#pragma unroll
+        for (int i = 0; i < L; ++i)            // the values "before" the first tile
+            *(uint4 *)(values + ((first - 1) & (S - 1)) * TILE + (i * THREADS + tid) * 16) = uint4{0, 0, 0, 0};
+        arrived<0>();
+        load_keys(first);
+#pragma unroll
+        for (int i = 1; i < S; ++i) {
+            fetch_ids(first + S - 1 + i);
+            if (first + i - 1 < last) load_values(first + i - 1);
+            if (first + i < last) load_keys(first + i);
+        }
+        if (first + S - 1 < last)
+            arrived<(S - 1) * PER>();
+        else
+            arrived<0>();
         __syncthreads();
-        load(first, pages0, vh, v_in, v_slot, a.v_page, a.v_slot, v_lds);
-        load(first + 1, pages1, kh, k_in, k_slot, a.k_page, a.k_slot, k_lds + TILE);
-        find_pages(first + 2, pages0);
-        if (active) multiply(keys, nothing);
-        // the pages of tile step + 1 and of step + 2; those of step + 3 take
-        // the place of the first
-        auto one_tile = [&](int step, int (&next)[L], int (&after)[L], auto odd_tile) INLINE {
-            constexpr int B = decltype(odd_tile)::value;
+        if (active) multiply(keys + (first & (S - 1)) * TILE, nothing);
+        for (int step = first; step < last; ++step) {
             const int t0 = step * BN;
-            if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, values + (1 - B) * TILE + 32 * ROW);
-            if (active) step32(t0, keys + B * TILE + 32 * ROW, values + (1 - B) * TILE + 32 * ROW);
-            arrived();
+            char *k_now = keys + (step & (S - 1)) * TILE, *k_next = keys + ((step + 1) & (S - 1)) * TILE;
+            char *v_now = values + (step & (S - 1)) * TILE, *v_before = values + ((step - 1) & (S - 1)) * TILE;
+            if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, v_before + 32 * ROW);
+            if (active) step32(t0, k_now + 32 * ROW, v_before + 32 * ROW);
+            // all up to turn step + 1 - S; where turns had no tile left to
+            // load their count is short of PER, and everything is waited for
+            if (step + S - 1 < last)
+                arrived<(S - 2) * PER>();
+            else
+                arrived<0>();
             __syncthreads();
-            if (step + 1 < last) {
-#pragma unroll
-                for (int i = 0; i < L; ++i) after[i] = renewed(after[i]);   // here, where it has arrived, not among the loads
-                load(step + 1, next, vh, v_in, v_slot, a.v_page, a.v_slot, v_lds + (1 - B) * TILE);
-                load(step + 2, after, kh, k_in, k_slot, a.k_page, a.k_slot, k_lds + B * TILE);
-                find_pages(step + 3, next);
+            if (step + S - 1 < last) {
+                fetch_ids(step + 2 * S - 1);
+                load_values(step + S - 1);
+                if (step + S < last) load_keys(step + S);
             }
-            if (partly_seen(t0)) odd_values(t0, values + B * TILE);
-            if (active) step32(t0 + 32, keys + (1 - B) * TILE, values + B * TILE);
-        };
-        for (int step = first; step < last; step += 2) {
-            one_tile(step, pages1, pages0, std::integral_constant<int, 0>());
-            if (step + 1 < last) one_tile(step + 1, pages0, pages1, std::integral_constant<int, 1>());
+            if (partly_seen(t0)) odd_values(t0, v_now);
+            if (active) step32(t0 + 32, k_next, v_now);
         }
         {
-            char *v_last = values + ((last - 1 - first) & 1) * TILE + 32 * ROW;
+            char *v_last = values + ((last - 1) & (S - 1)) * TILE + 32 * ROW;
             const int t0 = last * BN - 32;
             if (partly_seen(t0)) odd_values(t0, v_last);
             if (active) add(v_last, nothing);
