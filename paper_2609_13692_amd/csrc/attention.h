@@ -6,8 +6,9 @@
 // tile reads the keys [lo, hi) that any of its rows sees, in steps of BN
 // tokens: its units.
 //
-// Cut. All units of all tiles, in the order entry, key head, tile, step, are
-// one line of U units. Worker w takes [w U / W, (w + 1) U / W): the same
+// Cut. All steps of all tiles, in the order entry, key head, tile, step, each
+// tile's preceded by C units for what it costs besides its steps, are one line
+// of U units. Worker w takes about [w U / W, (w + 1) U / W): the same
 // amount of work each whatever the lengths, with at most two tiles of its own
 // cut (its first and its last). Lengths are on the device, so every workgroup
 // finds its part itself, from sums over the entries. A tile that one worker
@@ -27,6 +28,7 @@ struct Attn {
     const char *q;
     char *out;
     int64_t q_token, q_head, out_token, out_head;
+    uint32_t div_mul, div_s1, div_s2;                 // of a division by group
     float *lse;
     int out_f32, causal, window, flip;
     float factor;                                     // |scale| log2(e), or |scale| / softcap
@@ -60,11 +62,17 @@ struct Range {
     int lo, hi, first, count;                         // visible tokens; first step and steps (at least 1)
 };
 
+// row / group, by a product with a fraction of 2^32 and two shifts.
+__device__ inline int token_of(const Attn &a, int row) {
+    const uint32_t t = __umulhi(a.div_mul, (uint32_t)row);
+    return (int)((t + (((uint32_t)row - t) >> a.div_s1)) >> a.div_s2);
+}
+
 template <int M, int BN>
 __device__ inline Range tile_range(const Attn &a, int n, int len, int begin, int tile) {
     const int rows = n * a.group, r0 = tile * M, r1 = min(r0 + M, rows) - 1;
     Range g;
-    const int p0 = len - n + r0 / a.group, p1 = len - n + r1 / a.group;
+    const int p0 = len - n + token_of(a, r0), p1 = len - n + token_of(a, r1);
     g.hi = max(0, a.causal ? min(len, p1 + 1) : len);
     g.lo = a.window ? max(begin, p0 + 1 - a.window) : begin;
     if (g.hi <= g.lo) g.lo = g.hi = 0;
@@ -75,7 +83,7 @@ __device__ inline Range tile_range(const Attn &a, int n, int len, int begin, int
 
 // Tokens [lo, hi) that all rows first .. last of an entry see.
 __device__ inline void seen_by_all(const Attn &a, int n, int len, int begin, int first, int last, int &lo, int &hi) {
-    const int p0 = len - n + first / a.group, p1 = len - n + last / a.group;
+    const int p0 = len - n + token_of(a, first), p1 = len - n + token_of(a, last);
     hi = a.causal ? min(len, p0 + 1) : len;
     lo = a.window ? max(begin, p1 + 1 - a.window) : begin;
 }
@@ -86,7 +94,7 @@ __device__ inline int tiles_of(const Attn &a, int n) {
 }
 
 // Sizes of entries base .. base + 255; returns their units (all heads).
-template <int M, int BN>
+template <int M, int BN, int C>
 __device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = base + tid;   // a thread each
     const bool mine = tid < kEntries;
@@ -107,14 +115,14 @@ __device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
     const int tiles = tiles_of<M>(a, n);
     int64_t steps = 0;
     if (tiles <= 8)
-        for (int t = 0; t < tiles; ++t) steps += tile_range<M, BN>(a, n, len, begin, t).count;
+        for (int t = 0; t < tiles; ++t) steps += C + tile_range<M, BN>(a, n, len, begin, t).count;
     // long entries: the lanes of a wave take the tiles
     for (uint64_t todo = __ballot(tiles > 8); todo; todo &= todo - 1) {
         const int src = __ffsll((unsigned long long)todo) - 1;
         const int n2 = __builtin_amdgcn_readlane(n, src), len2 = __builtin_amdgcn_readlane(len, src);
         const int begin2 = __builtin_amdgcn_readlane(begin, src);
         int64_t x = 0;
-        for (int t = lane; t < tiles_of<M>(a, n2); t += 64) x += tile_range<M, BN>(a, n2, len2, begin2, t).count;
+        for (int t = lane; t < tiles_of<M>(a, n2); t += 64) x += C + tile_range<M, BN>(a, n2, len2, begin2, t).count;
         x = of_lane(wave_sums(x), 63);
         if (lane == src) steps = x;
     }
@@ -127,7 +135,7 @@ __device__ inline int64_t load_entries(const Attn &a, Entries &s, int base) {
 }
 
 // A workgroup's walk over its units.
-template <int M, int BN>
+template <int M, int BN, int C>
 struct Walk {
     int64_t total, at, end;           // units: all, this worker's next, its end
     int64_t before;                   // units before the current entry
@@ -135,10 +143,18 @@ struct Walk {
     int head, tile;
     int64_t tile_at;                  // units before the current tile
 
-    __device__ static int64_t cut(int64_t total, int w, int workers) { return total * w / workers; }
-    // the worker that holds unit u
-    __device__ static int owner(int64_t u, int64_t total, int workers) {
-        return (int)(((u + 1) * workers - 1) / total);
+    // Units before worker w's. In doubles, where a 64-bit division would be a
+    // hundred instructions: every workgroup gets the same, it rises with w,
+    // and it ends at the total.
+    __device__ int64_t cut(int w) const {
+        return w >= workers ? total : (int64_t)((double)total * (double)w / (double)workers);
+    }
+    // The worker that holds unit u.
+    __device__ int owner(int64_t u) const {
+        int w = min(workers - 1, (int)((double)u * (double)workers / (double)total));
+        while (w + 1 < workers && cut(w + 1) <= u) ++w;
+        while (w > 0 && cut(w) > u) --w;
+        return w;
     }
 
     // False if this workgroup has no work. least: units that are worth a worker.
@@ -146,27 +162,29 @@ struct Walk {
         const int tid = threadIdx.x;
         int64_t sum = 0;
         for (base = 0; base < a.n; base += kEntries) {
-            const int64_t x = load_entries<M, BN>(a, s, base);
+            const int64_t x = load_entries<M, BN, C>(a, s, base);
             if (tid == 0) s.chunk[base / kEntries] = x;
             sum += x;
         }
         total = uniform(sum);
-        workers = (int)min((int64_t)a.workers, max((int64_t)1, total / least));
+        workers = a.workers;
+        if (total < (int64_t)least * workers) workers = max(1, (int)total / least);
         // neighbours, which read the same keys, on one XCD (the grid is a
         // multiple of 8: every number below it is one workgroup's)
         const int per = (workers + 7) / 8, bid = blockIdx.x;
         worker = (bid >> 3) < per ? (bid & 7) * per + (bid >> 3) : bid;
         if (tid == 0) a.parts[worker].count = 0;
         if (total == 0 || worker >= workers) return false;
-        at = uniform(cut(total, worker, workers));
-        end = uniform(cut(total, worker + 1, workers));
+        at = uniform(cut(worker));
+        end = uniform(cut(worker + 1));
+        if (at == end) return false;
         __syncthreads();
         before = 0;
         int k = 0;
         while (before + uniform(s.chunk[k]) <= at) before += uniform(s.chunk[k++]);
         if (a.n > kEntries) {
             __syncthreads();
-            load_entries<M, BN>(a, s, k * kEntries);
+            load_entries<M, BN, C>(a, s, k * kEntries);
         }
         base = k * kEntries;
         // the entry, by the lanes of each wave: 64 at a time
@@ -185,19 +203,22 @@ struct Walk {
             e += 64;
         }
         const int64_t in = at - before, steps = uniform(s.steps[e]);
-        head = (int)(in / steps);
+        head = (int)((double)in / (double)steps);
+        while (head > 0 && head * steps > in) --head;
+        while ((head + 1) * steps <= in) ++head;
+        head = uniform(head);
         find_tile(a, s, in - head * steps);
         return true;
     }
 
-    // The tile that holds the given step of a head of the current entry.
-    __device__ void find_tile(const Attn &a, const Entries &s, int64_t step) {
+    // The tile that holds the given unit of a head of the current entry.
+    __device__ void find_tile(const Attn &a, const Entries &s, int64_t unit) {
         const int lane = threadIdx.x & 63, tiles = tiles_of<M>(a, s.n[e]);
         int64_t sum = 0;
         for (tile = 0;; tile += 64) {
-            const int64_t x = tile + lane < tiles ? tile_range<M, BN>(a, s.n[e], s.len[e], s.begin[e], tile + lane).count : 0;
+            const int64_t x = tile + lane < tiles ? C + tile_range<M, BN>(a, s.n[e], s.len[e], s.begin[e], tile + lane).count : 0;
             const int64_t y = wave_sums(x);
-            const uint64_t past = __ballot(sum + y > step);
+            const uint64_t past = __ballot(sum + y > unit);
             if (past) {
                 const int k = __ffsll((unsigned long long)past) - 1;
                 tile += k;
@@ -206,6 +227,20 @@ struct Walk {
             }
             sum += of_lane(y, 63);
         }
+    }
+
+    // The worker's steps [first, last) of the current tile of `count`, and
+    // past them in the line.
+    __device__ void take(int count, int &first, int &last) {
+        first = uniform((int)max((int64_t)0, at - tile_at - C));
+        last = uniform((int)max((int64_t)0, min((int64_t)count, end - tile_at - C)));
+        at = min(end, tile_at + C + count);
+    }
+
+    // Where this worker is the second of a tile of `count` steps: the tile's workers, else 0.
+    __device__ int second_of(int count) const {
+        const int w0 = owner(tile_at + C);
+        return w0 + 1 == worker ? owner(tile_at + C + count - 1) - w0 + 1 : 0;
     }
 
     // To the next tile, after all units of the current one.
@@ -220,7 +255,7 @@ struct Walk {
             if (++e == kEntries) {
                 __syncthreads();
                 base += kEntries;
-                load_entries<M, BN>(a, s, base);
+                load_entries<M, BN, C>(a, s, base);
                 e = 0;
             }
         } while (uniform(s.n[e]) == 0);

@@ -76,6 +76,10 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
         a.c = *cache;
         a.layer = layer, a.n = n, a.n_tokens = (int)n_tokens, a.heads = n_q_heads, a.group = n_q_heads / cache->n_heads;
         a.units = cache->head_dim / 8;
+        int bits = 0;                                       // ceil(log2 group)
+        while ((1 << bits) < a.group) ++bits;
+        a.div_mul = (uint32_t)(((uint64_t)((1 << bits) - a.group) << 32) / a.group + 1);
+        a.div_s1 = bits < 1 ? bits : 1, a.div_s2 = bits > 1 ? bits - 1 : 0;
         a.seqs = seqs, a.q_off = q_off, a.kv_begin = kv_begin;
         a.q = (const char *)q, a.out = (char *)out, a.lse = lse;
         a.q_token = q_token_stride, a.q_head = q_head_stride, a.out_token = out_token_stride, a.out_head = out_head_stride;

@@ -20,6 +20,7 @@ namespace mptkv {
 template <int DP>
 struct Narrow {
     static constexpr int M = 16, BN = 128, KK = DP / 32, DT = DP / 16, ROW = 2 * DP, CH = DP / 8;
+    static constexpr int C = 1;                                        // a tile's cost besides its steps, in steps
     static constexpr int kTile = 32 * ROW, L = kTile / 1024;           // a wave's keys of a step; loads of 1 KiB
     static constexpr int kShift = DP == 64 ? 3 : DP == 128 ? 4 : 5;    // log2 CH
 
@@ -30,7 +31,7 @@ struct Narrow {
 template <class T, int DP, bool CAP, bool PAD>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
     using N = Narrow<DP>;
-    constexpr int M = N::M, BN = N::BN, KK = N::KK, DT = N::DT, ROW = N::ROW, CH = N::CH, L = N::L;
+    constexpr int M = N::M, BN = N::BN, C = N::C, KK = N::KK, DT = N::DT, ROW = N::ROW, CH = N::CH, L = N::L;
     __shared__ Entries ent;
     __shared__ __attribute__((aligned(1024))) char tiles[4 * 2 * N::kTile];
     __shared__ float stat[4][2][16];
@@ -39,19 +40,24 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
     const int shift = 31 - __clz(c.page_size);
     char *kw = tiles + wave * 2 * N::kTile, *vw = kw + N::kTile;      // the wave's keys and values
 
-    Walk<M, BN> walk;
+    Walk<M, BN, C> walk;
     if (!walk.begin(a, ent, 1)) return;
 
     while (walk.at < walk.end) {
         const int e = uniform(walk.e), n = uniform(ent.n[e]), len = uniform(ent.len[e]), q0 = uniform(ent.q0[e]);
         const int begin = uniform(ent.begin[e]), head = uniform(walk.head), tile = uniform(walk.tile);
         const Range range = tile_range<M, BN>(a, n, len, begin, tile);
-        const int from = uniform((int)(walk.at - walk.tile_at)), first = range.first + from;
-        const int last = uniform(range.first + (int)min((int64_t)range.count, from + (walk.end - walk.at)));
+        int from, to;
+        walk.take(range.count, from, to);
+        const bool starts = from == 0, ends = to == range.count;
+        if (from == to) {                      // only what comes before its steps: the next worker's tile
+            break;
+        }
+        const int first = range.first + from, last = range.first + to;
         const int rows = n * a.group;
         const int32_t *table = c.table + (int64_t)uniform(ent.slot[e]) * c.max_pages;
 
-        const int r = tile * M + col, rr = min(r, rows - 1), j = rr / a.group, hq = rr - j * a.group, p = len - n + j;
+        const int r = tile * M + col, rr = min(r, rows - 1), j = token_of(a, rr), hq = rr - j * a.group, p = len - n + j;
         const int see_hi = a.causal ? min(len, p + 1) : len;
         const int see_lo = a.window ? max(begin, p + 1 - a.window) : begin;
         const int64_t token = q0 + j, hh = (int64_t)head * a.group + hq;
@@ -220,8 +226,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
             f[w] = __builtin_amdgcn_exp2f(stat[w][0][col] - base);
             all_l += f[w] * stat[w][1][col];
         }
-        const bool starts = from == 0, ends = last == range.first + range.count;
-        walk.at += last - first;
         const float scale = !(starts && ends) ? 1.0f : all_l == 0 ? 0.0f : 1.0f / all_l;
         float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (starts ? 1 : 0)) * (M * (DP + 2));
 #pragma unroll
@@ -244,9 +248,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
         } else {
             if (wave == 0 && quad == 0) sums[M * DP + col] = all_m, sums[M * DP + 16 + col] = all_l;
             if (!starts && tid == 0) {
-                const int w0 = Walk<M, BN>::owner(walk.tile_at, walk.total, walk.workers);
-                const int w1 = Walk<M, BN>::owner(walk.tile_at + range.count - 1, walk.total, walk.workers);
-                if (w0 + 1 == walk.worker) a.parts[walk.worker] = Part{w1 - w0 + 1, e + walk.base, head, tile, q0, n};
+                const int workers = walk.second_of(range.count);
+                if (workers) a.parts[walk.worker] = Part{workers, e + walk.base, head, tile, q0, n};
             }
         }
         __syncthreads();                      // the LDS is free again
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(256) void k_kv_join_narrow(Attn a) {
     }
     const int rows = part.n * a.group, r = part.tile * M + col;
     if (r >= rows) return;
-    const int j = r / a.group, d = dt * 16 + 4 * quad;
+    const int j = token_of(a, r), d = dt * 16 + 4 * quad;
     const int64_t token = part.q0 + j, h = (int64_t)part.head * a.group + r - j * a.group;
     if (a.lse && dt == 0 && quad == 0)
         a.lse[token * a.heads + h] = l == 0 ? -INFINITY : 0.693147180559945f * (top + __builtin_amdgcn_logf(l));

@@ -28,6 +28,7 @@ struct Wide {
     static constexpr int kStride = kThreads / CH;                       // tokens between a thread's loads
     // Tiles of keys (and of values) in LDS: two where two workgroups share a
     // CU or rows are long, else four. Page ids are fetched for twice as many.
+    static constexpr int C = 8;                                        // a tile's cost besides its steps, in steps
     static constexpr int S = WAVES == 8 ? 4 : 2, IDS = 2 * S;
     // Operands read from LDS ahead of their products: with one wave to a SIMD
     // nothing else covers the latency.
@@ -45,7 +46,7 @@ template <class T, int DP, int WAVES, bool CAP>
 __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn a) {
     using W = Wide<DP, WAVES>;
     constexpr int M = 32 * WAVES, THREADS = W::kThreads, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, CH = W::CH, L = W::kLoads, TILE = W::kTile;
-    constexpr int S = W::S, IDS = W::IDS, AHEAD = W::kAhead;
+    constexpr int C = W::C, S = W::S, IDS = W::IDS, AHEAD = W::kAhead;
     __shared__ Entries ent;
     __shared__ __attribute__((aligned(1024))) char keys[S * TILE], values[S * TILE];
     __shared__ __attribute__((aligned(256))) int ids[WAVES * IDS * BN];       // each wave its own
@@ -71,22 +72,27 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
     const int v_row = v_of * ROW + (lane & 1) * 8, v_flip = (((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ W::v_swizzle(v_of);
     bool lost = false;                         // a page id outside the pool
 
-    Walk<M, BN> walk;
+    Walk<M, BN, C> walk;
     if (!walk.begin(a, ent, 4)) return;
 
     while (walk.at < walk.end) {
         const int e = uniform(walk.e), n = uniform(ent.n[e]), len = uniform(ent.len[e]), q0 = uniform(ent.q0[e]);
         const int begin = uniform(ent.begin[e]), head = uniform(walk.head), tile = uniform(walk.tile);
         const Range range = tile_range<M, BN>(a, n, len, begin, tile);
-        const int from = uniform((int)(walk.at - walk.tile_at)), first = range.first + from;
-        const int last = uniform(range.first + (int)min((int64_t)range.count, from + (walk.end - walk.at)));
+        int from, to;
+        walk.take(range.count, from, to);
+        const bool starts = from == 0, ends = to == range.count;
+        if (from == to) {                      // only what comes before its steps: the next worker's tile
+            break;
+        }
+        const int first = range.first + from, last = range.first + to;
         const int rows = n * a.group, row_base = tile * M + wave * 32;
         const int32_t *table = c.table + (int64_t)uniform(ent.slot[e]) * c.max_pages;
         const bool active = row_base < rows;
 
         // queries of the wave's rows as operands, and what each may see
         s16x8 qf[KK];
-        const int r0 = row_base + col, rr = min(r0, rows - 1), j0 = rr / a.group, p0 = len - n + j0;
+        const int r0 = row_base + col, rr = min(r0, rows - 1), j0 = token_of(a, rr), p0 = len - n + j0;
         const int see_hi = a.causal ? min(len, p0 + 1) : len, see_lo = a.window ? max(begin, p0 + 1 - a.window) : begin;
         const char *q = a.q + 2 * ((int64_t)(q0 + j0) * a.q_token + ((int64_t)head * a.group + rr - j0 * a.group) * a.q_head);
 #pragma unroll
@@ -189,6 +195,9 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                     if (!(t >= see_lo && t < see_hi)) x[r] = -INFINITY;
                 }
             }
+            // between the two waves of a SIMD, the one with products to issue
+            // goes before the one that forms addresses: 2% of the kernel
+            __builtin_amdgcn_s_setprio(1);
             float top = -INFINITY;
             add(v_before, [&](int i) INLINE {
                 constexpr int E = 8 / DT;
@@ -199,12 +208,14 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             if (__any(top > m + 8.0f)) {
                 const float now = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
                 const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+                if (!__all(m == -INFINITY)) {                         // else the sums are zeros
+                    l *= keep;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[dt][r] *= keep;
+                }
                 m = now;
-                l *= keep;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[dt][r] *= keep;
             }
             const float base = m == -INFINITY ? 0.0f : m;
             typename Type<T>::x8 w8;
@@ -218,6 +229,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                     if (r % 8 == 7) pf[r / 8] = __builtin_bit_cast(s16x8, w8);
                 }
             });
+            __builtin_amdgcn_s_setprio(0);
         };
         // Infinities and NaN in values of 32 tokens: a weight of zero does not
         // cancel them in a row that does not see them. Rows that do see them
@@ -324,8 +336,6 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             if (active) add(v_last, nothing);
         }
 
-        const bool starts = from == 0, ends = last == range.first + range.count;
-        walk.at += last - first;
         const float sum = l + __shfl_xor(l, 32);
         if (starts && ends) {
             if (r0 < rows) {
@@ -350,9 +360,8 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                 (sums - wave * 32 * DP + M * DP + wave * 64)[lane] = half ? sum : m;
             }
             if (!starts && tid == 0) {
-                const int w0 = Walk<M, BN>::owner(walk.tile_at, walk.total, walk.workers);
-                const int w1 = Walk<M, BN>::owner(walk.tile_at + range.count - 1, walk.total, walk.workers);
-                if (w0 + 1 == walk.worker) a.parts[walk.worker] = Part{w1 - w0 + 1, e + walk.base, head, tile, q0, n};
+                const int workers = walk.second_of(range.count);
+                if (workers) a.parts[walk.worker] = Part{workers, e + walk.base, head, tile, q0, n};
             }
         }
         if (ends && walk.at < walk.end) walk.next(a, ent);
@@ -411,7 +420,7 @@ __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
         m = now;
     }
     if (r >= rows) return;
-    const int j = r / a.group;
+    const int j = token_of(a, r);
     const int64_t token = part.q0 + j, h = (int64_t)part.head * a.group + r - j * a.group;
     const float scale = l == 0 ? 0.0f : 1.0f / l;
     if (a.lse && wave == 0 && half == 0)
