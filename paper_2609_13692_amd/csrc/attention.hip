@@ -15,10 +15,18 @@ struct Choice {
     int workers, rows;       // workgroups, rows of a tile
 };
 
+// By the rows that an entry has for a key head on average (the lengths are on
+// the device). Microseconds, narrow / 4 waves / 8 waves, 32 entries over 4000
+// tokens and 128 over 300, 4 query heads a key head:
+//   dim 128: 16 rows 115/168/153; 32 rows 126/169/154 and 68/80/100; 48 rows
+//   312/176/155; 64 rows 240/176/156 and 114/86/108; 128 rows 487/190/158 and
+//   215/105/207; 160 rows 606/248/171; 256 rows 939/263/184 and 447/182/161
+//   dim 64: 20 rows 105/70/83; 128 rows 339/87/94; 256 rows 656/126/119
+//   dim 256 (2000 tokens): 16 rows 108/157; 20 rows 202/156
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
-    if (rows <= 16) return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
+    if (rows <= (dim == 128 ? 32 : 16)) return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
     if (rows <= 128 || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
     return {8, 256, 256};
 }

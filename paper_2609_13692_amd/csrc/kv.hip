@@ -14,7 +14,12 @@
 
 namespace mptkv {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kSlotBits = 1 << 16;            // slots whose marks are bits in LDS
+
+// A plan is one workgroup: small for short lists on small pools (a launch of a
+// few microseconds either way: 6.2 us with 1024 threads on 9 entries and 1000
+// pages, 4.1 with 256), 16 waves where there is more to read.
+inline int plan_threads(int n, int n_pages) { return n <= 512 && n_pages <= (1 << 16) ? 256 : 1024; }
 
 // The first 256 bytes of the workspace: what a plan tells its second launch
 // and, where it asks, the host.
@@ -47,14 +52,15 @@ static Plan plan_at(const mpt_kv_cache &c, void *ws) {
     return q;
 }
 
-// Exclusive sum over the workgroup's 1024 threads; *total is the whole sum.
+// Exclusive sum over the workgroup's threads; *total is the whole sum.
+template <int THREADS>
 __device__ inline int64_t block_scan(int64_t v, int64_t *total, int64_t *lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t x = wave_sums(v);
     if (lane == 63) lds[wave] = x;
     __syncthreads();
     int64_t before = 0, all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         const int64_t t = lds[w];
         if (w < wave) before += t;
         all += t;
@@ -71,20 +77,27 @@ __device__ inline int pages_of(const mpt_kv_cache &c, int tokens) {
 __device__ inline bool slot_ok(const mpt_kv_cache &c, int s) { return s >= 0 && s < c.max_seqs; }
 __device__ inline bool page_ok(const mpt_kv_cache &c, int p) { return p >= 0 && p < c.n_pages; }
 
-// Every listed index below `bound` gets its mark; an index that two entries
-// list is a duplicate. The barriers order the marks' stores (all in L2).
-__device__ inline uint32_t mark_all(int n, const int32_t *list, int bound, int32_t *mark, uint32_t bad) {
+// Listed indexes outside [0, bound) and those that two entries list: by bits
+// in LDS where they fit, else by marks in memory (an index gets its entry's
+// number there; the barriers order the stores, all in L2).
+template <int THREADS>
+__device__ inline uint32_t check_list(int n, const int32_t *list, int bound, int32_t *mark, uint32_t *bits, uint32_t bad) {
     uint32_t err = 0;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-        const int s = list[i];
-        if (s >= 0 && s < bound) atomicExch(&mark[s], -1);
+    const bool in_lds = bound <= kSlotBits;
+    if (in_lds) {
+        for (int i = threadIdx.x; i < (bound + 31) / 32; i += THREADS) bits[i] = 0;
+    } else {
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+            const int s = list[i];
+            if (s >= 0 && s < bound) atomicExch(&mark[s], -1);
+        }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         const int s = list[i];
         if (s < 0 || s >= bound)
             err |= bad;
-        else if (atomicExch(&mark[s], i) != -1)
+        else if (in_lds ? atomicOr(&bits[s >> 5], 1u << (s & 31)) >> (s & 31) & 1 : atomicExch(&mark[s], i) != -1)
             err |= MPT_KV_DUPLICATE;
     }
     return err;
@@ -93,17 +106,19 @@ __device__ inline uint32_t mark_all(int n, const int32_t *list, int bound, int32
 // Plan of forks (src != null) and growth: checks, pages needed and the
 // lowest-numbered free pages in ascending order, which leave free_bits here.
 // Each thread owns a run of words, so ranks are one sum over the workgroup.
-__global__ __launch_bounds__(kPlanThreads) void k_kv_plan(mpt_kv_cache c, int n, const int32_t *src, const int32_t *dst,
-                                                          const int32_t *keep, const int32_t *new_len, Plan p) {
-    __shared__ int64_t lds[kPlanThreads / 64];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, const int32_t *src, const int32_t *dst,
+                                                     const int32_t *keep, const int32_t *new_len, Plan p) {
+    __shared__ int64_t lds[THREADS / 64];
+    __shared__ uint32_t slots[kSlotBits / 32];
     __shared__ uint32_t err_all;
     const int tid = threadIdx.x;
     if (tid == 0) err_all = 0;
     __syncthreads();
-    uint32_t err = mark_all(n, dst, c.max_seqs, p.mark, MPT_KV_BAD_SLOT);
+    uint32_t err = check_list<THREADS>(n, dst, c.max_seqs, p.mark, slots, MPT_KV_BAD_SLOT);
     const int64_t most = (int64_t)c.max_pages * c.page_size;
     int64_t need_all = 0;
-    for (int base = 0; base < n; base += kPlanThreads) {
+    for (int base = 0; base < n; base += THREADS) {
         const int i = base + tid;
         int64_t need = 0;
         if (i < n) {
@@ -139,7 +154,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(mpt_kv_cache c, int n,
             p.from[i] = from;
         }
         int64_t sum;
-        const int64_t at = need_all + block_scan(need, &sum, lds);
+        const int64_t at = need_all + block_scan<THREADS>(need, &sum, lds);
         need_all += sum;
         if (i < n) {
             p.start[i] = (int32_t)(at < c.n_pages ? at : c.n_pages);
@@ -147,11 +162,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(mpt_kv_cache c, int n,
             if (slot_ok(c, dst[i])) p.mark[dst[i]] = src ? keep[i] : c.length[dst[i]];
         }
     }
-    const int words = (c.n_pages + 63) / 64, per = (words + kPlanThreads - 1) / kPlanThreads;
+    const int words = (c.n_pages + 63) / 64, per = (words + THREADS - 1) / THREADS;
     const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
     int64_t mine = 0, free_all;
     for (int w = w0; w < w1; ++w) mine += __popcll(c.free_bits[w]);
-    int64_t at = block_scan(mine, &free_all, lds);
+    int64_t at = block_scan<THREADS>(mine, &free_all, lds);
     if (need_all > free_all) err |= MPT_KV_NO_PAGES;
     if (err) atomicOr(&err_all, err);
     __syncthreads();
@@ -207,8 +222,8 @@ __device__ inline void drop(const mpt_kv_cache &c, int page) {
 }
 
 // Forks and growth as planned: workgroup (i, 0) writes entry i's row of the
-// table and the references, workgroups (i, layer) copy the tokens of a
-// partial page.
+// table and the references, workgroups (i, y) copy the keys or the values of
+// a partial page's tokens in a layer.
 __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t *src, const int32_t *dst,
                                                   const int32_t *new_len, Plan p) {
     if (p.head->err) return;
@@ -217,9 +232,11 @@ __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t 
     const int full = now / c.page_size, part = now - full * c.page_size;
     if (from >= 0) {
         const int to = p.a[first], units = c.head_dim / 8;
-        for (int layer = blockIdx.y; layer < c.n_layers; layer += gridDim.y) {
-            copy_rows((char *)c.k, c.k_stride, layer, from, to, part, c.n_heads, units);
-            copy_rows((char *)c.v, c.v_stride, layer, from, to, part, c.n_heads, units);
+        for (int y = blockIdx.y; y < 2 * c.n_layers; y += gridDim.y) {
+            if (y & 1)
+                copy_rows((char *)c.v, c.v_stride, y >> 1, from, to, part, c.n_heads, units);
+            else
+                copy_rows((char *)c.k, c.k_stride, y >> 1, from, to, part, c.n_heads, units);
         }
     }
     if (blockIdx.y) return;
@@ -248,14 +265,13 @@ __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t 
     }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_kv_plan_free(mpt_kv_cache c, int n, const int32_t *seqs,
-                                                               const int32_t *keep, Plan p) {
-    __shared__ uint32_t err_all;
+template <int THREADS>
+__device__ inline uint32_t check_free(const mpt_kv_cache &c, int n, const int32_t *seqs, const int32_t *keep, const Plan &p) {
+    __shared__ uint32_t err_all, slots[kSlotBits / 32];
     if (threadIdx.x == 0) err_all = 0;
-    __syncthreads();
-    uint32_t err = mark_all(n, seqs, c.max_seqs, p.mark, MPT_KV_BAD_SLOT);
+    uint32_t err = check_list<THREADS>(n, seqs, c.max_seqs, p.mark, slots, MPT_KV_BAD_SLOT);
     const int64_t most = (int64_t)c.max_pages * c.page_size;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         const int s = seqs[i], now = slot_ok(c, s) ? c.length[s] : 0, k = keep ? keep[i] : 0;
         if (k < 0 || k > now || now > most) err |= MPT_KV_BAD_LENGTH;
     }
@@ -265,41 +281,64 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan_free(mpt_kv_cache c, i
         p.head->err = err_all;
         if (err_all) flag(c, err_all);
     }
+    return err_all;
 }
 
-__global__ __launch_bounds__(256) void k_kv_free(mpt_kv_cache c, const int32_t *seqs, const int32_t *keep, Plan p) {
-    if (p.head->err) return;
-    const int s = seqs[blockIdx.x], k = keep ? keep[blockIdx.x] : 0, now = c.length[s];
+// Pages of slot s past its first k tokens, a lane each.
+__device__ inline void drop_pages(const mpt_kv_cache &c, int s, int k, int now, int first, int step) {
     const int32_t *row = c.table + (int64_t)s * c.max_pages;
-    for (int j = pages_of(c, k) + threadIdx.x; j < pages_of(c, now); j += 256) {
+    for (int j = pages_of(c, k) + first; j < pages_of(c, now); j += step) {
         const int page = row[j];
         if (page_ok(c, page))
             drop(c, page);
         else
             flag(c, MPT_KV_BAD_PAGE);
     }
+}
+
+__global__ __launch_bounds__(1024) void k_kv_plan_free(mpt_kv_cache c, int n, const int32_t *seqs, const int32_t *keep, Plan p) {
+    check_free<1024>(c, n, seqs, keep, p);
+}
+
+__global__ __launch_bounds__(256) void k_kv_free(mpt_kv_cache c, const int32_t *seqs, const int32_t *keep, Plan p) {
+    if (p.head->err) return;
+    const int s = seqs[blockIdx.x], k = keep ? keep[blockIdx.x] : 0, now = c.length[s];
+    drop_pages(c, s, k, now, threadIdx.x, 256);
     __syncthreads();
     if (threadIdx.x == 0) c.length[s] = k;
 }
 
+// Checks and drops of short lists with short tables in one launch: a wave per
+// sequence.
+constexpr int kSmallFree = 8192;
+__global__ __launch_bounds__(1024) void k_kv_free_small(mpt_kv_cache c, int n, const int32_t *seqs, const int32_t *keep, Plan p) {
+    if (check_free<1024>(c, n, seqs, keep, p)) return;
+    const int lane = threadIdx.x & 63;
+    for (int i = threadIdx.x >> 6; i < n; i += 16) {
+        const int s = seqs[i], k = keep ? keep[i] : 0, now = c.length[s];
+        drop_pages(c, s, k, now, lane, 64);
+        if (lane == 0) c.length[s] = k;
+    }
+}
+
 // Number of free pages, for calls whose caller asks.
-__global__ __launch_bounds__(kPlanThreads) void k_kv_count(mpt_kv_cache c, Plan p) {
-    __shared__ int64_t lds[kPlanThreads / 64];
+__global__ __launch_bounds__(1024) void k_kv_count(mpt_kv_cache c, Plan p) {
+    __shared__ int64_t lds[16];
     int64_t mine = 0, all;
-    for (int w = threadIdx.x; w < (c.n_pages + 63) / 64; w += kPlanThreads) mine += __popcll(c.free_bits[w]);
-    block_scan(mine, &all, lds);
+    for (int w = threadIdx.x; w < (c.n_pages + 63) / 64; w += 1024) mine += __popcll(c.free_bits[w]);
+    block_scan<1024>(mine, &all, lds);
     if (threadIdx.x == 0) p.head->value = all;
 }
 
 // Plan of a compaction: the j-th used page from n_live on goes to the j-th
 // free page below. a[j] and b[j] are the two; the words are rewritten here.
-__global__ __launch_bounds__(kPlanThreads) void k_kv_plan_moves(mpt_kv_cache c, Plan p) {
-    __shared__ int64_t lds[kPlanThreads / 64];
-    const int tid = threadIdx.x, words = (c.n_pages + 63) / 64, per = (words + kPlanThreads - 1) / kPlanThreads;
+__global__ __launch_bounds__(1024) void k_kv_plan_moves(mpt_kv_cache c, Plan p) {
+    __shared__ int64_t lds[16];
+    const int tid = threadIdx.x, words = (c.n_pages + 63) / 64, per = (words + 1024 - 1) / 1024;
     const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
     int64_t mine = 0, free_all;
     for (int w = w0; w < w1; ++w) mine += __popcll(c.free_bits[w]);
-    block_scan(mine, &free_all, lds);
+    block_scan<1024>(mine, &free_all, lds);
     const int live = c.n_pages - (int)free_all;
     // bits of word w whose pages lie below x
     auto below = [](int w, int x) -> uint64_t {
@@ -312,7 +351,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan_moves(mpt_kv_cache c, 
         holes += __popcll(f & lo);
         movers += __popcll(~f & ~lo & in);
     }
-    int64_t h = block_scan(holes, &all, lds), m = block_scan(movers, &all, lds);
+    int64_t h = block_scan<1024>(holes, &all, lds), m = block_scan<1024>(movers, &all, lds);
     for (int w = w0; w < w1; ++w) {
         const uint64_t f = c.free_bits[w], lo = below(w, live), in = below(w, c.n_pages);
         for (uint64_t x = ~f & ~lo & in; x; x &= x - 1) p.a[m++] = w * 64 + __ffsll((unsigned long long)x) - 1;
@@ -368,18 +407,27 @@ __global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Plan p, int tab
     }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_kv_plan_copy(mpt_kv_cache c, int n, const int32_t *src,
+// Checks of a list of copies: marks of the destinations (each once, and none
+// of them a source) in b, then the two lists in a and b.
+__global__ __launch_bounds__(1024) void k_kv_plan_copy(mpt_kv_cache c, int n, const int32_t *src,
                                                                const int32_t *dst, Plan p) {
     __shared__ uint32_t err_all;
     if (threadIdx.x == 0) err_all = 0;
-    // a is the list of sources once the marks (in b) have been looked at
     uint32_t err = 0;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads)
+    for (int i = threadIdx.x; i < n; i += 1024)
         if (page_ok(c, src[i])) atomicExch(&p.b[src[i]], -1);
     __syncthreads();
-    err |= mark_all(n, dst, c.n_pages, p.b, MPT_KV_BAD_PAGE);
+    for (int i = threadIdx.x; i < n; i += 1024)
+        if (page_ok(c, dst[i])) atomicExch(&p.b[dst[i]], -1);
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        if (!page_ok(c, dst[i]))
+            err |= MPT_KV_BAD_PAGE;
+        else if (atomicExch(&p.b[dst[i]], i) != -1)
+            err |= MPT_KV_DUPLICATE;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 1024) {
         if (!page_ok(c, src[i]))
             err |= MPT_KV_BAD_PAGE;
         else if (atomicAdd(&p.b[src[i]], 0) != -1)
@@ -388,9 +436,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan_copy(mpt_kv_cache c, i
     if (err) atomicOr(&err_all, err);
     __syncthreads();
     err = err_all;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) p.a[i] = src[i];
+    for (int i = threadIdx.x; i < n; i += 1024) p.a[i] = src[i];
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) p.b[i] = dst[i];
+    for (int i = threadIdx.x; i < n; i += 1024) p.b[i] = dst[i];
     if (threadIdx.x == 0) {
         p.head->err = err;
         p.head->moves = n;
@@ -587,15 +635,18 @@ static int grow(const mpt_kv_cache *c, int n, const int32_t *src, const int32_t 
     const Plan p = plan_at(*c, ws);
     {
         mptlib::LaunchScope scope("k_kv_plan", n, s);
-        k_kv_plan<<<1, kPlanThreads, 0, s>>>(*c, n, src, dst, keep, new_len, p);
+        if (plan_threads(n, c->n_pages) == 256)
+            k_kv_plan<256><<<1, 256, 0, s>>>(*c, n, src, dst, keep, new_len, p);
+        else
+            k_kv_plan<1024><<<1, 1024, 0, s>>>(*c, n, src, dst, keep, new_len, p);
     }
     if (n) {
         mptlib::LaunchScope scope("k_kv_apply", n, s);
-        k_kv_apply<<<dim3(n, c->n_layers < 64 ? c->n_layers : 64), 256, 0, s>>>(*c, src, dst, new_len, p);
+        k_kv_apply<<<dim3(n, c->n_layers < 32 ? 2 * c->n_layers : 64), 256, 0, s>>>(*c, src, dst, new_len, p);
     }
     if (free_pages && !src) {                  // copies of shared pages may have left some without references
         mptlib::LaunchScope scope("k_kv_count", c->n_pages, s);
-        k_kv_count<<<1, kPlanThreads, 0, s>>>(*c, p);
+        k_kv_count<<<1, 1024, 0, s>>>(*c, p);
     }
     return report(p, free_pages, what, s);
 }
@@ -667,17 +718,20 @@ extern "C" int mpt_kv_free(const mpt_kv_cache *cache, int n, const int32_t *seqs
         if (int rc = check_plan(cache, n, cache ? cache->max_seqs : 0, workspace, workspace_bytes)) return rc;
         hipStream_t s = (hipStream_t)stream;
         const Plan p = plan_at(*cache, workspace);
-        {
-            mptlib::LaunchScope scope("k_kv_plan_free", n, s);
-            k_kv_plan_free<<<1, kPlanThreads, 0, s>>>(*cache, n, seqs, keep, p);
-        }
-        if (n) {
+        if ((int64_t)n * cache->max_pages <= kSmallFree) {
+            mptlib::LaunchScope scope("k_kv_free_small", n, s);
+            k_kv_free_small<<<1, 1024, 0, s>>>(*cache, n, seqs, keep, p);
+        } else {
+            {
+                mptlib::LaunchScope scope("k_kv_plan_free", n, s);
+                k_kv_plan_free<<<1, 1024, 0, s>>>(*cache, n, seqs, keep, p);
+            }
             mptlib::LaunchScope scope("k_kv_free", n, s);
             k_kv_free<<<n, 256, 0, s>>>(*cache, seqs, keep, p);
         }
         if (free_pages) {
             mptlib::LaunchScope scope("k_kv_count", cache->n_pages, s);
-            k_kv_count<<<1, kPlanThreads, 0, s>>>(*cache, p);
+            k_kv_count<<<1, 1024, 0, s>>>(*cache, p);
         }
         return report(p, free_pages, "mpt_kv_free", s);
     });
@@ -692,7 +746,7 @@ extern "C" int mpt_kv_compact(const mpt_kv_cache *cache, int64_t *live_pages, vo
         const Plan p = plan_at(*cache, workspace);
         {
             mptlib::LaunchScope scope("k_kv_plan_moves", cache->n_pages, s);
-            k_kv_plan_moves<<<1, kPlanThreads, 0, s>>>(*cache, p);
+            k_kv_plan_moves<<<1, 1024, 0, s>>>(*cache, p);
         }
         {
             mptlib::LaunchScope scope("k_kv_move", cache->n_pages, s);
@@ -712,7 +766,7 @@ extern "C" int mpt_kv_copy(const mpt_kv_cache *cache, int n, const int32_t *src,
         const Plan p = plan_at(*cache, workspace);
         {
             mptlib::LaunchScope scope("k_kv_plan_copy", n, s);
-            k_kv_plan_copy<<<1, kPlanThreads, 0, s>>>(*cache, n, src, dst, p);
+            k_kv_plan_copy<<<1, 1024, 0, s>>>(*cache, n, src, dst, p);
         }
         if (n) {
             mptlib::LaunchScope scope("k_kv_move", n, s);

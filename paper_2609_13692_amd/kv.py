@@ -14,7 +14,7 @@ import math
 
 import torch
 
-from .mpt import KvDescriptor, MptError, _check, _stream, load
+from .mpt import KvDescriptor, MptError, _check, load
 
 BF16, F16, F32 = 0, 1, 2
 _KIND = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
@@ -22,17 +22,30 @@ MAX_PARTS = 16
 STATUS_BITS = {1: "slot", 2: "length", 4: "page", 8: "duplicate", 16: "not empty", 32: "no pages", 64: "shared page"}
 
 
-def _list(t, n, name, device):
-    """Address of a contiguous int32 device tensor of at least n elements."""
-    if t.dtype != torch.int32:
+def _list(t, n, name, index):
+    """Address of a contiguous int32 tensor of at least n elements on GPU `index`."""
+    if t.dtype is not torch.int32:
         raise TypeError(f"{name} must be torch.int32, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if t.numel() < n:
-        raise ValueError(f"{name} has {t.numel()} elements, needs {n}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on GPU {index}, got {t.device}")
+    if not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name} must be contiguous, of at least {n} elements; got {tuple(t.shape)}")
     return t.data_ptr()
+
+
+def _on(stream, index):
+    """Address of a stream (None: GPU index's current one), and what new
+    tensors that its work uses are made under."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index) or None, None
+    return stream.cuda_stream or None, torch.cuda.stream(stream)
+
+
+def _new(shape, dtype, device, under):
+    if under is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with under:                    # the allocator then orders reuse by that stream
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 class KvCache:
@@ -69,7 +82,7 @@ class KvCache:
         self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
         self.free_bits, self.status = free_bits, status
         self.device, self.dtype, self.page_size, self.n_heads, self.head_dim = k.device, k.dtype, size, heads, dim
-        self.max_seqs = table.shape[0]
+        self.max_seqs, self._index = table.shape[0], k.get_device()
         d = KvDescriptor()
         d.k, d.v = k.data_ptr(), v.data_ptr()
         d.k_stride[:], d.v_stride[:] = k.stride()[:4], v.stride()[:4]
@@ -84,7 +97,8 @@ class KvCache:
         if n == 0:
             raise MptError(-1, "mpt_kv_workspace_bytes", self._lib.mpt_last_error().decode())
         self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-        self._at_ws, self._at_sizes = None, {}
+        self._ws_at, self._ws_bytes = self._ws.data_ptr(), n
+        self._at_ws, self._at_bytes, self._at_sizes, self._scale = None, 0, {}, 1.0 / math.sqrt(dim)
 
     @classmethod
     def create(cls, n_layers, n_pages, page_size, n_heads, head_dim, max_seqs, max_len, dtype=torch.bfloat16,
@@ -103,64 +117,67 @@ class KvCache:
         return c
 
     def reset(self, stream=None):
-        _check(self._lib.mpt_kv_reset(self._p, _stream(stream)), "mpt_kv_reset")
+        _check(self._lib.mpt_kv_reset(self._p, _on(stream, self._index)[0]), "mpt_kv_reset")
 
     def take_status(self, stream=None) -> list[str]:
         """What calls have found wrong in device data since the last look."""
         bits = ctypes.c_uint32(0)
-        _check(self._lib.mpt_kv_status(self._p, ctypes.addressof(bits), _stream(stream)), "mpt_kv_status")
+        _check(self._lib.mpt_kv_status(self._p, ctypes.addressof(bits), _on(stream, self._index)[0]), "mpt_kv_status")
         return [name for bit, name in STATUS_BITS.items() if bits.value & bit]
 
-    def _pages(self, name, lists, check, stream, counted=True):
-        f = getattr(self._lib, "mpt_kv_" + name)
-        out = ctypes.c_int64(0)
-        n = next((t.numel() for t in lists if t is not None), 0)
-        args = [None if t is None else _list(t, n, name + " list", self.device) for t in lists]
-        rc = f(self._p, *((n,) if counted else ()), *args, ctypes.addressof(out) if check else None,
-               self._ws.data_ptr(), self._ws.numel(), _stream(stream))
-        _check(rc, "mpt_kv_" + name)
-        return int(out.value) if check else None
+    def _pages(self, name, lists, check, stream):
+        out = ctypes.c_int64(0) if check else None
+        args = []
+        if lists:
+            n = lists[0].numel()
+            args = [n] + [None if t is None else _list(t, n, name, self._index) for t in lists]
+        rc = getattr(self._lib, name)(self._p, *args, ctypes.addressof(out) if check else None, self._ws_at,
+                                      self._ws_bytes, _on(stream, self._index)[0])
+        if rc:
+            _check(rc, name)
+        return out.value if check else None
 
     def fork(self, src, dst, keep, new_len, check=False, stream=None):
         """Empty slots dst become sequences of new_len tokens sharing the first
         keep with src (-1: none). With check, waits and returns the number of
         free pages left, or raises."""
-        return self._pages("fork", (src, dst, keep, new_len), check, stream)
+        return self._pages("mpt_kv_fork", (src, dst, keep, new_len), check, stream)
 
     def extend(self, seqs, new_len, check=False, stream=None):
         """Grows sequences to new_len tokens."""
-        return self._pages("extend", (seqs, new_len), check, stream)
+        return self._pages("mpt_kv_extend", (seqs, new_len), check, stream)
 
     def free(self, seqs, keep=None, check=False, stream=None):
         """Cuts sequences to keep tokens (None: to none)."""
-        return self._pages("free", (seqs, keep), check, stream)
+        return self._pages("mpt_kv_free", (seqs, keep), check, stream)
 
     def compact(self, check=False, stream=None):
         """Moves the pages in use to the lowest numbers; with check returns
         how many they are."""
-        return self._pages("compact", (), check, stream, counted=False)
+        return self._pages("mpt_kv_compact", (), check, stream)
 
     def copy(self, src, dst, check=False, stream=None):
         """Copies page contents (all layers)."""
-        return self._pages("copy", (src, dst), check, stream)
+        return self._pages("mpt_kv_copy", (src, dst), check, stream)
 
     def _rows(self, t, heads, name, dtype):
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.dtype != dtype:
-            raise ValueError(f"{name} must be [tokens, {heads}, {self.head_dim}] of {dtype}, got {tuple(t.shape)} of {t.dtype}")
-        if t.device != self.device or t.stride(2) != 1:
+        shape = t.shape
+        if len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim or t.dtype is not dtype:
+            raise ValueError(f"{name} must be [tokens, {heads}, {self.head_dim}] of {dtype}, got {tuple(shape)} of {t.dtype}")
+        stride = t.stride()
+        if t.get_device() != self._index or stride[2] != 1:
             raise ValueError(f"{name} must be on {self.device}, with contiguous rows")
-        return t.data_ptr(), t.stride(0), t.stride(1)
+        return t.data_ptr(), stride[0], stride[1]
 
     def append(self, layer, k_new, v_new, q_off, seqs, stream=None):
         """Writes the newest tokens' keys and values of one layer; q_off [n + 1]
         cuts the tokens into the sequences in seqs [n]."""
-        n, tokens = seqs.numel(), k_new.shape[0]
+        n, tokens, index = seqs.numel(), k_new.shape[0], self._index
         if v_new.shape[0] != tokens:
             raise ValueError("k_new and v_new must have one row per token")
-        rc = self._lib.mpt_kv_append(self._p, layer, n, _list(seqs, n, "seqs", self.device),
-                                     _list(q_off, n + 1, "q_off", self.device), tokens,
-                                     *self._rows(k_new, self.n_heads, "k_new", self.dtype),
-                                     *self._rows(v_new, self.n_heads, "v_new", self.dtype), _stream(stream))
+        rc = self._lib.mpt_kv_append(self._p, layer, n, _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index),
+                                     tokens, *self._rows(k_new, self.n_heads, "k_new", self.dtype),
+                                     *self._rows(v_new, self.n_heads, "v_new", self.dtype), _on(stream, index)[0])
         if rc:
             _check(rc, "mpt_kv_append")
 
@@ -168,14 +185,16 @@ class KvCache:
                lse=None, out_dtype=None, stream=None):
         """(out, lse) of the newest tokens' queries over their sequences (see
         mpt_kv_attention). scale defaults to 1 / sqrt(dim)."""
-        n, tokens, heads = seqs.numel(), q.shape[0], q.shape[1]
+        tokens, heads, dim = q.shape
+        n, index = seqs.numel(), self._index
+        at, under = _on(stream, index)
         if out is None:
-            out = torch.empty((tokens, heads, self.head_dim), dtype=out_dtype or self.dtype, device=self.device)
+            out = _new((tokens, heads, dim), out_dtype or self.dtype, self.device, under)
         elif out.shape[0] != tokens or (out_dtype or out.dtype) != out.dtype:
             raise ValueError("out must have one row per token, of out_dtype")
         if lse is None:
-            lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device)
-        elif lse.dtype != torch.float32 or lse.device != self.device or lse.shape != (tokens, heads) or not lse.is_contiguous():
+            lse = _new((tokens, heads), torch.float32, self.device, under)
+        elif lse.dtype is not torch.float32 or lse.get_device() != index or lse.shape != (tokens, heads) or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32 [tokens, heads] device tensor")
         key = (n, tokens, heads)
         need = self._at_sizes.get(key)
@@ -183,16 +202,17 @@ class KvCache:
             need = self._lib.mpt_kv_attention_workspace_bytes(self._p, n, tokens, heads)
             if len(self._at_sizes) < 4096:
                 self._at_sizes[key] = need
-        if need and (self._at_ws is None or self._at_ws.numel() < need):
-            self._at_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        if need > self._at_bytes:
+            if self._at_ws is not None and under is not None:
+                self._at_ws.record_stream(stream)      # calls on it may still use the smaller one
+            self._at_ws = _new(need, torch.uint8, self.device, under)
+            self._at_bytes = need
         ws = self._at_ws
         rc = self._lib.mpt_kv_attention(
-            self._p, layer, n, _list(seqs, n, "seqs", self.device), _list(q_off, n + 1, "q_off", self.device), tokens,
-            heads, *self._rows(q, heads, "q", self.dtype), *self._rows(out, heads, "out", out.dtype),
-            _KIND.get(out.dtype, -1), lse.data_ptr(),
-            None if kv_begin is None else _list(kv_begin, n, "kv_begin", self.device), 1 if causal else 0, window, softcap,
-            1.0 / math.sqrt(self.head_dim) if scale is None else scale, ws.data_ptr() if ws is not None else None,
-            ws.numel() if ws is not None else 0, _stream(stream))
+            self._p, layer, n, _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index), tokens, heads,
+            *self._rows(q, heads, "q", self.dtype), *self._rows(out, heads, "out", out.dtype), _KIND.get(out.dtype, -1),
+            lse.data_ptr(), None if kv_begin is None else _list(kv_begin, n, "kv_begin", index), 1 if causal else 0, window,
+            softcap, self._scale if scale is None else scale, ws.data_ptr() if ws is not None else None, self._at_bytes, at)
         if rc:
             _check(rc, "mpt_kv_attention")
         return out, lse
@@ -205,27 +225,30 @@ def merge(parts, lses, out_dtype=None, out=None, lse=None, stream=None):
     if len(parts) != len(lses) or not 1 <= len(parts) <= MAX_PARTS:
         raise ValueError(f"needs 1 .. {MAX_PARTS} parts, each with its lse")
     first = parts[0]
-    if first.dtype not in _KIND:
-        raise TypeError(f"parts must be bfloat16, float16 or float32, got {first.dtype}")
+    kind, index = _KIND.get(first.dtype), first.get_device()
+    if kind is None or index < 0:
+        raise TypeError(f"parts must be bfloat16, float16 or float32 device tensors, got {first.dtype} on {first.device}")
     shape, device = first.shape, first.device
+    rows = shape[:-1]
     for p, l in zip(parts, lses):
-        if p.shape != shape or p.dtype != first.dtype or p.device != device or not p.is_contiguous() or not p.is_cuda:
+        if p.shape != shape or p.dtype is not first.dtype or p.get_device() != index or not p.is_contiguous():
             raise ValueError("parts must be contiguous device tensors of one shape and type")
-        if l.shape != shape[:-1] or l.dtype != torch.float32 or l.device != device or not l.is_contiguous():
+        if l.shape != rows or l.dtype is not torch.float32 or l.get_device() != index or not l.is_contiguous():
             raise ValueError("lses must be contiguous float32 device tensors of the parts' shape without the last dimension")
+    at, under = _on(stream, index)
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype or first.dtype, device=device)
-    elif out.shape != shape or out.device != device or not out.is_contiguous() or out.dtype not in _KIND or \
-            (out_dtype or out.dtype) != out.dtype:
+        out = _new(shape, out_dtype or first.dtype, device, under)
+    elif out.shape != shape or out.get_device() != index or not out.is_contiguous() or (out_dtype or out.dtype) != out.dtype:
         raise ValueError("out must be a contiguous device tensor of the parts' shape and out_dtype")
     if lse is None:
-        lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-    elif lse.shape != shape[:-1] or lse.dtype != torch.float32 or lse.device != device or not lse.is_contiguous():
+        lse = _new(rows, torch.float32, device, under)
+    elif lse.shape != rows or lse.dtype is not torch.float32 or lse.get_device() != index or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 device tensor")
     n = len(parts)
-    rc = load().mpt_kv_merge(n, lse.numel(), shape[-1], (ctypes.c_void_p * n)(*[p.data_ptr() for p in parts]),
-                             (ctypes.c_void_p * n)(*[l.data_ptr() for l in lses]), _KIND[first.dtype], out.data_ptr(),
-                             _KIND.get(out.dtype, -1), lse.data_ptr(), _stream(stream))
+    pointers = ctypes.c_void_p * n
+    rc = load().mpt_kv_merge(n, lse.numel(), shape[-1], pointers(*[p.data_ptr() for p in parts]),
+                             pointers(*[l.data_ptr() for l in lses]), kind, out.data_ptr(), _KIND.get(out.dtype, -1),
+                             lse.data_ptr(), at)
     if rc:
         _check(rc, "mpt_kv_merge")
     return out, lse
