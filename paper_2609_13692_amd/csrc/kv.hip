@@ -189,10 +189,30 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
 
 // One tensor's rows of the first `tokens` slots, page a to page b of a layer:
 // 16 bytes per lane and step, in the order in which the rows lie in memory.
-__device__ inline void copy_rows(char *base, const int64_t *stride, int64_t layer, int a, int b, int tokens, int heads,
-                                 int units) {
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline void copy_rows(char *base, const int64_t *stride, int64_t layer, int a, int b, int tokens,
+                                 int page_size, int heads, int units) {
     const int64_t from = layer * stride[0] + (int64_t)a * stride[1], to = layer * stride[0] + (int64_t)b * stride[1];
     const bool slots_inside = stride[2] < stride[3];
+    // rows without gaps between them: as one run
+    const int64_t row_size = units * 8, other = (slots_inside ? page_size : heads) * row_size;
+    if ((slots_inside ? stride[2] == row_size && stride[3] == other && tokens == page_size
+                      : stride[3] == row_size && stride[2] == other)) {
+        const char *a0 = base + 2 * from;
+        char *b0 = base + 2 * to;
+        const int total = tokens * heads * units;
+        int x = threadIdx.x;
+        for (; x + 7 * (int)blockDim.x < total; x += 8 * blockDim.x) {
+            u32x4 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = __builtin_nontemporal_load((const u32x4 *)a0 + x + u * blockDim.x);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) __builtin_nontemporal_store(v[u], (u32x4 *)b0 + x + u * blockDim.x);
+        }
+        for (; x < total; x += blockDim.x) ((u32x4 *)b0)[x] = ((const u32x4 *)a0)[x];
+        return;
+    }
     const int inner = slots_inside ? tokens : heads, total = tokens * heads * units;
     const int64_t s_in = slots_inside ? stride[2] : stride[3], s_out = slots_inside ? stride[3] : stride[2];
     int x = threadIdx.x;
@@ -234,9 +254,9 @@ __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t 
         const int to = p.a[first], units = c.head_dim / 8;
         for (int y = blockIdx.y; y < 2 * c.n_layers; y += gridDim.y) {
             if (y & 1)
-                copy_rows((char *)c.v, c.v_stride, y >> 1, from, to, part, c.n_heads, units);
+                copy_rows((char *)c.v, c.v_stride, y >> 1, from, to, part, c.page_size, c.n_heads, units);
             else
-                copy_rows((char *)c.k, c.k_stride, y >> 1, from, to, part, c.n_heads, units);
+                copy_rows((char *)c.k, c.k_stride, y >> 1, from, to, part, c.page_size, c.n_heads, units);
         }
     }
     if (blockIdx.y) return;
@@ -375,9 +395,9 @@ __global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Plan p, int tab
         const int j = (int)(x / (2 * c.n_layers)), rest = (int)(x - (int64_t)j * 2 * c.n_layers);
         const int a = p.a[j], b = p.b[j];
         if (rest & 1)
-            copy_rows((char *)c.v, c.v_stride, rest >> 1, a, b, c.page_size, c.n_heads, units);
+            copy_rows((char *)c.v, c.v_stride, rest >> 1, a, b, c.page_size, c.page_size, c.n_heads, units);
         else
-            copy_rows((char *)c.k, c.k_stride, rest >> 1, a, b, c.page_size, c.n_heads, units);
+            copy_rows((char *)c.k, c.k_stride, rest >> 1, a, b, c.page_size, c.page_size, c.n_heads, units);
         if (tables && rest == 0 && threadIdx.x == 0) {
             c.ref[b] = c.ref[a];
             c.ref[a] = 0;
