@@ -605,8 +605,12 @@ int mpt_kv_append(const mpt_kv_cache *cache, int layer, int n, const int32_t *se
                   int64_t k_token_stride, int64_t k_head_stride, const void *v_new,
                   int64_t v_token_stride, int64_t v_head_stride, void *stream);
 
-/* Bytes of device workspace (256-byte aligned) for mpt_kv_attention of up to
- * n_tokens tokens with n_q_heads query heads (0 for sizes out of range). */
+/* Bytes of device workspace (256-byte aligned) for mpt_kv_attention of n
+ * entries and n_tokens tokens with n_q_heads query heads: at most 68 MiB, the
+ * partial sums of two tiles per workgroup (0 for sizes out of range: n <=
+ * MPT_KV_MAX_ENTRIES, n_tokens <= 2^30, and as many rows n_tokens * n_q_heads /
+ * n_heads). */
+#define MPT_KV_MAX_ENTRIES 65536
 size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_t n_tokens,
                                         int n_q_heads);
 
@@ -621,7 +625,8 @@ size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_
  *     lse = log sum exp(s_t),   out = sum exp(s_t - lse) v_t.
  * Rows that see no token (or only scores of minus infinity) get out = 0 and
  * lse = minus infinity. What lies in tokens that a row does not see, NaN and
- * infinities included, has no effect on it. Decoding is a chunk of one token;
+ * infinities included, has no effect on it; bad slots count as empty, tokens on
+ * bad pages as zeros, and tokens of no entry get no output. Decoding is a chunk of one token;
  * a prefix that several sequences share is one slot with all of their queries
  * and causal = 0, joined with their own parts (kv_begin) by mpt_kv_merge.
  *   seqs [n]       device; a slot may be listed several times

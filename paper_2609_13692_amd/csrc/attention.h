@@ -49,7 +49,7 @@ struct Part {
 };
 
 constexpr int kEntries = 256;                         // entries whose sizes are held at a time
-constexpr int kMaxEntries = kEntries * kEntries;
+static_assert(MPT_KV_MAX_ENTRIES == kEntries * kEntries, "Entries::chunk has a place for each 256");
 
 struct Entries {
     int q0[kEntries], n[kEntries], len[kEntries], begin[kEntries], slot[kEntries];
@@ -400,7 +400,7 @@ __device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
 
 inline int pad_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
-// Launch of one kernel for the sizes of a call; false if the launch failed.
+// Launch of a kernel and of its join.
 void launch_wide(const Attn &a, int waves, hipStream_t s);
 void launch_narrow(const Attn &a, hipStream_t s);
 

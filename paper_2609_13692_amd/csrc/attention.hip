@@ -43,7 +43,7 @@ using namespace mptkv;
 
 extern "C" size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_t n_tokens, int n_q_heads) {
     mptlib::clear_error();
-    if (check_cache(cache) != MPT_OK || n < 0 || n > kMaxEntries || n_tokens < 0 || n_tokens > (1 << 30) || n_q_heads < 1 ||
+    if (check_cache(cache) != MPT_OK || n < 0 || n > MPT_KV_MAX_ENTRIES || n_tokens < 0 || n_tokens > (1 << 30) || n_q_heads < 1 ||
         n_q_heads > 65535 || n_q_heads % cache->n_heads)
         return 0;
     return attention_bytes(*cache, n, n_tokens, n_q_heads);
@@ -58,7 +58,7 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
     return mptlib::guarded(__func__, [&]() -> int {
         if (int rc = check_cache(cache)) return rc;
         if (layer < 0 || layer >= cache->n_layers) return fail(MPT_E_INVALID, "layer = %d", layer);
-        if (n < 0 || n > kMaxEntries || n_tokens < 0 || n_tokens > (1 << 30))
+        if (n < 0 || n > MPT_KV_MAX_ENTRIES || n_tokens < 0 || n_tokens > (1 << 30))
             return fail(MPT_E_INVALID, "n = %d, n_tokens = %lld", n, (long long)n_tokens);
         if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % cache->n_heads)
             return fail(MPT_E_INVALID, "n_q_heads = %d is no multiple of the cache's %d", n_q_heads, cache->n_heads);
@@ -94,7 +94,10 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
         a.out_f32 = out_dtype == MPT_KV_F32, a.causal = causal != 0, a.flip = scale < 0;
         a.window = window < (1 << 30) ? window : 0;         // no sequence is longer
         const float log2e = 1.44269504088896341f;
-        a.factor = softcap > 0 ? std::fabs(scale) / softcap : std::fabs(scale) * log2e;
+        // not 0, which times the minus infinity of a hidden token would be NaN
+        a.factor = std::fmax(softcap > 0 ? std::fabs(scale) / softcap : std::fabs(scale) * log2e, 1e-37f);
+        if (!std::isfinite(a.factor) || !std::isfinite(softcap * log2e))
+            return fail(MPT_E_INVALID, "scale = %g, softcap = %g", scale, softcap);
         a.cap = softcap * log2e;
         for (int i = 1; i < 3; ++i)
             if (cache->k_stride[i] / 8 * (i == 2 ? cache->page_size : 1) > UINT32_MAX ||

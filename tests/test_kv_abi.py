@@ -85,7 +85,7 @@ def test_append_and_attention_check_their_arguments(lib):
     assert lib.mpt_kv_append(p, 0, 0, None, None, 0, None, 8, 8, None, 8, 8, None) == 0
     need = lib.mpt_kv_attention_workspace_bytes(p, 1, 1, 32)
     assert need >= 256 and need % 256 == 0
-    for n, t, h in ((-1, 1, 32), (1, -1, 32), (1, 1 << 31, 32), (1, 1, 0), (1, 1, 12)):
+    for n, t, h in ((-1, 1, 32), (65537, 1, 32), (1, -1, 32), (1, (1 << 30) + 1, 32), (1, 1 << 31, 32), (1, 1, 0), (1, 1, 12)):
         assert lib.mpt_kv_attention_workspace_bytes(p, n, t, h) == 0
     ok = dict(layer=0, n=1, seqs=DUMMY, q_off=DUMMY, tokens=1, heads=32, q=DUMMY, qs=[4096, 128], out=DUMMY, os=[4096, 128],
               out_dtype=0, window=0, softcap=0.0, scale=1.0, ws=4096, ws_bytes=need)
@@ -95,14 +95,15 @@ def test_append_and_attention_check_their_arguments(lib):
         return lib.mpt_kv_attention(p, a["layer"], a["n"], a["seqs"], a["q_off"], a["tokens"], a["heads"], a["q"], *a["qs"],
                                     a["out"], *a["os"], a["out_dtype"], None, None, 1, a["window"], a["softcap"], a["scale"],
                                     a["ws"], a["ws_bytes"], None)
-    for bad in (dict(layer=2), dict(n=-1), dict(n=(1 << 20) + 1), dict(tokens=1 << 31), dict(heads=0), dict(heads=12), dict(seqs=None),
+    for bad in (dict(layer=2), dict(n=-1), dict(n=65537), dict(n=(1 << 20) + 1), dict(tokens=(1 << 30) + 1), dict(tokens=1 << 31), dict(heads=0), dict(heads=12), dict(seqs=None),
                 dict(q_off=None), dict(q=None), dict(out=None), dict(q=DUMMY + 8), dict(out=DUMMY + 4), dict(qs=[4, 8]),
                 dict(os=[8, 9]), dict(out_dtype=1), dict(out_dtype=3), dict(window=-1), dict(softcap=-1.0),
-                dict(softcap=float("nan")), dict(softcap=float("inf")), dict(scale=float("nan"))):
+                dict(softcap=float("nan")), dict(softcap=float("inf")), dict(scale=float("nan")), dict(softcap=1e-30, scale=1e20)):
         assert call(**bad) == -1, bad
     for bad in (dict(ws=None), dict(ws=4096 + 16), dict(ws_bytes=need - 1)):
         assert call(**bad) == -6, bad
     assert call(n=0) == 0 and call(tokens=0) == 0
+    assert lib.mpt_kv_attention_workspace_bytes(p, 25, 8250, 32) <= 68 << 20
 
 
 def test_merge_checks_its_arguments(lib):
