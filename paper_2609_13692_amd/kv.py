@@ -58,8 +58,10 @@ class KvCache:
     per page: together the state described at ``mpt_kv_cache``.
     :meth:`create` allocates and empties one.
 
-    The cache holds the workspaces of its calls, which grow as needed; calls
-    on one cache must be ordered (one stream, or events between streams).
+    The cache holds the workspaces of its calls: of attention one for each size
+    that its calls need (at most three), all of them for as long as the cache
+    lives, so that graphs captured earlier stay valid. Calls on one cache must
+    be ordered (one stream, or events between streams).
     """
 
     def __init__(self, k, v, table, length, ref, free_bits, status):
@@ -98,7 +100,8 @@ class KvCache:
             raise MptError(-1, "mpt_kv_workspace_bytes", self._lib.mpt_last_error().decode())
         self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         self._ws_at, self._ws_bytes = self._ws.data_ptr(), n
-        self._at_ws, self._at_bytes, self._at_sizes, self._scale = None, 0, {}, 1.0 / math.sqrt(dim)
+        self._ws_stream = torch._C._cuda_getCurrentRawStream(self._index) or None
+        self._at_ws, self._at_sizes, self._scale = {}, {}, 1.0 / math.sqrt(dim)
 
     @classmethod
     def create(cls, n_layers, n_pages, page_size, n_heads, head_dim, max_seqs, max_len, dtype=torch.bfloat16,
@@ -125,6 +128,16 @@ class KvCache:
         _check(self._lib.mpt_kv_status(self._p, ctypes.addressof(bits), _on(stream, self._index)[0]), "mpt_kv_status")
         return [name for bit, name in STATUS_BITS.items() if bits.value & bit]
 
+    def _on(self, stream):
+        """As the function _on. The allocator learns of a stream that the
+        workspaces were not used on before."""
+        at, under = _on(stream, self._index)
+        if at != self._ws_stream:
+            self._ws_stream = at
+            for ws in (self._ws, *self._at_ws.values()):
+                ws.record_stream(stream or torch.cuda.current_stream(self._index))
+        return at, under
+
     def _pages(self, name, lists, check, stream):
         out = ctypes.c_int64(0) if check else None
         args = []
@@ -132,7 +145,7 @@ class KvCache:
             n = lists[0].numel()
             args = [n] + [None if t is None else _list(t, n, name, self._index) for t in lists]
         rc = getattr(self._lib, name)(self._p, *args, ctypes.addressof(out) if check else None, self._ws_at,
-                                      self._ws_bytes, _on(stream, self._index)[0])
+                                      self._ws_bytes, self._on(stream)[0])
         if rc:
             _check(rc, name)
         return out.value if check else None
@@ -187,7 +200,7 @@ class KvCache:
         mpt_kv_attention). scale defaults to 1 / sqrt(dim)."""
         tokens, heads, dim = q.shape
         n, index = seqs.numel(), self._index
-        at, under = _on(stream, index)
+        at, under = self._on(stream)
         if out is None:
             out = _new((tokens, heads, dim), out_dtype or self.dtype, self.device, under)
         elif out.shape[0] != tokens or (out_dtype or out.dtype) != out.dtype:
@@ -202,17 +215,14 @@ class KvCache:
             need = self._lib.mpt_kv_attention_workspace_bytes(self._p, n, tokens, heads)
             if len(self._at_sizes) < 4096:
                 self._at_sizes[key] = need
-        if need > self._at_bytes:
-            if self._at_ws is not None and under is not None:
-                self._at_ws.record_stream(stream)      # calls on it may still use the smaller one
-            self._at_ws = _new(need, torch.uint8, self.device, under)
-            self._at_bytes = need
-        ws = self._at_ws
+        ws = self._at_ws.get(need)
+        if ws is None:
+            ws = self._at_ws[need] = _new(need, torch.uint8, self.device, under)
         rc = self._lib.mpt_kv_attention(
             self._p, layer, n, _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index), tokens, heads,
             *self._rows(q, heads, "q", self.dtype), *self._rows(out, heads, "out", out.dtype), _KIND.get(out.dtype, -1),
-            lse.data_ptr(), None if kv_begin is None else _list(kv_begin, n, "kv_begin", index), 1 if causal else 0, window,
-            softcap, self._scale if scale is None else scale, ws.data_ptr() if ws is not None else None, self._at_bytes, at)
+            lse.data_ptr(), None if kv_begin is None else _list(kv_begin, n, "kv_begin", index), 1 if causal else 0,
+            min(window, 1 << 30), softcap, self._scale if scale is None else scale, ws.data_ptr(), need, at)
         if rc:
             _check(rc, "mpt_kv_attention")
         return out, lse

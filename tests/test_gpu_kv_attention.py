@@ -270,6 +270,37 @@ def test_replays_of_a_captured_call():
         assert c.take_status() == []
 
 
+def test_replays_after_calls_of_other_sizes():
+    """A graph captured with the workspace of a decode step, replayed after
+    eager calls that need other workspaces, on other streams, and after their
+    memory could have been handed out again."""
+    c, slots, ks, vs = filled([500, 70], 16, 2, 64, torch.bfloat16, 34)
+    q = torch.randn((2, 8, 64), device="cuda").bfloat16()
+    off = ints([0, 1, 2])
+    out, lse = c.attend(1, q, off, slots)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(1, q, off, slots, out=out, lse=lse)
+    side = torch.cuda.Stream()
+    for counts in ([30, 17], [300, 70], [1, 1]):
+        many = torch.randn((sum(counts), 8, 64), device="cuda").bfloat16()
+        side.wait_stream(torch.cuda.current_stream())
+        big, _ = c.attend(1, many, ints(np.concatenate([[0], np.cumsum(counts)])), slots, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        filler = [torch.full((1 << 22,), 3.0, device="cuda") for _ in range(24)]
+        q.normal_()
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all((x == 3.0).all() for x in filler)
+        want, want_lse = c.attend(1, q, off, slots)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), counts
+        check(c, slots, ks, vs, counts, 8, 35, torch.bfloat16)
+        del filler, big, many
+    assert c.take_status() == []
+
+
 def test_another_stream():
     c, slots, ks, vs = filled([300, 40], 16, 2, 64, torch.bfloat16, 31)
     q = torch.randn((2, 8, 64), device="cuda").bfloat16()
