@@ -34,6 +34,7 @@ struct Attn {
     float factor;                                     // |scale| log2(e), or |scale| / softcap
     float cap;                                        // softcap log2(e)
     uint32_t k_page, k_slot, v_page, v_slot;          // strides in 16-byte units
+    int near;                                         // offsets of a head's rows have 32 bits, factors 24
     const char *k, *v;                                // of the layer
     int64_t k_head, v_head;                           // bytes
     int workers;
@@ -267,6 +268,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -329,6 +331,13 @@ __device__ inline void load_lds16(const char *from, uint32_t lds) {
 __device__ inline void load_lds4(const void *from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory");
 }
+// The same at 32-bit offsets from one address.
+__device__ inline void load_lds16(const void *base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(uniform((int)lds)), "v"(offset), "s"(uniform((int64_t)base)) : "memory");
+}
+__device__ inline void load_lds4(const void *base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(uniform((int)lds)), "v"(offset), "s"(uniform((int64_t)base)) : "memory");
+}
 // Waits until at most N of the wave's later loads are on their way: loads
 // arrive in order, so all before those N have.
 template <int N>
@@ -347,10 +356,22 @@ __device__ inline uint64_t row_at(uint32_t page, uint32_t slot, uint32_t page_st
     return ((uint64_t)page * page_stride + (uint64_t)slot * slot_stride) << 4;
 }
 
+template <class V>
+__device__ inline V from_lds(uint32_t at) {
+    return *(const __attribute__((address_space(3))) V *)(uintptr_t)at;
+}
+
 // Four elements of one column from four rows: the lanes of 16 exchange what
 // they read, lane i of them getting column i.
-__device__ inline s16x4 read_column4(const char *lds) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)lds);
+__device__ inline s16x4 read_column4(uint32_t at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)at);
+}
+__device__ inline s16x4 read_column4(const char *lds) { return read_column4(lds_address(lds)); }
+
+template <class T>
+__device__ inline uint32_t pack(float x, float y) {
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, t2));
 }
 
 // Positions in log2 units of a score x = q.k: x |scale| log2(e), or with a

@@ -105,6 +105,11 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
                 return fail(MPT_E_INVALID, "cache: a page, or the stride of pages, of 64 GiB or more");
         a.k_page = (uint32_t)(cache->k_stride[1] / 8), a.k_slot = (uint32_t)(cache->k_stride[2] / 8);
         a.v_page = (uint32_t)(cache->v_stride[1] / 8), a.v_slot = (uint32_t)(cache->v_stride[2] / 8);
+        const auto near = [&](uint64_t page, uint64_t slot) {
+            return cache->n_pages <= 1 << 24 && page < 1 << 24 &&
+                   (cache->n_pages - 1) * page + (cache->page_size - 1) * slot + a.units <= 1 << 28;
+        };
+        a.near = near(a.k_page, a.k_slot) && near(a.v_page, a.v_slot);
         a.k = (const char *)cache->k + 2 * layer * cache->k_stride[0];
         a.v = (const char *)cache->v + 2 * layer * cache->v_stride[0];
         a.k_head = 2 * cache->k_stride[3], a.v_head = 2 * cache->v_stride[3];

@@ -1,5 +1,5 @@
 // Attention kernel for many rows per key head (chunks of new tokens): tiles of
-// 128 rows, 32 to each of the four waves.
+// 128 or 256 rows, 32 to each of the four or eight waves.
 //
 // Scores are formed transposed, S' = K Q', with 32x32x16 products: lane l then
 // holds query l % 32 and 16 of 32 tokens, so the running maximum and sum of a
@@ -12,8 +12,19 @@
 // The maximum that weights are taken against is moved only when a score
 // exceeds it by 2^8: products with weights up to 256 are as exact, and the
 // sums are rescaled a few times per row instead of at every step.
+//
+// What bounds it is the instructions that the vector units issue beside the
+// products: 16 exponentials and 56 others for 32 tokens of a wave with heads
+// of 128, against 16 products, with two waves to a SIMD. So tiles that nothing
+// is masked in run in groups, where places in LDS are constants, page ids are
+// clamped instead of selected by, and offsets into the pool have 32 bits; one
+// more instruction per operand read cost 3%. Chunks of 1024 tokens over 16k,
+// 32 heads on 8 of 128: 1140 us without such groups, 1053 with them (1000
+// TFLOP/s; a library product of 8192^3 reaches 1210 on this card).
 
 #include "attention.h"
+
+#include <type_traits>
 
 namespace mptkv {
 
@@ -30,8 +41,9 @@ struct Wide {
     // CU or rows are long, else four. Page ids are fetched for twice as many.
     static constexpr int C = 8;                                        // a tile's cost besides its steps, in steps
     static constexpr int S = WAVES == 8 ? 4 : 2, IDS = 2 * S;
-    // Operands read from LDS ahead of their products: with one wave to a SIMD
-    // nothing else covers the latency.
+    // Operands read from LDS ahead of their products (heads of 128: one 1118
+    // us, two 1053, three, with more registers than there are, 1163); with one
+    // wave to a SIMD nothing else covers the latency.
     static constexpr int kAhead = DP == 256 ? 6 : 2;
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight
@@ -55,21 +67,19 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
     const int shift = 31 - __clz(c.page_size);
     const uint32_t k_lds = uniform((int)(lds_address(keys) + wave * 1024)), v_lds = uniform((int)(lds_address(values) + wave * 1024));
     const uint32_t id_lds = uniform((int)(lds_address(ids) + wave * IDS * BN * 4));
-    // the thread's tokens of a tile are kStride apart from `own` on; its pieces
-    // of their rows; the rows' places in a page whose slots are counted from
-    // the tile's first (a tile is a part of a page, or pages are of the tile)
+    // The thread's tokens of a tile are kStride apart from `own` on: its pieces
+    // of their rows, and with them the first one's place in a page whose slots
+    // are counted from the tile's first (a tile is a part of a page, or pages
+    // are of the tile), for pools whose offsets have 32 bits.
     const int own = tid / CH, kp = (tid % CH) ^ W::k_swizzle(own), vp = (tid % CH) ^ W::v_swizzle(own);
-    const bool k_in = kp < a.units, v_in = vp < a.units;
-    uint32_t k_slot[L], v_slot[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-        k_slot[i] = (uint32_t)((i * W::kStride + own) & (c.page_size - 1)) * a.k_slot;
-        v_slot[i] = (uint32_t)((i * W::kStride + own) & (c.page_size - 1)) * a.v_slot;
-    }
-    // where a lane reads its operands: rows of 32 tokens of keys, 8 of values
-    const int k_row = col * ROW, k_flip = half ^ W::k_swizzle(col);
+    const uint32_t k_near = (uint32_t)(own & (c.page_size - 1)) * a.k_slot + kp, v_near = (uint32_t)(own & (c.page_size - 1)) * a.v_slot + vp;
+    const bool near = a.near && a.units == CH;
+    // Where a lane reads its operands: rows of 32 tokens of keys, 8 of values.
+    // Rows are as long as the swizzle reaches, so a piece's place is the
+    // first's with some bits turned over.
+    const uint32_t k_at = lds_address(keys) + col * ROW + 16 * (half ^ W::k_swizzle(col));
     const int v_of = 4 * half + (lane & 15) / 4;
-    const int v_row = v_of * ROW + (lane & 1) * 8, v_flip = (((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ W::v_swizzle(v_of);
+    const uint32_t v_at = lds_address(values) + v_of * ROW + (lane & 1) * 8 + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ W::v_swizzle(v_of));
     bool lost = false;                         // a page id outside the pool
 
     Walk<M, BN, C> walk;
@@ -90,6 +100,15 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         const int32_t *table = c.table + (int64_t)uniform(ent.slot[e]) * c.max_pages;
         const bool active = row_base < rows;
 
+        // The pages of a tile's tokens (of some token of the range for those
+        // outside it, whose loads take zeros), on their way before the queries.
+        const char *kh = a.k + head * a.k_head, *vh = a.v + head * a.v_head;
+        auto fetch_ids = [&](int step) INLINE {
+            const int t = max(0, max(range.lo, min(range.hi - 1, step * BN + lane)));
+            load_lds4(table + (t >> shift), id_lds + ((step - first) & (IDS - 1)) * BN * 4);
+        };
+#pragma unroll
+        for (int i = 0; i < S; ++i) fetch_ids(first + i);
         // queries of the wave's rows as operands, and what each may see
         s16x8 qf[KK];
         const int r0 = row_base + col, rr = min(r0, rows - 1), j0 = token_of(a, rr), p0 = len - n + j0;
@@ -107,7 +126,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         seen_by_all(a, n, len, begin, min(row_base, rows - 1), min(row_base + 31, rows - 1), wave_lo, wave_hi);
         seen_by_all(a, n, len, begin, tile * M, min(tile * M + M, rows) - 1, tile_lo, tile_hi);
 
-        f32x16 o[DT], s;
+        f32x16 o[DT], s0, s1;
         s16x8 pf[2];
         float m = -INFINITY, l = 0;
         pf[0] = pf[1] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
@@ -116,40 +135,56 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[dt][r] = 0;
 
-        // The pages of a tile's tokens (of some token of the range for those
-        // outside it, whose loads take zeros), and its keys or values.
-        const char *kh = a.k + head * a.k_head + 16 * kp, *vh = a.v + head * a.v_head + 16 * vp;
-        auto fetch_ids = [&](int step) INLINE {
-            const int t = max(0, max(range.lo, min(range.hi - 1, step * BN + lane)));
-            load_lds4(table + (t >> shift), id_lds + (step & (IDS - 1)) * BN * 4);
-        };
-        auto load = [&](int step, const char *rows0, bool in, const uint32_t (&slot)[L], uint32_t page_stride, uint32_t slot_stride, uint32_t lds) INLINE {
-            const char *tile0 = rows0 + ((uint64_t)((uint32_t)(step * BN) & (c.page_size - 1)) * slot_stride << 4);
-            const int *page = ids + (wave * IDS + (step & (IDS - 1))) * BN + own;
+        // The keys or values of a tile. What places them is formed here, not
+        // kept: the main loop takes every register.
+        auto load = [&](int step, const char *rows0, auto swizzle, uint32_t page_stride, uint32_t slot_stride, uint32_t lds) INLINE {
+            const int at = renewed(tid), token = at / CH, piece = (at % CH) ^ swizzle(token);
+            const bool in = piece < a.units;
+            const char *tile0 = rows0 + 16 * piece + ((uint64_t)((uint32_t)(step * BN) & (c.page_size - 1)) * slot_stride << 4);
+            const int *page = ids + (wave * IDS + ((step - first) & (IDS - 1))) * BN + token;
             auto all = [&](auto seen) INLINE {
 #pragma unroll
                 for (int i = 0; i < L; ++i) {
                     const int id = page[i * W::kStride];
                     const bool there = (unsigned)id < (unsigned)c.n_pages, see = seen(i);
                     lost |= see && !there;
-                    const uint64_t u = (uint64_t)(uint32_t)id * page_stride + slot[i];
-                    load_lds16(or_zeros(see && there && in, tile0 + (u << 4)), lds + (step & (S - 1)) * TILE + i * 16 * THREADS);
+                    const uint32_t slot = (uint32_t)(i * W::kStride + token) & (c.page_size - 1);
+                    load_lds16(or_zeros(see && there && in, tile0 + row_at(id, slot, page_stride, slot_stride)),
+                               lds + ((step - first) & (S - 1)) * TILE + i * 16 * THREADS);
                 }
             };
             if (step * BN >= range.lo && step * BN + BN <= range.hi)
                 all([](int) INLINE { return true; });
             else
-                all([&](int i) INLINE { return (unsigned)(step * BN + i * W::kStride + own - range.lo) < (unsigned)(range.hi - range.lo); });
+                all([&](int i) INLINE { return (unsigned)(step * BN + i * W::kStride + token - range.lo) < (unsigned)(range.hi - range.lo); });
         };
-        auto load_keys = [&](int step) INLINE { load(step, kh, k_in, k_slot, a.k_page, a.k_slot, k_lds); };
-        auto load_values = [&](int step) INLINE { load(step, vh, v_in, v_slot, a.v_page, a.v_slot, v_lds); };
+        auto load_keys = [&](int step) INLINE { load(step, kh, [](int t) INLINE { return W::k_swizzle(t); }, a.k_page, a.k_slot, k_lds); };
+        auto load_values = [&](int step) INLINE { load(step, vh, [](int t) INLINE { return W::v_swizzle(t); }, a.v_page, a.v_slot, v_lds); };
+        // The same for whole tiles (CH pieces a row) of pools whose offsets have 32 bits. A page
+        // id outside the pool becomes the last page, and is reported.
+        auto fetch_ids_near = [&](int step) INLINE {
+            const int t = min(range.hi - 1, step * BN + renewed(lane));
+            load_lds4(table, (uint32_t)(t >> shift) * 4, id_lds + ((step - first) & (IDS - 1)) * BN * 4);
+        };
+        auto load_near = [&](int step, const char *rows0, uint32_t slot, uint32_t page_stride, uint32_t slot_stride, uint32_t lds) INLINE {
+            const int *page = ids + (wave * IDS + ((step - first) & (IDS - 1))) * BN + own;
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const uint32_t id = page[i * W::kStride], there = min(id, (uint32_t)c.n_pages - 1);
+                lost |= id != there;
+                // own is less than kStride: the other tokens' bits of a slot are the same for all lanes
+                const char *from = rows0 + ((uint64_t)((uint32_t)(step * BN + i * W::kStride) & (c.page_size - 1)) * slot_stride << 4);
+                load_lds16(from, (__umul24(there, page_stride) + slot) << 4, lds + i * 16 * THREADS);
+            }
+        };
         // The products of a step, in groups that the compiler keeps in order:
         // an operand from LDS (read some groups ahead), its product, and beside
         // it a share of the step's other work.
-        // S' = K Q' of 32 tokens
-        auto multiply = [&](const char *kb, auto beside) INLINE {
+        // S' = K Q' of 32 tokens (base: where the lane's first
+        // operand lies; kb, vb: bytes from there, constants)
+        auto multiply = [&](uint32_t base, int kb, f32x16 &s, auto beside) INLINE {
             s16x8 kf[AHEAD + 1];
-            auto read = [&](int kk) INLINE { kf[kk % (AHEAD + 1)] = *(const s16x8 *)(kb + k_row + (((2 * kk) ^ k_flip) << 4)); };
+            auto read = [&](int kk) INLINE { kf[kk % (AHEAD + 1)] = from_lds<s16x8>((base ^ 32 * kk) + kb); };
 #pragma unroll
             for (int kk = 0; kk < AHEAD; ++kk) read(kk);
 #pragma unroll
@@ -161,10 +196,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             }
         };
         // O' += V' P' of 32 tokens
-        auto add = [&](const char *vb, auto beside) INLINE {
+        auto add = [&](uint32_t base, int vb, auto beside) INLINE {
             s16x8 vf[AHEAD + 1];
             auto read = [&](int i) INLINE {
-                const char *x = vb + (i / DT) * 16 * ROW + v_row + (((i % DT * 4) ^ v_flip) << 4);
+                const uint32_t x = (base ^ 64 * (i % DT)) + vb + (i / DT) * 16 * ROW;
                 const s16x4 y = read_column4(x), z = read_column4(x + 8 * ROW);
                 vf[i % (AHEAD + 1)] = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
             };
@@ -179,27 +214,27 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             }
         };
         auto nothing = [](int) INLINE {};
-        // One step of 32 tokens from t0: products with the values of the step
-        // before beside this step's maximum, scores of the next step beside
-        // this step's weights.
-        auto step32 = [&](int t0, const char *k_next, const char *v_before) INLINE {
-            f32x16 x = s;
+        // One step of 32 tokens from t0 with scores x: products with the values
+        // of the step before beside this step's maximum, scores of the next
+        // step beside this step's weights.
+        auto step32 = [&](auto all_seen, f32x16 &x, f32x16 &next, int t0, uint32_t k_base, int k_next, uint32_t v_base, int v_before) INLINE {
             if constexpr (CAP) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] = score<true>(a, x[r]);
             }
-            if (t0 < wave_lo || t0 + 32 > wave_hi) {
+            if (!all_seen && (t0 < wave_lo || t0 + 32 > wave_hi)) {
+                const int before = t0 + 4 * renewed(half), lo = see_lo - before, hi = see_hi - before;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int t = t0 + 4 * half + 8 * (r / 4) + r % 4;
-                    if (!(t >= see_lo && t < see_hi)) x[r] = -INFINITY;
+                    const int t = 8 * (r / 4) + r % 4;
+                    if (!(t >= lo && t < hi)) x[r] = -INFINITY;
                 }
             }
             // between the two waves of a SIMD, the one with products to issue
             // goes before the one that forms addresses: 2% of the kernel
             __builtin_amdgcn_s_setprio(1);
             float top = -INFINITY;
-            add(v_before, [&](int i) INLINE {
+            add(v_base, v_before, [&](int i) INLINE {
                 constexpr int E = 8 / DT;
 #pragma unroll
                 for (int y = i * E; y < i * E + E; ++y) top = fmaxf(top, x[y]);
@@ -218,17 +253,21 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                 m = now;
             }
             const float base = m == -INFINITY ? 0.0f : m;
-            typename Type<T>::x8 w8;
-            multiply(k_next, [&](int i) INLINE {
+            float even = 0;
+            u32x4 packed[2];
+            multiply(k_base, k_next, next, [&](int i) INLINE {
                 constexpr int E = 16 / KK;
 #pragma unroll
                 for (int r = i * E; r < i * E + E; ++r) {
                     const float w = __builtin_amdgcn_exp2f(CAP ? x[r] - base : __builtin_fmaf(x[r], a.factor, -base));
                     l += w;
-                    w8[r % 8] = (T)w;
-                    if (r % 8 == 7) pf[r / 8] = __builtin_bit_cast(s16x8, w8);
+                    if (r % 2)
+                        packed[r / 8][r % 8 / 2] = pack<T>(even, w);
+                    else
+                        even = w;
                 }
             });
+            pf[0] = __builtin_bit_cast(s16x8, packed[0]), pf[1] = __builtin_bit_cast(s16x8, packed[1]);
             __builtin_amdgcn_s_setprio(0);
         };
         // Infinities and NaN in values of 32 tokens: a weight of zero does not
@@ -290,10 +329,8 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         constexpr int PER = 2 * L + 1;
         __syncthreads();                       // the previous rows' products have read their buffers
 #pragma unroll
-        for (int i = 0; i < S; ++i) fetch_ids(first + i);
-#pragma unroll
         for (int i = 0; i < L; ++i)            // the values "before" the first tile
-            *(uint4 *)(values + ((first - 1) & (S - 1)) * TILE + (i * THREADS + tid) * 16) = uint4{0, 0, 0, 0};
+            *(uint4 *)(values + (S - 1) * TILE + (i * THREADS + tid) * 16) = uint4{0, 0, 0, 0};
         arrived<0>();
         load_keys(first);
 #pragma unroll
@@ -307,13 +344,41 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         else
             arrived<0>();
         __syncthreads();
-        if (active) multiply(keys + (first & (S - 1)) * TILE, nothing);
-        for (int step = first; step < last; ++step) {
-            const int t0 = step * BN;
-            char *k_now = keys + (step & (S - 1)) * TILE, *k_next = keys + ((step + 1) & (S - 1)) * TILE;
-            char *v_now = values + (step & (S - 1)) * TILE, *v_before = values + ((step - 1) & (S - 1)) * TILE;
-            if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, v_before + 32 * ROW);
-            if (active) step32(t0, k_now + 32 * ROW, v_before + 32 * ROW);
+        if (active) multiply(k_at, 0, s0, nothing);
+        for (int step = first; step < last;) {
+            if constexpr (DP < 256) {
+                // S tiles whose tokens every row of the tile sees, with S more
+                // to load: places in LDS are constants, nothing is masked, and
+                // offsets into the pool have 32 bits. (Heads of 256 run out of
+                // registers here: 109 us against 98 for nine of them with a
+                // window.)
+                const int t0 = step * BN;
+                if (near && ((step - first) & (S - 1)) == 0 && (step == first ? t0 : t0 - 32) >= tile_lo &&
+                    t0 + S * BN <= tile_hi && step + 2 * S <= last && t0 + 2 * S * BN <= range.hi) {
+                    auto turn = [&](auto r_) INLINE {
+                        constexpr int R = decltype(r_)::value, N = (R + 1) % S, B = (R + S - 1) % S;
+                        if (active) step32(std::true_type(), s0, s1, 0, k_at, R * TILE + 32 * ROW, v_at, B * TILE + 32 * ROW);
+                        arrived<(S - 2) * PER>();
+                        __syncthreads();
+                        fetch_ids_near(step + R + 2 * S - 1);
+                        load_near(step + R + S - 1, vh, v_near, a.v_page, a.v_slot, v_lds + B * TILE);
+                        load_near(step + R + S, kh, k_near, a.k_page, a.k_slot, k_lds + R * TILE);
+                        if (active) step32(std::true_type(), s1, s0, 0, k_at, N * TILE, v_at, R * TILE);
+                    };
+                    turn(std::integral_constant<int, 0>());
+                    turn(std::integral_constant<int, 1>());
+                    if constexpr (S == 4) {
+                        turn(std::integral_constant<int, 2>());
+                        turn(std::integral_constant<int, 3>());
+                    }
+                    step += S;
+                    continue;
+                }
+            }
+            const int t0 = step * BN, at = (step - first) & (S - 1);
+            const int now = at * TILE, next = ((at + 1) & (S - 1)) * TILE, before = ((at - 1) & (S - 1)) * TILE;
+            if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, values + before + 32 * ROW);
+            if (active) step32(std::false_type(), s0, s1, t0, k_at + now, 32 * ROW, v_at + before, 32 * ROW);
             // all up to turn step + 1 - S; where turns had no tile left to
             // load their count is short of PER, and everything is waited for
             if (step + S - 1 < last)
@@ -326,21 +391,23 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                 load_values(step + S - 1);
                 if (step + S < last) load_keys(step + S);
             }
-            if (partly_seen(t0)) odd_values(t0, v_now);
-            if (active) step32(t0 + 32, k_next, v_now);
+            if (partly_seen(t0)) odd_values(t0, values + now);
+            if (active) step32(std::false_type(), s1, s0, t0 + 32, k_at + next, 0, v_at + now, 0);
+            ++step;
         }
         {
-            char *v_last = values + ((last - 1) & (S - 1)) * TILE + 32 * ROW;
-            const int t0 = last * BN - 32;
-            if (partly_seen(t0)) odd_values(t0, v_last);
-            if (active) add(v_last, nothing);
+            const int v_last = ((last - 1 - first) & (S - 1)) * TILE + 32 * ROW, t0 = last * BN - 32;
+            if (partly_seen(t0)) odd_values(t0, values + v_last);
+            if (active) add(v_at + v_last, 0, nothing);
         }
 
         const float sum = l + __shfl_xor(l, 32);
         if (starts && ends) {
-            if (r0 < rows) {
+            const int r = row_base + renewed(col);
+            if (r < rows) {
                 const float scale = sum == 0 ? 0.0f : 1.0f / sum;
-                const int64_t token = q0 + j0, hq = (int64_t)head * a.group + r0 - j0 * a.group;
+                const int j = token_of(a, r);
+                const int64_t token = q0 + j, hq = (int64_t)head * a.group + r - j * a.group;
                 if (a.lse && half == 0)
                     a.lse[token * a.heads + hq] = sum == 0 ? -INFINITY : 0.693147180559945f * (m + __builtin_amdgcn_logf(sum));
 #pragma unroll

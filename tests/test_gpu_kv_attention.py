@@ -220,6 +220,42 @@ def test_long_context_and_same_result_every_time():
             assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+LONG = [
+    # lengths, new tokens, heads, kv heads, dim, page: tiles of 256 rows, and of 128
+    ([1500, 900], [70, 64], 8, 2, 128, 16),
+    ([1700, 1300], [33, 50], 8, 1, 64, 256),
+    ([1100, 1031], [40, 20], 6, 2, 128, 1),
+    ([1000], [16], 4, 1, 64, 4),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: f"h{s[2]}k{s[3]}d{s[4]}p{s[5]}")
+def test_many_tokens_that_every_row_sees(shape, dtype):
+    """Chunks over contexts of many tiles of keys, which the kernel takes in
+    groups where nothing is masked: with the groups starting and ending at all
+    places, by lengths, windows and first visible tokens."""
+    lengths, counts, heads, kv_heads, dim, page = shape
+    c, slots, ks, vs = filled(lengths, page, kv_heads, dim, DT[dtype], 36, heads_first=page == 256)
+    check(c, slots, ks, vs, counts, heads, 37, DT[dtype])
+    check(c, slots, ks, vs, counts, heads, 38, DT[dtype], window=700, softcap=10.0)
+    check(c, slots, ks, vs, counts, heads, 39, DT[dtype], begin=[65 + 3 * i for i in range(len(counts))], causal=False)
+
+
+def test_bad_pages_inside_a_long_context():
+    """Ids outside the pool among many good ones are reported and not
+    followed, and do not matter to another sequence."""
+    c, slots, ks, vs = filled([1500, 1500], 16, 1, 128, torch.bfloat16, 40)
+    q = torch.randn((140, 4, 128), device="cuda").bfloat16()
+    off = ints([0, 70, 140])
+    want, _ = c.attend(1, q, off, slots)
+    for page, bad in ((40, 1 << 30), (41, -1), (93, c.ref.numel())):
+        c.table[int(slots[0]), page] = bad
+    got, _ = c.attend(1, q, off, slots)
+    assert c.take_status() == ["page"]
+    assert torch.equal(got[70:], want[70:])
+
+
 def test_many_short_sequences():
     lengths = [1 + (7 * i) % 90 for i in range(300)]
     c, slots, ks, vs = filled(lengths, 16, 1, 64, torch.bfloat16, 22)
