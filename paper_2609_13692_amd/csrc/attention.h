@@ -406,17 +406,18 @@ __device__ inline uint32_t odd8(s16x8 x) {
     return (((u.x & kE) + kOne) | ((u.y & kE) + kOne) | ((u.z & kE) + kOne) | ((u.w & kE) + kOne)) & 0x80008000u;
 }
 
-template <class T>
-__device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
-    if (a.out_f32) {
-        *(f32x4 *)(a.out + 4 * at) = x;
+template <class T, bool F32>
+__device__ inline void put4(char *out, int64_t at, f32x4 x) {
+    if constexpr (F32) {
+        *(f32x4 *)(out + 4 * at) = x;
     } else {
         typedef T t4 __attribute__((ext_vector_type(4)));
-        t4 y;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = (T)x[i];
-        *(t4 *)(a.out + 2 * at) = y;
+        *(t4 *)(out + 2 * at) = __builtin_convertvector(x, t4);
     }
+}
+template <class T>
+__device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
+    a.out_f32 ? put4<T, true>(a.out, at, x) : put4<T, false>(a.out, at, x);
 }
 
 inline int pad_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }

@@ -19,8 +19,15 @@
 // is masked in run in groups, where places in LDS are constants, page ids are
 // clamped instead of selected by, and offsets into the pool have 32 bits; one
 // more instruction per operand read cost 3%. Chunks of 1024 tokens over 16k,
-// 32 heads on 8 of 128: 1140 us without such groups, 1053 with them (1000
-// TFLOP/s; a library product of 8192^3 reaches 1210 on this card).
+// 32 heads on 8 of 128: 1140 us without such groups, 1053 with them.
+//
+// What bounds calls with few steps is the fetching of instructions, each of
+// which a workgroup meets for the first time. So outside the groups one piece
+// of code serves both halves of a tile, and one the loads of all tiles: the
+// kernels went from 70 to 47 KB (heads of 256) and from 52 to 40 (128), nine
+// chunks over up to 4099 tokens with a window from 101 to 92 us, 25 ragged
+// chunks over up to 8400 from 816 to 775 (797 TFLOP/s), the chunks above to
+// 1031 (1021 TFLOP/s; a library product of 8192^3 reaches 1210 on this card).
 
 #include "attention.h"
 
@@ -44,7 +51,7 @@ struct Wide {
     // Operands read from LDS ahead of their products (heads of 128: one 1118
     // us, two 1053, three, with more registers than there are, 1163); with one
     // wave to a SIMD nothing else covers the latency.
-    static constexpr int kAhead = DP == 256 ? 6 : 2;
+    static constexpr int kAhead = DP == 256 ? 3 : 2;
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight
     // tokens' pieces, values so that four tokens' 64 bytes, fall on all banks;
@@ -120,6 +127,8 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             u32x4 x = mptkv::load<u32x4>(or_zeros(r0 < rows && piece < a.units, q + 16 * piece));
             if (a.flip) x ^= 0x80008000u;
             qf[kk] = __builtin_bit_cast(s16x8, x);
+            // wide heads: in the registers that only products read, where they stay
+            if constexpr (DP == 256) asm volatile("" : "+a"(qf[kk]));
         }
         // tokens that all rows of the wave, and of the tile, see
         int wave_lo, wave_hi, tile_lo, tile_hi;
@@ -142,21 +151,16 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             const bool in = piece < a.units;
             const char *tile0 = rows0 + 16 * piece + ((uint64_t)((uint32_t)(step * BN) & (c.page_size - 1)) * slot_stride << 4);
             const int *page = ids + (wave * IDS + ((step - first) & (IDS - 1))) * BN + token;
-            auto all = [&](auto seen) INLINE {
 #pragma unroll
-                for (int i = 0; i < L; ++i) {
-                    const int id = page[i * W::kStride];
-                    const bool there = (unsigned)id < (unsigned)c.n_pages, see = seen(i);
-                    lost |= see && !there;
-                    const uint32_t slot = (uint32_t)(i * W::kStride + token) & (c.page_size - 1);
-                    load_lds16(or_zeros(see && there && in, tile0 + row_at(id, slot, page_stride, slot_stride)),
-                               lds + ((step - first) & (S - 1)) * TILE + i * 16 * THREADS);
-                }
-            };
-            if (step * BN >= range.lo && step * BN + BN <= range.hi)
-                all([](int) INLINE { return true; });
-            else
-                all([&](int i) INLINE { return (unsigned)(step * BN + i * W::kStride + token - range.lo) < (unsigned)(range.hi - range.lo); });
+            for (int i = 0; i < L; ++i) {
+                const int id = page[i * W::kStride];
+                const bool there = (unsigned)id < (unsigned)c.n_pages;
+                const bool see = (unsigned)(step * BN + i * W::kStride + token - range.lo) < (unsigned)(range.hi - range.lo);
+                lost |= see && !there;
+                const uint32_t slot = (uint32_t)(i * W::kStride + token) & (c.page_size - 1);
+                load_lds16(or_zeros(see && there && in, tile0 + row_at(id, slot, page_stride, slot_stride)),
+                           lds + ((step - first) & (S - 1)) * TILE + i * 16 * THREADS);
+            }
         };
         auto load_keys = [&](int step) INLINE { load(step, kh, [](int t) INLINE { return W::k_swizzle(t); }, a.k_page, a.k_slot, k_lds); };
         auto load_values = [&](int step) INLINE { load(step, vh, [](int t) INLINE { return W::v_swizzle(t); }, a.v_page, a.v_slot, v_lds); };
@@ -332,11 +336,12 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         for (int i = 0; i < L; ++i)            // the values "before" the first tile
             *(uint4 *)(values + (S - 1) * TILE + (i * THREADS + tid) * 16) = uint4{0, 0, 0, 0};
         arrived<0>();
-        load_keys(first);
-#pragma unroll
-        for (int i = 1; i < S; ++i) {
-            fetch_ids(first + S - 1 + i);
-            if (first + i - 1 < last) load_values(first + i - 1);
+#pragma unroll 1
+        for (int i = 0; i < S; ++i) {
+            if (i) {
+                fetch_ids(first + S - 1 + i);
+                if (first + i - 1 < last) load_values(first + i - 1);
+            }
             if (first + i < last) load_keys(first + i);
         }
         if (first + S - 1 < last)
@@ -350,7 +355,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                 // S tiles whose tokens every row of the tile sees, with S more
                 // to load: places in LDS are constants, nothing is masked, and
                 // offsets into the pool have 32 bits. (Heads of 256 run out of
-                // registers here: 109 us against 98 for nine of them with a
+                // registers here: 109 us against 98 for nine chunks with a
                 // window.)
                 const int t0 = step * BN;
                 if (near && ((step - first) & (S - 1)) == 0 && (step == first ? t0 : t0 - 32) >= tile_lo &&
@@ -375,24 +380,31 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                     continue;
                 }
             }
-            const int t0 = step * BN, at = (step - first) & (S - 1);
-            const int now = at * TILE, next = ((at + 1) & (S - 1)) * TILE, before = ((at - 1) & (S - 1)) * TILE;
-            if (step > first && partly_seen(t0 - 32)) odd_values(t0 - 32, values + before + 32 * ROW);
-            if (active) step32(std::false_type(), s0, s1, t0, k_at + now, 32 * ROW, v_at + before, 32 * ROW);
-            // all up to turn step + 1 - S; where turns had no tile left to
-            // load their count is short of PER, and everything is waited for
-            if (step + S - 1 < last)
-                arrived<(S - 2) * PER>();
-            else
-                arrived<0>();
-            __syncthreads();
-            if (step + S - 1 < last) {
-                fetch_ids(step + 2 * S - 1);
-                load_values(step + S - 1);
-                if (step + S < last) load_keys(step + S);
+            // any other tile, its two halves by one piece of code: a call with
+            // few steps waits for its instructions more than for anything else
+            const int at = (step - first) & (S - 1), now = at * TILE, next = ((at + 1) & (S - 1)) * TILE, before = ((at - 1) & (S - 1)) * TILE;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const int t = step * BN + 32 * h, v_before = h ? now : before + 32 * ROW;
+                if (t > first * BN && partly_seen(t - 32)) odd_values(t - 32, values + v_before);
+                if (active) {
+                    step32(std::false_type(), s0, s1, t, k_at + (h ? next : now + 32 * ROW), 0, v_at + v_before, 0);
+                    s0 = s1;
+                }
+                if (h) break;
+                // all up to turn step + 1 - S; where turns had no tile left to
+                // load their count is short of PER, and everything is waited for
+                if (step + S - 1 < last)
+                    arrived<(S - 2) * PER>();
+                else
+                    arrived<0>();
+                __syncthreads();
+                if (step + S - 1 < last) {
+                    fetch_ids(step + 2 * S - 1);
+                    load_values(step + S - 1);
+                    if (step + S < last) load_keys(step + S);
+                }
             }
-            if (partly_seen(t0)) odd_values(t0, values + now);
-            if (active) step32(std::false_type(), s1, s0, t0 + 32, k_at + next, 0, v_at + now, 0);
             ++step;
         }
         {
@@ -410,15 +422,18 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
                 const int64_t token = q0 + j, hq = (int64_t)head * a.group + r - j * a.group;
                 if (a.lse && half == 0)
                     a.lse[token * a.heads + hq] = sum == 0 ? -INFINITY : 0.693147180559945f * (m + __builtin_amdgcn_logf(sum));
+                const int64_t to = token * a.out_token + hq * a.out_head + 4 * half;
+                auto store = [&](auto f32) INLINE {
+                    char *row = a.out + (f32 ? 4 : 2) * to;
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const int d = dt * 32 + 2 * r + 4 * half;
-                        if (d < 8 * a.units)
-                            store4<T>(a, token * a.out_token + hq * a.out_head + d,
-                                      f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]} * scale);
+                    for (int x = 0; x < DT * 4; ++x) {
+                        if (x >= a.units) break;
+                        const f32x16 &y = o[x / 4];
+                        const int i = x % 4 * 4;
+                        put4<T, f32>(row, 8 * x, f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]} * scale);
                     }
+                };
+                a.out_f32 ? store(std::true_type()) : store(std::false_type());
             }
         } else {
             // unnormalised sums, in the order of the registers
