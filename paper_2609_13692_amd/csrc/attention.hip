@@ -16,18 +16,26 @@ struct Choice {
 };
 
 // By the rows that an entry has for a key head on average (the lengths are on
-// the device). Microseconds, narrow / 4 waves / 8 waves, 32 entries over 4000
-// tokens and 128 over 300, 4 query heads a key head:
-//   dim 128: 16 rows 115/168/153; 32 rows 126/169/154 and 68/80/100; 48 rows
-//   312/176/155; 64 rows 240/176/156 and 114/86/108; 128 rows 487/190/158 and
-//   215/105/207; 160 rows 606/248/171; 256 rows 939/263/184 and 447/182/161
-//   dim 64: 20 rows 105/70/83; 128 rows 339/87/94; 256 rows 656/126/119
-//   dim 256 (2000 tokens): 16 rows 108/157; 20 rows 202/156
+// the device), and for heads of 128 by whether a tile can have a CU for itself.
+// Microseconds, narrow / 4 waves / 8 waves, 4 query heads on each of 8 key
+// heads:
+//   dim 128, 32 entries over 4000 tokens: 16 rows 116/164/131; 32 rows
+//   122/164/131; 48 rows 302/173/132; 128 rows 452/192/139; 160 rows
+//   573/214/148; 256 rows 895/233/181. 32 over 300: 48 rows 33/32/28; 128 rows
+//   50/38/34. 8 over 4000: 48 rows 75/57/48; 128 rows 81/77/55; over 300 22/31/33
+//   dim 128, 128 entries over 300: 16 rows 39/54/69; 32 rows 62/52/70; 48 rows
+//   85/57/73; 128 rows 208/76/98; 256 rows 444/136/137. 128 over 4000, where it
+//   turns (the call does not know): 48 rows 1086/505/428; 128 rows 2863/547/471
+//   dim 64, 32 entries over 4000: 16 rows 54/61/62; 20 rows 95/62/65; 128 rows
+//   325/74/73; 256 rows 632/106/102. 128 over 4000: 128 rows 1459/219/293; 160
+//   rows 1840/421/355
+//   dim 256, 32 entries over 2000: 16 rows 105/132; 20 rows 198/135
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
+    const bool own_cu = dim == 128 && (int64_t)n * c.n_heads <= 256;
     if (rows <= (dim == 128 ? 32 : 16)) return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
-    if (rows <= 128 || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
+    if ((rows <= 128 && !own_cu) || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
     return {8, 256, 256};
 }
 

@@ -263,6 +263,17 @@ def test_many_short_sequences():
     check(c, slots, ks, vs, [1 + i % l for i, l in enumerate(lengths)], 2, 24, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_many_entries_of_a_few_rows_each(dtype):
+    """More tiles of 128 rows than the card has CUs, on either side of that
+    (heads of 128 go by another kernel there), over contexts of all lengths."""
+    for n in (128, 131):
+        lengths = [10 + (97 * i) % 641 for i in range(n)]
+        c, slots, ks, vs = filled(lengths, 16, 2, 128, DT[dtype], 41)
+        check(c, slots, ks, vs, [8 + i % 3 for i in range(n)], 8, 42, DT[dtype])
+        check(c, slots, ks, vs, [9] * n, 8, 43, DT[dtype], window=300, softcap=15.0)
+
+
 def test_decodes_and_a_chunk_in_one_batch():
     lengths = [500, 60, 200, 90, 31]
     c, slots, ks, vs = filled(lengths, 16, 2, 128, torch.bfloat16, 25)
