@@ -113,6 +113,11 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
     __shared__ uint32_t slots[kSlotBits / 32];
     __shared__ uint32_t err_all;
     const int tid = threadIdx.x;
+    // the free pages first: their words are on their way beside the lists
+    const int words = (c.n_pages + 63) / 64, per = (words + THREADS - 1) / THREADS;
+    const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
+    int64_t mine = 0;
+    for (int w = w0; w < w1; ++w) mine += __popcll(c.free_bits[w]);
     if (tid == 0) err_all = 0;
     __syncthreads();
     uint32_t err = check_list<THREADS>(n, dst, c.max_seqs, p.mark, slots, MPT_KV_BAD_SLOT);
@@ -162,11 +167,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
             if (slot_ok(c, dst[i])) p.mark[dst[i]] = src ? keep[i] : c.length[dst[i]];
         }
     }
-    const int words = (c.n_pages + 63) / 64, per = (words + THREADS - 1) / THREADS;
-    const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
-    int64_t mine = 0, free_all;
-    for (int w = w0; w < w1; ++w) mine += __popcll(c.free_bits[w]);
-    int64_t at = block_scan<THREADS>(mine, &free_all, lds);
+    int64_t free_all, at = block_scan<THREADS>(mine, &free_all, lds);
     if (need_all > free_all) err |= MPT_KV_NO_PAGES;
     if (err) atomicOr(&err_all, err);
     __syncthreads();
@@ -202,15 +203,17 @@ __device__ inline void copy_rows(char *base, const int64_t *stride, int64_t laye
         const char *a0 = base + 2 * from;
         char *b0 = base + 2 * to;
         const int total = tokens * heads * units;
-        int x = threadIdx.x;
-        for (; x + 7 * (int)blockDim.x < total; x += 8 * blockDim.x) {
+        // eight loads on their way at a time, of short runs too (one after the
+        // other, the tokens of a partial page took seven round trips)
+        for (int x = threadIdx.x; x < total; x += 8 * blockDim.x) {
             u32x4 v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = __builtin_nontemporal_load((const u32x4 *)a0 + x + u * blockDim.x);
+            for (int u = 0; u < 8; ++u)
+                if (x + u * (int)blockDim.x < total) v[u] = __builtin_nontemporal_load((const u32x4 *)a0 + x + u * blockDim.x);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) __builtin_nontemporal_store(v[u], (u32x4 *)b0 + x + u * blockDim.x);
+            for (int u = 0; u < 8; ++u)
+                if (x + u * (int)blockDim.x < total) __builtin_nontemporal_store(v[u], (u32x4 *)b0 + x + u * blockDim.x);
         }
-        for (; x < total; x += blockDim.x) ((u32x4 *)b0)[x] = ((const u32x4 *)a0)[x];
         return;
     }
     const int inner = slots_inside ? tokens : heads, total = tokens * heads * units;

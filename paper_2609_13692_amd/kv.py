@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -19,6 +20,7 @@ from .mpt import KvDescriptor, MptError, _check, load
 BF16, F16, F32 = 0, 1, 2
 _KIND = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 MAX_PARTS = 16
+_POINTERS = [struct.Struct(f"{n}P").pack for n in range(MAX_PARTS + 1)]      # host arrays of device pointers
 STATUS_BITS = {1: "slot", 2: "length", 4: "page", 8: "duplicate", 16: "not empty", 32: "no pages", 64: "shared page"}
 
 
@@ -46,6 +48,13 @@ def _new(shape, dtype, device, under):
         return torch.empty(shape, dtype=dtype, device=device)
     with under:                    # the allocator then orders reuse by that stream
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _like(t, dtype, under):
+    if under is None:
+        return torch.empty_like(t, dtype=dtype)
+    with under:
+        return torch.empty_like(t, dtype=dtype)
 
 
 class KvCache:
@@ -234,30 +243,30 @@ def merge(parts, lses, out_dtype=None, out=None, lse=None, stream=None):
     mpt_kv_merge)."""
     if len(parts) != len(lses) or not 1 <= len(parts) <= MAX_PARTS:
         raise ValueError(f"needs 1 .. {MAX_PARTS} parts, each with its lse")
-    first = parts[0]
+    first, first_lse = parts[0], lses[0]
     kind, index = _KIND.get(first.dtype), first.get_device()
     if kind is None or index < 0:
         raise TypeError(f"parts must be bfloat16, float16 or float32 device tensors, got {first.dtype} on {first.device}")
-    shape, device = first.shape, first.device
+    shape, dtype = first.shape, first.dtype
     rows = shape[:-1]
     for p, l in zip(parts, lses):
-        if p.shape != shape or p.dtype is not first.dtype or p.get_device() != index or not p.is_contiguous():
+        if p.dtype is not dtype or p.get_device() != index or not p.is_contiguous() or p.shape != shape:
             raise ValueError("parts must be contiguous device tensors of one shape and type")
-        if l.shape != rows or l.dtype is not torch.float32 or l.get_device() != index or not l.is_contiguous():
+        if l.dtype is not torch.float32 or l.get_device() != index or not l.is_contiguous() or l.shape != rows:
             raise ValueError("lses must be contiguous float32 device tensors of the parts' shape without the last dimension")
     at, under = _on(stream, index)
     if out is None:
-        out = _new(shape, out_dtype or first.dtype, device, under)
+        out = _like(first, out_dtype or dtype, under)
     elif out.shape != shape or out.get_device() != index or not out.is_contiguous() or (out_dtype or out.dtype) != out.dtype:
         raise ValueError("out must be a contiguous device tensor of the parts' shape and out_dtype")
     if lse is None:
-        lse = _new(rows, torch.float32, device, under)
+        lse = _like(first_lse, torch.float32, under)
     elif lse.shape != rows or lse.dtype is not torch.float32 or lse.get_device() != index or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 device tensor")
     n = len(parts)
-    pointers = ctypes.c_void_p * n
-    rc = load().mpt_kv_merge(n, lse.numel(), shape[-1], pointers(*[p.data_ptr() for p in parts]),
-                             pointers(*[l.data_ptr() for l in lses]), kind, out.data_ptr(), _KIND.get(out.dtype, -1),
+    pack = _POINTERS[n]
+    rc = load().mpt_kv_merge(n, first_lse.numel(), shape[-1], pack(*[p.data_ptr() for p in parts]),
+                             pack(*[l.data_ptr() for l in lses]), kind, out.data_ptr(), _KIND.get(out.dtype, -1),
                              lse.data_ptr(), at)
     if rc:
         _check(rc, "mpt_kv_merge")
