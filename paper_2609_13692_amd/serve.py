@@ -105,25 +105,29 @@ class LayoutServer:
     def decode(self, q, shared_depth=1):
         """Attention of one query per request (q [requests, heads, dim], not
         appended) over its prompt, the trie's nodes at shared_depth read once
-        for all requests below them."""
+        for all requests below them (0: every request reads its whole prompt)."""
         t, requests = self.trie, len(self.trie.leaf)
-        first = t.leaf.copy()
+        first = t.leaf.copy()                  # the node whose tokens are read once, -1: none
         while (deep := (first >= 0) & (t.depth[np.maximum(first, 0)] > shared_depth)).any():
             first[deep] = t.parent[first[deep]]
-        order = np.argsort(first, kind="stable")
-        order = order[first[order] >= 0]       # requests without chunks see nothing
-        groups, counts = np.unique(first[order], return_counts=True)
+        # requests by that node, those without one last; requests without chunks see nothing
+        order = np.argsort(np.where(first < 0, len(t.parent), first), kind="stable")
+        order = order[t.leaf[order] >= 0]
+        shared = int((first[order] >= 0).sum())
+        groups, counts = np.unique(first[order[:shared]], return_counts=True)
         pick = torch.as_tensor(order, device=self.device)
         sorted_q = q[pick].contiguous()
         each = np.arange(len(order) + 1)
-        parts = [self.cache.attend(0, sorted_q, self._ints(np.concatenate([[0], np.cumsum(counts)])), self._ints(groups),
-                                   causal=False, out_dtype=torch.float32),
-                 self.cache.attend(0, sorted_q, self._ints(each), self._ints(t.leaf[order]), causal=False,
-                                   kv_begin=self._ints(t.length[first[order]]), out_dtype=torch.float32)]
-        out, lse = kv.merge([p[0] for p in parts], [p[1] for p in parts], out_dtype=q.dtype)
+        begin = np.where(first[order] < 0, 0, t.length[first[order]])
+        out, lse = self.cache.attend(0, sorted_q, self._ints(each), self._ints(t.leaf[order]), causal=False,
+                                     kv_begin=self._ints(begin), out_dtype=torch.float32)
         whole = torch.zeros((requests, self.heads, q.shape[2]), dtype=q.dtype, device=self.device)
         whole_lse = torch.full((requests, self.heads), -float("inf"), device=self.device)
-        whole[pick], whole_lse[pick] = out, lse
+        if shared:
+            prefix, prefix_lse = self.cache.attend(0, sorted_q[:shared], self._ints(np.concatenate([[0], np.cumsum(counts)])),
+                                                   self._ints(groups), causal=False, out_dtype=torch.float32)
+            kv.merge([prefix, out[:shared]], [prefix_lse, lse[:shared]], out=out[:shared], lse=lse[:shared])
+        whole[pick], whole_lse[pick] = out.to(q.dtype), lse
         return whole, whole_lse
 
 

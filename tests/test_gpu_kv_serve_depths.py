@@ -1,0 +1,44 @@
+"""Decode steps of a served layout at every depth of sharing, whatever depth
+the prefill kept: attention over each request's whole prompt, in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from kv_reference import attention, attention_bounds, close
+from paper_2609_13692_amd import serve
+from paper_2609_13692_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+HEADS, KV_HEADS, DIM = 4, 2, 64
+# requests that are prefixes of others, alone in their first chunk, equal and empty
+INST = wl.from_sets([[0, 1, 2], [0, 1, 3], [0, 4], [0], [], [5, 1], [5, 2, 3], [0, 1, 2], [6]], [19, 3, 40, 16, 1, 33, 7],
+                    name="prefixes")
+
+
+def served():
+    project = serve.random_projection(INST, HEADS, KV_HEADS, DIM, torch.bfloat16, 2)
+    trie = serve.trie_of(INST.req_off, INST.req_chunks, INST.weights)
+    return project, serve.LayoutServer(trie, project, HEADS, KV_HEADS, DIM)
+
+
+def check_decode(project, server, **how):
+    q = torch.randn((INST.m, HEADS, DIM), device="cuda").to(torch.bfloat16)
+    out, lse = server.decode(q, **how)
+    assert out.dtype == q.dtype and server.cache.take_status() == []
+    for i, (a, b) in enumerate(zip(INST.req_off[:-1], INST.req_off[1:])):
+        if a == b:
+            assert not out[i].any() and (lse[i] == -float("inf")).all()
+            continue
+        _, k, v = (torch.cat(x).double().cpu().numpy() for x in zip(*(project(int(c)) for c in INST.req_chunks[a:b])))
+        ref = attention(q[i:i + 1].double().cpu().numpy(), k, v, len(k) - 1, causal=False)
+        bo, bl = attention_bounds(*ref, len(k), DIM, torch.bfloat16, torch.bfloat16)
+        close(out[i:i + 1].double().cpu().numpy(), ref[0], bo, f"decode of request {i}")
+        close(lse[i:i + 1].double().cpu().numpy(), ref[1], bl, f"lse of request {i}")
+
+
+@pytest.mark.parametrize("keep_depth", [0, 1, 2])
+def test_decode_without_sharing(keep_depth):
+    project, server = served()
+    server.prefill(keep_depth=keep_depth)
+    check_decode(project, server, shared_depth=0)
