@@ -73,13 +73,15 @@ class LayoutServer:
         self.cache = kv.KvCache.create(1, max(1, pages), page_size, kv_heads, dim, max(1, len(tokens)),
                                        int(trie.length.max(initial=1)) + page_size, dtype, device)
         self.outputs = {}                      # attention outputs of each node's tokens
+        self.held = np.zeros(len(tokens), dtype=bool)   # nodes whose slots hold their prefix
 
     def _ints(self, x):
         return torch.as_tensor(np.asarray(x, dtype=np.int32), device=self.device)
 
     def prefill(self, keep_depth=0) -> int:
         """Computes every node, slot i for node i; returns the tokens
-        computed. Nodes up to keep_depth keep their slots."""
+        computed. Nodes up to keep_depth keep their slots, so that decode can
+        read them once for the requests below them."""
         t, computed = self.trie, 0
         ends = np.zeros(len(t.parent), dtype=bool)
         ends[t.leaf[t.leaf >= 0]] = True
@@ -92,24 +94,29 @@ class LayoutServer:
             off = np.concatenate([[0], np.cumsum(self.new_tokens[level])])
             self.cache.append(0, k, v, self._ints(off), self._ints(level))
             out, _ = self.cache.attend(0, q, self._ints(off), self._ints(level))
+            self.held[level] = True
             for i, a, b in zip(level, off, off[1:]):
                 self.outputs[int(i)] = out[a:b]
             computed += int(off[-1])
             done = np.flatnonzero((t.depth == d - 1) & ~ends & (t.depth > keep_depth))
             if len(done):
                 self.cache.free(self._ints(done))
+                self.held[done] = False
         live = self.cache.compact(check=True)
         self.live_pages = live
         return computed
 
     def decode(self, q, shared_depth=1):
         """Attention of one query per request (q [requests, heads, dim], not
-        appended) over its prompt, the trie's nodes at shared_depth read once
-        for all requests below them (0: every request reads its whole prompt)."""
+        appended) over its prompt. Nodes are read once for all requests below
+        them: of each request the deepest up to shared_depth whose slot prefill
+        kept (keep_depth); a request without one reads its whole prompt."""
         t, requests = self.trie, len(self.trie.leaf)
+        if not self.held[t.leaf[t.leaf >= 0]].all():
+            raise RuntimeError("prefill has not computed every prompt")
         first = t.leaf.copy()                  # the node whose tokens are read once, -1: none
-        while (deep := (first >= 0) & (t.depth[np.maximum(first, 0)] > shared_depth)).any():
-            first[deep] = t.parent[first[deep]]
+        while (up := (first >= 0) & ((t.depth[np.maximum(first, 0)] > shared_depth) | ~self.held[np.maximum(first, 0)])).any():
+            first[up] = t.parent[first[up]]
         # requests by that node, those without one last; requests without chunks see nothing
         order = np.argsort(np.where(first < 0, len(t.parent), first), kind="stable")
         order = order[t.leaf[order] >= 0]

@@ -42,3 +42,22 @@ def test_decode_without_sharing(keep_depth):
     project, server = served()
     server.prefill(keep_depth=keep_depth)
     check_decode(project, server, shared_depth=0)
+
+
+def test_decode_with_the_default_depths():
+    project, server = served()
+    server.prefill()
+    check_decode(project, server)
+
+
+@pytest.mark.parametrize("keep_depth,shared_depth", [(0, 1), (0, 2), (0, 9), (1, 1), (1, 2), (1, 9), (2, 1), (2, 2), (9, 9)])
+def test_decode_at_depths_kept_and_not(keep_depth, shared_depth):
+    project, server = served()
+    server.prefill(keep_depth=keep_depth)
+    check_decode(project, server, shared_depth=shared_depth)
+
+
+def test_decode_before_the_prompts_are_there_is_refused():
+    _, server = served()
+    with pytest.raises(RuntimeError):
+        server.decode(torch.zeros((INST.m, HEADS, DIM), dtype=torch.bfloat16, device="cuda"))
