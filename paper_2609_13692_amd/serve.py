@@ -115,7 +115,8 @@ class LayoutServer:
         if not self.held[t.leaf[t.leaf >= 0]].all():
             raise RuntimeError("prefill has not computed every prompt")
         first = t.leaf.copy()                  # the node whose tokens are read once, -1: none
-        while (up := (first >= 0) & ((t.depth[np.maximum(first, 0)] > shared_depth) | ~self.held[np.maximum(first, 0)])).any():
+        depth, held = np.append(t.depth, 0), np.append(self.held, True)     # the root's are the last
+        while (up := (first >= 0) & ((depth[first] > shared_depth) | ~held[first])).any():
             first[up] = t.parent[first[up]]
         # requests by that node, those without one last; requests without chunks see nothing
         order = np.argsort(np.where(first < 0, len(t.parent), first), kind="stable")
@@ -125,7 +126,7 @@ class LayoutServer:
         pick = torch.as_tensor(order, device=self.device)
         sorted_q = q[pick].contiguous()
         each = np.arange(len(order) + 1)
-        begin = np.where(first[order] < 0, 0, t.length[first[order]])
+        begin = np.append(t.length, 0)[first[order]]
         out, lse = self.cache.attend(0, sorted_q, self._ints(each), self._ints(t.leaf[order]), causal=False,
                                      kv_begin=self._ints(begin), out_dtype=torch.float32)
         whole = torch.zeros((requests, self.heads, q.shape[2]), dtype=q.dtype, device=self.device)

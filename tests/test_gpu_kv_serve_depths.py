@@ -61,3 +61,11 @@ def test_decode_before_the_prompts_are_there_is_refused():
     _, server = served()
     with pytest.raises(RuntimeError):
         server.decode(torch.zeros((INST.m, HEADS, DIM), dtype=torch.bfloat16, device="cuda"))
+
+
+def test_a_layout_without_chunks():
+    trie = serve.trie_of([0, 0, 0], [], [])
+    server = serve.LayoutServer(trie, None, HEADS, KV_HEADS, DIM)
+    assert server.prefill() == 0 and server.live_pages == 0
+    out, lse = server.decode(torch.ones((2, HEADS, DIM), dtype=torch.bfloat16, device="cuda"))
+    assert out.shape == (2, HEADS, DIM) and not out.any() and (lse == -float("inf")).all()
