@@ -36,11 +36,22 @@ def _list(t, n, name, index):
 
 
 def _on(stream, index):
-    """Address of a stream (None: GPU index's current one), and what new
+    """Address of a stream of GPU index (None: its current one), and what new
     tensors that its work uses are made under."""
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(index) or None, None
+    if stream.device_index != index:
+        raise ValueError(f"stream must be on GPU {index}, is on GPU {stream.device_index}")
     return stream.cuda_stream or None, torch.cuda.stream(stream)
+
+
+def _run(index, call, *args):
+    """The call with GPU index as the current one, where launches go: the
+    address of a default stream does not say whose it is."""
+    if torch._C._cuda_getDevice() == index:
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
 
 
 def _new(shape, dtype, device, under):
@@ -129,12 +140,13 @@ class KvCache:
         return c
 
     def reset(self, stream=None):
-        _check(self._lib.mpt_kv_reset(self._p, _on(stream, self._index)[0]), "mpt_kv_reset")
+        _check(_run(self._index, self._lib.mpt_kv_reset, self._p, _on(stream, self._index)[0]), "mpt_kv_reset")
 
     def take_status(self, stream=None) -> list[str]:
         """What calls have found wrong in device data since the last look."""
         bits = ctypes.c_uint32(0)
-        _check(self._lib.mpt_kv_status(self._p, ctypes.addressof(bits), _on(stream, self._index)[0]), "mpt_kv_status")
+        at = _on(stream, self._index)[0]
+        _check(_run(self._index, self._lib.mpt_kv_status, self._p, ctypes.addressof(bits), at), "mpt_kv_status")
         return [name for bit, name in STATUS_BITS.items() if bits.value & bit]
 
     def _on(self, stream):
@@ -153,8 +165,8 @@ class KvCache:
         if lists:
             n = lists[0].numel()
             args = [n] + [None if t is None else _list(t, n, name, self._index) for t in lists]
-        rc = getattr(self._lib, name)(self._p, *args, ctypes.addressof(out) if check else None, self._ws_at,
-                                      self._ws_bytes, self._on(stream)[0])
+        rc = _run(self._index, getattr(self._lib, name), self._p, *args, ctypes.addressof(out) if check else None,
+                  self._ws_at, self._ws_bytes, self._on(stream)[0])
         if rc:
             _check(rc, name)
         return out.value if check else None
@@ -197,9 +209,9 @@ class KvCache:
         n, tokens, index = seqs.numel(), k_new.shape[0], self._index
         if v_new.shape[0] != tokens:
             raise ValueError("k_new and v_new must have one row per token")
-        rc = self._lib.mpt_kv_append(self._p, layer, n, _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index),
-                                     tokens, *self._rows(k_new, self.n_heads, "k_new", self.dtype),
-                                     *self._rows(v_new, self.n_heads, "v_new", self.dtype), _on(stream, index)[0])
+        rc = _run(index, self._lib.mpt_kv_append, self._p, layer, n, _list(seqs, n, "seqs", index),
+                  _list(q_off, n + 1, "q_off", index), tokens, *self._rows(k_new, self.n_heads, "k_new", self.dtype),
+                  *self._rows(v_new, self.n_heads, "v_new", self.dtype), _on(stream, index)[0])
         if rc:
             _check(rc, "mpt_kv_append")
 
@@ -227,8 +239,9 @@ class KvCache:
         ws = self._at_ws.get(need)
         if ws is None:
             ws = self._at_ws[need] = _new(need, torch.uint8, self.device, under)
-        rc = self._lib.mpt_kv_attention(
-            self._p, layer, n, _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index), tokens, heads,
+        rc = _run(
+            index, self._lib.mpt_kv_attention, self._p, layer, n, _list(seqs, n, "seqs", index),
+            _list(q_off, n + 1, "q_off", index), tokens, heads,
             *self._rows(q, heads, "q", self.dtype), *self._rows(out, heads, "out", out.dtype), _KIND.get(out.dtype, -1),
             lse.data_ptr(), None if kv_begin is None else _list(kv_begin, n, "kv_begin", index), 1 if causal else 0,
             min(window, 1 << 30), softcap, self._scale if scale is None else scale, ws.data_ptr(), need, at)
@@ -265,9 +278,8 @@ def merge(parts, lses, out_dtype=None, out=None, lse=None, stream=None):
         raise ValueError("lse must be a contiguous float32 device tensor")
     n = len(parts)
     pack = _POINTERS[n]
-    rc = load().mpt_kv_merge(n, first_lse.numel(), shape[-1], pack(*[p.data_ptr() for p in parts]),
-                             pack(*[l.data_ptr() for l in lses]), kind, out.data_ptr(), _KIND.get(out.dtype, -1),
-                             lse.data_ptr(), at)
+    rc = _run(index, load().mpt_kv_merge, n, first_lse.numel(), shape[-1], pack(*[p.data_ptr() for p in parts]),
+              pack(*[l.data_ptr() for l in lses]), kind, out.data_ptr(), _KIND.get(out.dtype, -1), lse.data_ptr(), at)
     if rc:
         _check(rc, "mpt_kv_merge")
     return out, lse
