@@ -76,6 +76,8 @@ __device__ inline int pages_of(const mpt_kv_cache &c, int tokens) {
 
 __device__ inline bool slot_ok(const mpt_kv_cache &c, int s) { return s >= 0 && s < c.max_seqs; }
 __device__ inline bool page_ok(const mpt_kv_cache &c, int p) { return p >= 0 && p < c.n_pages; }
+// A page of the pool that a table can refer to: one with references.
+__device__ inline bool page_held(const mpt_kv_cache &c, int p) { return page_ok(c, p) && c.ref[p] > 0; }
 
 // Listed indexes outside [0, bound) and those that two entries list: by bits
 // in LDS where they fit, else by marks in memory (an index gets its entry's
@@ -138,7 +140,10 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
                     err |= MPT_KV_BAD_LENGTH;
                 else {
                     const int full = k / c.page_size;
-                    if (k % c.page_size) from = c.table[(int64_t)s * c.max_pages + full];
+                    if (k % c.page_size) {
+                        from = c.table[(int64_t)s * c.max_pages + full];
+                        if (!page_held(c, from)) err |= MPT_KV_BAD_PAGE;
+                    }
                     need = pages_of(c, want) - full;
                 }
                 if (now != 0) err |= MPT_KV_NOT_EMPTY;
@@ -155,7 +160,6 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
                     }
                 }
             }
-            if (from != -1 && !page_ok(c, from)) err |= MPT_KV_BAD_PAGE;
             p.from[i] = from;
         }
         int64_t sum;

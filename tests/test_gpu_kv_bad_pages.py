@@ -1,0 +1,51 @@
+"""Page ids in tables that are no pages of the pool, or pages without
+references: the page calls find them before they change anything, say so in
+the status, and to a caller that asks."""
+import pytest
+import torch
+
+from paper_2609_13692_amd import kv
+
+pytestmark = pytest.mark.gpu
+
+N_PAGES, PAGE = 90, 4
+
+
+def ints(x):
+    return torch.tensor(list(x), dtype=torch.int32, device="cuda")
+
+
+# tables short enough for checks inside the plan, and long ones
+@pytest.fixture(params=[80, 40000], ids=["short", "long"])
+def cache(request):
+    c = kv.KvCache.create(2, N_PAGES, PAGE, 2, 16, 6, request.param)
+    c.k.normal_()
+    c.v.normal_()
+    c.fork(ints([-1, -1, -1]), ints([0, 2, 5]), ints([0, 0, 0]), ints([70, 19, 30]), check=True)
+    c.fork(ints([0]), ints([1]), ints([30]), ints([41]), check=True)
+    c.free(ints([5]), check=True)
+    return c
+
+
+# no page, the first past the pool, far past it, and a page that is free
+BAD = [-1, N_PAGES, 1 << 30, -(1 << 31), N_PAGES - 1]
+
+
+def refused(c, call, *args):
+    state = (c.k, c.v, c.table, c.length, c.ref, c.free_bits)
+    before = [x.clone() for x in state]
+    assert c.take_status() == []
+    with pytest.raises(kv.MptError) as e:
+        call(*args, check=True)
+    assert e.value.name == "MPT_E_RANGE"
+    assert c.take_status() == ["page"]
+    call(*args)                                    # unasked: the same, and no exception
+    assert c.take_status() == ["page"]
+    for x, y in zip(before, state):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bad", BAD)
+def test_fork_that_copies_from_a_bad_page(cache, bad):
+    cache.table[2, 4] = bad                        # tokens 16 .. 18
+    refused(cache, cache.fork, ints([0, 2]), ints([3, 4]), ints([8, 18]), ints([20, 18]))
