@@ -2,9 +2,11 @@
 // compaction), copies of their contents, appends, and the join of attention
 // over parts of a context.
 //
-// A page call is two launches: one workgroup checks the lists, sums up what
-// they need and picks the pages (k_kv_plan, k_kv_plan_free, k_kv_plan_moves),
-// and a wide launch applies it, or returns at once if the plan found an error.
+// A page call is two launches: one workgroup checks the lists and the pages
+// that they refer to, sums up what they need and picks the pages (k_kv_plan,
+// k_kv_plan_free, k_kv_plan_moves), and a wide launch applies it, or returns at
+// once if the plan found an error. The pages of long lists are checked by a
+// launch of their own before it.
 // Free pages are the set bits of one word per 64 pages, so a pool of 2^20
 // pages is picked from by reading 128 KiB.
 
@@ -105,12 +107,46 @@ __device__ inline uint32_t check_list(int n, const int32_t *list, int bound, int
     return err;
 }
 
+// Whether one of the pages first .. last - 1 of slot s cannot be referred to, a
+// lane each, four on their way at a time.
+__device__ inline bool bad_pages(const mpt_kv_cache &c, int s, int first, int last, int lane, int step) {
+    const int32_t *row = c.table + (int64_t)s * c.max_pages;
+    bool bad = false;
+    for (int j = first + lane; j < last; j += 4 * step) {
+        int page[4], ref[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) page[u] = row[j + u * step < last ? j + u * step : j];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) ref[u] = c.ref[page_ok(c, page[u]) ? page[u] : 0];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) bad |= !page_ok(c, page[u]) || ref[u] < 1;
+    }
+    return bad;
+}
+
+// Pages that a fork shares: keep / page_size of slot s, none if the two are refused.
+__device__ inline int shared_pages(const mpt_kv_cache &c, int s, int keep) {
+    if (!slot_ok(c, s) || keep < 0 || keep > c.length[s]) return 0;
+    return min(keep / c.page_size, c.max_pages);
+}
+
+// Lists and tables whose pages one workgroup checks beside its plan; past it a
+// launch before the plan does, a workgroup per entry.
+constexpr int64_t kSmallTables = 8192;
+
+__global__ __launch_bounds__(256) void k_kv_check_fork(mpt_kv_cache c, const int32_t *src, const int32_t *keep, Plan p) {
+    const int i = blockIdx.x, s = src[i];
+    const bool bad = bad_pages(c, s, 0, shared_pages(c, s, keep[i]), threadIdx.x, 256);
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) p.from[i] = any;
+}
+
 // Plan of forks (src != null) and growth: checks, pages needed and the
 // lowest-numbered free pages in ascending order, which leave free_bits here.
 // Each thread owns a run of words, so ranks are one sum over the workgroup.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, const int32_t *src, const int32_t *dst,
-                                                     const int32_t *keep, const int32_t *new_len, Plan p) {
+                                                     const int32_t *keep, const int32_t *new_len, bool checked, Plan p) {
     __shared__ int64_t lds[THREADS / 64];
     __shared__ uint32_t slots[kSlotBits / 32];
     __shared__ uint32_t err_all;
@@ -123,6 +159,10 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
     if (tid == 0) err_all = 0;
     __syncthreads();
     uint32_t err = check_list<THREADS>(n, dst, c.max_seqs, p.mark, slots, MPT_KV_BAD_SLOT);
+    // sixteen lanes an entry: the chains of reads of as many at a time
+    if (src && !checked)
+        for (int i = tid >> 4; i < n; i += THREADS / 16)
+            if (bad_pages(c, src[i], 0, shared_pages(c, src[i], keep[i]), tid & 15, 16)) err |= MPT_KV_BAD_PAGE;
     const int64_t most = (int64_t)c.max_pages * c.page_size;
     int64_t need_all = 0;
     for (int base = 0; base < n; base += THREADS) {
@@ -134,6 +174,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
             if (src) {
                 const int s = src[i];
                 k = keep[i];
+                if (checked && p.from[i]) err |= MPT_KV_BAD_PAGE;
                 if (s < -1 || s >= c.max_seqs)
                     err |= MPT_KV_BAD_SLOT;
                 else if (k < 0 || k > (s < 0 ? 0 : c.length[s]) || want < k || want > most)
@@ -275,10 +316,7 @@ __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t 
         for (int j = tid; j < full; j += blockDim.x) {
             const int page = other[j];
             row[j] = page;
-            if (page_ok(c, page))
-                atomicAdd(&c.ref[page], 1);
-            else
-                flag(c, MPT_KV_BAD_PAGE);
+            atomicAdd(&c.ref[page], 1);
         }
     }
     for (int j = have + tid; j < total; j += blockDim.x) {
@@ -665,12 +703,17 @@ static int grow(const mpt_kv_cache *c, int n, const int32_t *src, const int32_t 
                 const int32_t *new_len, int64_t *free_pages, void *ws, size_t bytes, hipStream_t s, const char *what) {
     if (int rc = check_plan(c, n, c ? c->max_seqs : 0, ws, bytes)) return rc;
     const Plan p = plan_at(*c, ws);
+    const bool checked = src && (int64_t)n * c->max_pages > kSmallTables;
+    if (checked) {
+        mptlib::LaunchScope scope("k_kv_check_fork", n, s);
+        k_kv_check_fork<<<n, 256, 0, s>>>(*c, src, keep, p);
+    }
     {
         mptlib::LaunchScope scope("k_kv_plan", n, s);
         if (plan_threads(n, c->n_pages) == 256)
-            k_kv_plan<256><<<1, 256, 0, s>>>(*c, n, src, dst, keep, new_len, p);
+            k_kv_plan<256><<<1, 256, 0, s>>>(*c, n, src, dst, keep, new_len, checked, p);
         else
-            k_kv_plan<1024><<<1, 1024, 0, s>>>(*c, n, src, dst, keep, new_len, p);
+            k_kv_plan<1024><<<1, 1024, 0, s>>>(*c, n, src, dst, keep, new_len, checked, p);
     }
     if (n) {
         mptlib::LaunchScope scope("k_kv_apply", n, s);

@@ -49,3 +49,13 @@ def refused(c, call, *args):
 def test_fork_that_copies_from_a_bad_page(cache, bad):
     cache.table[2, 4] = bad                        # tokens 16 .. 18
     refused(cache, cache.fork, ints([0, 2]), ints([3, 4]), ints([8, 18]), ints([20, 18]))
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("at", [0, 3])
+def test_fork_that_shares_a_bad_page(cache, at, bad):
+    cache.table[2, at] = bad
+    refused(cache, cache.fork, ints([0, 2]), ints([3, 4]), ints([8, 16]), ints([20, 18]))
+    # pages past those that are kept do not matter
+    cache.fork(ints([2]), ints([3]), ints([4 * at]), ints([4 * at + 1]), check=True)
+    assert cache.take_status() == []
