@@ -195,7 +195,9 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(mpt_kv_cache c, int n, cons
                 // a last page with room that others refer to is copied first
                 if (want > now && now % c.page_size && slot_ok(c, d)) {
                     const int page = c.table[(int64_t)d * c.max_pages + now / c.page_size];
-                    if (page_ok(c, page) && c.ref[page] > 1) {
+                    if (!page_held(c, page)) {
+                        err |= MPT_KV_BAD_PAGE;
+                    } else if (c.ref[page] > 1) {
                         from = page;
                         ++need;
                     }

@@ -59,3 +59,11 @@ def test_fork_that_shares_a_bad_page(cache, at, bad):
     # pages past those that are kept do not matter
     cache.fork(ints([2]), ints([3]), ints([4 * at]), ints([4 * at + 1]), check=True)
     assert cache.take_status() == []
+
+
+@pytest.mark.parametrize("bad", BAD)
+def test_growth_of_a_bad_page(cache, bad):
+    cache.table[2, 4] = bad
+    refused(cache, cache.extend, ints([0, 2]), ints([78, 20]))
+    cache.extend(ints([0, 2]), ints([78, 19]), check=True)     # as long as it was: nothing is read
+    assert cache.take_status() == []
