@@ -130,14 +130,22 @@ __device__ inline int shared_pages(const mpt_kv_cache &c, int s, int keep) {
     return min(keep / c.page_size, c.max_pages);
 }
 
+// Pages of slot s that a cut to k tokens drops end there (0: the two are refused).
+__device__ inline int dropped_end(const mpt_kv_cache &c, int s, int k) {
+    const int now = slot_ok(c, s) ? c.length[s] : 0;
+    return k < 0 || k > now || now > (int64_t)c.max_pages * c.page_size ? 0 : pages_of(c, now);
+}
+
 // Lists and tables whose pages one workgroup checks beside its plan; past it a
 // launch before the plan does, a workgroup per entry.
 constexpr int64_t kSmallTables = 8192;
 
-__global__ __launch_bounds__(256) void k_kv_check_fork(mpt_kv_cache c, const int32_t *src, const int32_t *keep, Plan p) {
-    const int i = blockIdx.x, s = src[i];
-    const bool bad = bad_pages(c, s, 0, shared_pages(c, s, keep[i]), threadIdx.x, 256);
-    const int any = __syncthreads_or(bad);
+// The pages that forks of list[i] share, or that cuts of it drop.
+template <bool DROP>
+__global__ __launch_bounds__(256) void k_kv_check(mpt_kv_cache c, const int32_t *list, const int32_t *keep, Plan p) {
+    const int i = blockIdx.x, s = list[i], k = keep ? keep[i] : 0;
+    const int first = DROP ? pages_of(c, k) : 0, last = DROP ? dropped_end(c, s, k) : shared_pages(c, s, k);
+    const int any = __syncthreads_or(bad_pages(c, s, first, last, threadIdx.x, 256));
     if (threadIdx.x == 0) p.from[i] = any;
 }
 
@@ -285,10 +293,15 @@ __device__ inline void copy_rows(char *base, const int64_t *stride, int64_t laye
     }
 }
 
+// A reference less. A page that counts fewer than the tables have, which no
+// look at one entry shows, stays at none.
 __device__ inline void drop(const mpt_kv_cache &c, int page) {
     const int old = atomicSub(&c.ref[page], 1);
     if (old == 1) atomicOr((unsigned long long *)&c.free_bits[page >> 6], 1ull << (page & 63));
-    if (old <= 0) flag(c, MPT_KV_BAD_PAGE);
+    if (old <= 0) {
+        atomicAdd(&c.ref[page], 1);
+        flag(c, MPT_KV_BAD_PAGE);
+    }
 }
 
 // Forks and growth as planned: workgroup (i, 0) writes entry i's row of the
@@ -333,7 +346,8 @@ __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t 
 }
 
 template <int THREADS>
-__device__ inline uint32_t check_free(const mpt_kv_cache &c, int n, const int32_t *seqs, const int32_t *keep, const Plan &p) {
+__device__ inline uint32_t check_free(const mpt_kv_cache &c, int n, const int32_t *seqs, const int32_t *keep, bool checked,
+                                      const Plan &p) {
     __shared__ uint32_t err_all, slots[kSlotBits / 32];
     if (threadIdx.x == 0) err_all = 0;
     uint32_t err = check_list<THREADS>(n, seqs, c.max_seqs, p.mark, slots, MPT_KV_BAD_SLOT);
@@ -341,7 +355,13 @@ __device__ inline uint32_t check_free(const mpt_kv_cache &c, int n, const int32_
     for (int i = threadIdx.x; i < n; i += THREADS) {
         const int s = seqs[i], now = slot_ok(c, s) ? c.length[s] : 0, k = keep ? keep[i] : 0;
         if (k < 0 || k > now || now > most) err |= MPT_KV_BAD_LENGTH;
+        if (checked && p.from[i]) err |= MPT_KV_BAD_PAGE;
     }
+    if (!checked)
+        for (int i = threadIdx.x >> 4; i < n; i += THREADS / 16) {
+            const int s = seqs[i], k = keep ? keep[i] : 0;
+            if (bad_pages(c, s, pages_of(c, k), dropped_end(c, s, k), threadIdx.x & 15, 16)) err |= MPT_KV_BAD_PAGE;
+        }
     if (err) atomicOr(&err_all, err);
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -354,17 +374,11 @@ __device__ inline uint32_t check_free(const mpt_kv_cache &c, int n, const int32_
 // Pages of slot s past its first k tokens, a lane each.
 __device__ inline void drop_pages(const mpt_kv_cache &c, int s, int k, int now, int first, int step) {
     const int32_t *row = c.table + (int64_t)s * c.max_pages;
-    for (int j = pages_of(c, k) + first; j < pages_of(c, now); j += step) {
-        const int page = row[j];
-        if (page_ok(c, page))
-            drop(c, page);
-        else
-            flag(c, MPT_KV_BAD_PAGE);
-    }
+    for (int j = pages_of(c, k) + first; j < pages_of(c, now); j += step) drop(c, row[j]);
 }
 
 __global__ __launch_bounds__(1024) void k_kv_plan_free(mpt_kv_cache c, int n, const int32_t *seqs, const int32_t *keep, Plan p) {
-    check_free<1024>(c, n, seqs, keep, p);
+    check_free<1024>(c, n, seqs, keep, true, p);
 }
 
 __global__ __launch_bounds__(256) void k_kv_free(mpt_kv_cache c, const int32_t *seqs, const int32_t *keep, Plan p) {
@@ -377,9 +391,8 @@ __global__ __launch_bounds__(256) void k_kv_free(mpt_kv_cache c, const int32_t *
 
 // Checks and drops of short lists with short tables in one launch: a wave per
 // sequence.
-constexpr int kSmallFree = 8192;
 __global__ __launch_bounds__(1024) void k_kv_free_small(mpt_kv_cache c, int n, const int32_t *seqs, const int32_t *keep, Plan p) {
-    if (check_free<1024>(c, n, seqs, keep, p)) return;
+    if (check_free<1024>(c, n, seqs, keep, false, p)) return;
     const int lane = threadIdx.x & 63;
     for (int i = threadIdx.x >> 6; i < n; i += 16) {
         const int s = seqs[i], k = keep ? keep[i] : 0, now = c.length[s];
@@ -707,8 +720,8 @@ static int grow(const mpt_kv_cache *c, int n, const int32_t *src, const int32_t 
     const Plan p = plan_at(*c, ws);
     const bool checked = src && (int64_t)n * c->max_pages > kSmallTables;
     if (checked) {
-        mptlib::LaunchScope scope("k_kv_check_fork", n, s);
-        k_kv_check_fork<<<n, 256, 0, s>>>(*c, src, keep, p);
+        mptlib::LaunchScope scope("k_kv_check", n, s);
+        k_kv_check<false><<<n, 256, 0, s>>>(*c, src, keep, p);
     }
     {
         mptlib::LaunchScope scope("k_kv_plan", n, s);
@@ -795,10 +808,14 @@ extern "C" int mpt_kv_free(const mpt_kv_cache *cache, int n, const int32_t *seqs
         if (int rc = check_plan(cache, n, cache ? cache->max_seqs : 0, workspace, workspace_bytes)) return rc;
         hipStream_t s = (hipStream_t)stream;
         const Plan p = plan_at(*cache, workspace);
-        if ((int64_t)n * cache->max_pages <= kSmallFree) {
+        if ((int64_t)n * cache->max_pages <= kSmallTables) {
             mptlib::LaunchScope scope("k_kv_free_small", n, s);
             k_kv_free_small<<<1, 1024, 0, s>>>(*cache, n, seqs, keep, p);
         } else {
+            {
+                mptlib::LaunchScope scope("k_kv_check", n, s);
+                k_kv_check<true><<<n, 256, 0, s>>>(*cache, seqs, keep, p);
+            }
             {
                 mptlib::LaunchScope scope("k_kv_plan_free", n, s);
                 k_kv_plan_free<<<1, 1024, 0, s>>>(*cache, n, seqs, keep, p);

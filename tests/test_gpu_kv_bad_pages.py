@@ -67,3 +67,23 @@ def test_growth_of_a_bad_page(cache, bad):
     refused(cache, cache.extend, ints([0, 2]), ints([78, 20]))
     cache.extend(ints([0, 2]), ints([78, 19]), check=True)     # as long as it was: nothing is read
     assert cache.take_status() == []
+
+
+@pytest.mark.parametrize("bad", BAD)
+def test_free_of_a_bad_page(cache, bad):
+    cache.table[2, 2] = bad
+    refused(cache, cache.free, ints([0, 2]))
+    refused(cache, cache.free, ints([0, 2]), ints([30, 8]))
+    cache.free(ints([0, 2]), ints([30, 9]), check=True)        # the bad one is kept
+    assert cache.take_status() == []
+
+
+def test_a_page_loses_no_reference_that_it_does_not_have(cache):
+    """Two tables list a page that counts one reference."""
+    cache.table[2, 0] = cache.table[0, 17]
+    cache.free(ints([0, 2]))
+    assert cache.take_status() == ["page"]
+    ref = cache.ref.tolist()
+    assert min(ref) == 0
+    free = [(int(cache.free_bits[p // 64]) >> p % 64) & 1 for p in range(N_PAGES)]
+    assert free == [int(r == 0) for r in ref]
