@@ -490,7 +490,11 @@ int mpt_pinned_assemble(int m, int64_t nnz, const int64_t *req_off, const int32_
  * (MPT_E_RANGE, MPT_E_DUP, MPT_E_STATE or MPT_E_PAGES). Without it, and in
  * mpt_kv_append, mpt_kv_attention and mpt_kv_merge, nothing synchronises, and
  * the calls can be captured into a graph. Page ids outside [0, n_pages) and
- * slots outside [0, max_seqs) are never followed.
+ * slots outside [0, max_seqs) are never followed. The page calls look at every
+ * page that they share, copy from, drop or (compaction) move, not at those
+ * that stay as they are. Counts in ref that are lower than the tables' show
+ * only when a page would lose a reference that it does not count: it then keeps
+ * none, MPT_KV_BAD_PAGE is set and the call goes through.
  * Calls on one cache must be ordered by the caller (one stream, or events).
  */
 #define MPT_KV_BF16 0

@@ -410,10 +410,28 @@ __global__ __launch_bounds__(1024) void k_kv_count(mpt_kv_cache c, Plan p) {
     if (threadIdx.x == 0) p.head->value = all;
 }
 
+// The pages of all tables, a wave per slot.
+__global__ __launch_bounds__(256) void k_kv_check_tables(mpt_kv_cache c, Plan p) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t s = blockIdx.x * 4 + (threadIdx.x >> 6); s < c.max_seqs; s += gridDim.x * 4) {
+        const int any = __any(bad_pages(c, (int)s, 0, min(pages_of(c, c.length[s]), c.max_pages), lane, 64));
+        if (lane == 0) p.from[s] = any;
+    }
+}
+
 // Plan of a compaction: the j-th used page from n_live on goes to the j-th
 // free page below. a[j] and b[j] are the two; the words are rewritten here.
 __global__ __launch_bounds__(1024) void k_kv_plan_moves(mpt_kv_cache c, Plan p) {
     __shared__ int64_t lds[16];
+    bool bad = false;
+    for (int64_t s = threadIdx.x; s < c.max_seqs; s += 1024) bad |= p.from[s] != 0;
+    if (__syncthreads_or(bad)) {
+        if (threadIdx.x == 0) {
+            p.head->err = MPT_KV_BAD_PAGE;
+            flag(c, MPT_KV_BAD_PAGE);
+        }
+        return;
+    }
     const int tid = threadIdx.x, words = (c.n_pages + 63) / 64, per = (words + 1024 - 1) / 1024;
     const int w0 = tid * per < words ? tid * per : words, w1 = w0 + per < words ? w0 + per : words;
     int64_t mine = 0, free_all;
@@ -472,7 +490,7 @@ __global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Plan p, int tab
         const int pages = min(pages_of(c, c.length[s]), c.max_pages);
         for (int j = threadIdx.x; j < pages; j += 256) {
             const int page = row[j];
-            if (page < live || page >= c.n_pages) continue;
+            if (page < live) continue;
             int lo = 0, hi = moves;
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
@@ -838,6 +856,10 @@ extern "C" int mpt_kv_compact(const mpt_kv_cache *cache, int64_t *live_pages, vo
         if (int rc = check_plan(cache, 0, 0, workspace, workspace_bytes)) return rc;
         hipStream_t s = (hipStream_t)stream;
         const Plan p = plan_at(*cache, workspace);
+        {
+            mptlib::LaunchScope scope("k_kv_check_tables", cache->max_seqs, s);
+            k_kv_check_tables<<<mptlib::grid_for(cache->max_seqs, 4, 2048), 256, 0, s>>>(*cache, p);
+        }
         {
             mptlib::LaunchScope scope("k_kv_plan_moves", cache->n_pages, s);
             k_kv_plan_moves<<<1, 1024, 0, s>>>(*cache, p);

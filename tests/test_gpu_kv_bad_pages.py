@@ -87,3 +87,13 @@ def test_a_page_loses_no_reference_that_it_does_not_have(cache):
     assert min(ref) == 0
     free = [(int(cache.free_bits[p // 64]) >> p % 64) & 1 for p in range(N_PAGES)]
     assert free == [int(r == 0) for r in ref]
+
+
+@pytest.mark.parametrize("bad", BAD + [1])
+def test_compaction_of_a_bad_page(cache, bad):
+    cache.free(ints([0]), ints([41]), check=True)
+    cache.free(ints([1]), check=True)
+    if bad == 1:                                   # a hole below the pages in use
+        cache.free(ints([0]), ints([0]), check=True)
+    cache.table[2, 2] = bad
+    refused(cache, cache.compact)
