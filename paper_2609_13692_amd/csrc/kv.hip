@@ -582,8 +582,9 @@ __global__ __launch_bounds__(256) void k_kv_append(mpt_kv_cache c, int layer, in
                                                    int64_t kh, const char *v_new, int64_t vt, int64_t vh) {
     const int lane = threadIdx.x & 63, units = c.head_dim / 8, total = c.n_heads * units;
     const int shift = 31 - __clz(c.page_size);
-    for (int token = blockIdx.x * 4 + (threadIdx.x >> 6); token < n_tokens; token += gridDim.x * 4) {
-        const int i = wave_find(q_off, n, token);
+    // in 64 bits: the next number past n_tokens, which may be 2^31 - 1
+    for (int64_t token = blockIdx.x * 4 + (threadIdx.x >> 6); token < n_tokens; token += gridDim.x * 4) {
+        const int i = wave_find(q_off, n, (int)token);
         if (i < 0 || i >= n || !slot_ok(c, seqs[i])) {
             if (lane == 0) flag(c, MPT_KV_BAD_SLOT);
             continue;

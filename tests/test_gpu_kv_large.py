@@ -1,0 +1,39 @@
+"""The largest numbers that the paged cache's calls take."""
+import pytest
+import torch
+
+from paper_2609_13692_amd import kv
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(list(x), dtype=torch.int32, device="cuda")
+
+
+@pytest.fixture
+def room():
+    """60 to 80 GB for one test, given back afterwards."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("less than 100 GB of device memory are free")
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_append_of_as_many_tokens_as_it_takes(room):
+    """2^31 - 1 tokens, the most of a call, of two sequences of 2^30 and 2^30 - 1."""
+    lengths, page = [1 << 30, (1 << 30) - 1], 1024
+    c = kv.KvCache.create(1, 1 << 21, page, 1, 8, 2, 1 << 30, torch.float16)
+    c.fork(ints([-1, -1]), ints([0, 1]), ints([0, 0]), ints(lengths), check=True)
+    k, v = (torch.randn((1, 1, 8), device="cuda").half() for _ in range(2))
+    total = sum(lengths)
+    c.append(0, k.expand(total, 1, 8), v.expand(total, 1, 8), ints([0, lengths[0], total]), ints([0, 1]))
+    assert c.take_status() == []
+    for x, row in ((c.k, k), (c.v, v)):
+        for first in range(0, 1 << 21, 1 << 17):
+            same = (x[0, first:first + (1 << 17)] == row[0]).all(-1)
+            if first + (1 << 17) == 1 << 21:
+                assert not same[-1, -1] and not x[0, -1, -1].any()
+                same[-1, -1] = True
+            assert same.all()
