@@ -504,6 +504,7 @@ int mpt_pinned_assemble(int m, int64_t nnz, const int64_t *req_off, const int32_
 #define MPT_KV_MAX_PAGE_SIZE 1024
 #define MPT_KV_MAX_PAGES (1 << 26)
 #define MPT_KV_MAX_PARTS 16
+#define MPT_KV_MAX_LIST ((1 << 24) - 1)   /* entries of a list of sequences in a page call */
 
 #define MPT_KV_BAD_SLOT 1u        /* a slot outside [0, max_seqs), or offsets that are no CSR */
 #define MPT_KV_BAD_LENGTH 2u      /* a length outside its range */
@@ -551,7 +552,7 @@ size_t mpt_kv_workspace_bytes(const mpt_kv_cache *cache);
  *   src, dst, keep, new_len [n]  device; dst distinct and empty; 0 <= keep[i]
  *                                <= length[src[i]], keep[i] <= new_len[i]
  *   free_pages                   HOST out, nullable: free pages afterwards
- * All or nothing.
+ * n <= MPT_KV_MAX_LIST, here and in the two calls below. All or nothing.
  */
 int mpt_kv_fork(const mpt_kv_cache *cache, int n, const int32_t *src, const int32_t *dst,
                 const int32_t *keep, const int32_t *new_len, int64_t *free_pages,

@@ -708,6 +708,12 @@ int check_cache(const mpt_kv_cache *c) {
     return MPT_OK;
 }
 
+// Entries that a list of sequences can have: distinct slots, a workgroup each of
+// a launch of less than 2^32 threads (a plan must not take pages that the
+// launch after it cannot hand out).
+static int list_limit(const mpt_kv_cache *c) { return !c ? 0 : c->max_seqs < MPT_KV_MAX_LIST ? c->max_seqs : MPT_KV_MAX_LIST; }
+static_assert(MPT_KV_MAX_LIST * 256ull < 1ull << 32, "k_kv_apply and k_kv_free take 256 threads an entry");
+
 static int check_plan(const mpt_kv_cache *c, int n, int most, void *ws, size_t bytes) {
     if (int rc = check_cache(c)) return rc;
     if (n < 0 || n > most) return fail(MPT_E_INVALID, "n = %d outside [0, %d]", n, most);
@@ -735,7 +741,7 @@ static int report(const Plan &p, int64_t *value, const char *what, hipStream_t s
 
 static int grow(const mpt_kv_cache *c, int n, const int32_t *src, const int32_t *dst, const int32_t *keep,
                 const int32_t *new_len, int64_t *free_pages, void *ws, size_t bytes, hipStream_t s, const char *what) {
-    if (int rc = check_plan(c, n, c ? c->max_seqs : 0, ws, bytes)) return rc;
+    if (int rc = check_plan(c, n, list_limit(c), ws, bytes)) return rc;
     const Plan p = plan_at(*c, ws);
     const bool checked = src && (int64_t)n * c->max_pages > kSmallTables;
     if (checked) {
@@ -824,7 +830,7 @@ extern "C" int mpt_kv_free(const mpt_kv_cache *cache, int n, const int32_t *seqs
     mptlib::clear_error();
     return mptlib::guarded(__func__, [&]() -> int {
         if (n > 0 && !seqs) return fail(MPT_E_INVALID, "seqs is NULL");
-        if (int rc = check_plan(cache, n, cache ? cache->max_seqs : 0, workspace, workspace_bytes)) return rc;
+        if (int rc = check_plan(cache, n, list_limit(cache), workspace, workspace_bytes)) return rc;
         hipStream_t s = (hipStream_t)stream;
         const Plan p = plan_at(*cache, workspace);
         if ((int64_t)n * cache->max_pages <= kSmallTables) {

@@ -37,3 +37,17 @@ def test_append_of_as_many_tokens_as_it_takes(room):
                 assert not same[-1, -1] and not x[0, -1, -1].any()
                 same[-1, -1] = True
             assert same.all()
+
+
+def test_lists_of_as_many_sequences_as_they_take():
+    """2^24 - 1 sequences forked, grown and freed in one call each."""
+    n, pages = (1 << 24) - 1, (1 << 25) + 5
+    c = kv.KvCache.create(1, pages, 1, 1, 8, n + 3, 2, torch.float16)
+    dst = torch.randperm(n + 3, device="cuda", dtype=torch.int32)[:n].contiguous()
+    none, one = torch.full((n,), -1, dtype=torch.int32, device="cuda"), torch.ones(n, dtype=torch.int32, device="cuda")
+    assert c.fork(none, dst, torch.zeros_like(one), one, check=True) == pages - n
+    assert torch.equal(c.table[dst.long(), 0], torch.arange(n, device="cuda", dtype=torch.int32))
+    assert c.extend(dst, 2 * one, check=True) == pages - 2 * n
+    assert torch.equal(c.table[dst.long(), 1], n + torch.arange(n, device="cuda", dtype=torch.int32))
+    assert c.free(dst, one, check=True) == pages - n
+    assert torch.equal(c.ref, (torch.arange(pages, device="cuda") < n).int()) and c.take_status() == []
