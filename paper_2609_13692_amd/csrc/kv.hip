@@ -485,8 +485,9 @@ __global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Plan p, int tab
     }
     if (!tables) return;
     const int live = (int)p.head->value;
-    for (int s = blockIdx.x; s < c.max_seqs; s += gridDim.x) {
-        int32_t *row = c.table + (int64_t)s * c.max_pages;
+    // in 64 bits: the next number past max_seqs, which may be 2^31 - 1
+    for (int64_t s = blockIdx.x; s < c.max_seqs; s += gridDim.x) {
+        int32_t *row = c.table + s * c.max_pages;
         const int pages = min(pages_of(c, c.length[s]), c.max_pages);
         for (int j = threadIdx.x; j < pages; j += 256) {
             const int page = row[j];

@@ -51,3 +51,16 @@ def test_lists_of_as_many_sequences_as_they_take():
     assert torch.equal(c.table[dst.long(), 1], n + torch.arange(n, device="cuda", dtype=torch.int32))
     assert c.free(dst, one, check=True) == pages - n
     assert torch.equal(c.ref, (torch.arange(pages, device="cuda") < n).int()) and c.take_status() == []
+
+
+def test_compaction_of_as_many_slots_as_there_can_be(room):
+    slots = (1 << 31) - 1
+    c = kv.KvCache.create(1, 200, 1, 1, 8, slots, 1, torch.float16)
+    c.k.normal_()
+    used = [0, 7, 1 << 30, slots - 2, slots - 1]
+    c.fork(ints([-1] * 105), ints(list(range(100, 200)) + used), ints([0] * 105), ints([1] * 105), check=True)
+    k = c.k.clone()
+    c.free(ints(range(100, 200)), check=True)
+    assert c.compact(check=True) == 5
+    assert [int(c.table[s, 0]) for s in used] == [0, 1, 2, 3, 4] and c.ref.tolist() == [1] * 5 + [0] * 195
+    assert torch.equal(c.k[:, :5], k[:, 100:105]) and c.take_status() == []
