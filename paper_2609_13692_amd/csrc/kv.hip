@@ -657,7 +657,7 @@ __device__ inline void store8(void *p, int64_t at, const float *x) {
 template <int TI, int TO>
 __global__ __launch_bounds__(256) void k_kv_merge(int n_parts, int64_t rows, int dim, Parts p, void *out, float *lse) {
     const int units = dim / 8, per = 256 / units, r = threadIdx.x / units, u = threadIdx.x - r * units;
-    const int64_t row = (int64_t)blockIdx.x * per + r, at = row * dim + u * 8;
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * per + r, at = row * dim + u * 8;
     const bool there = r < per && row < rows;
     float top = -INFINITY, sum = 0, acc[8] = {}, total = 0;
     if (there) {
@@ -955,11 +955,14 @@ extern "C" int mpt_kv_merge(int n_parts, int64_t rows, int dim, const void *cons
             {k_kv_merge<2, 0>, k_kv_merge<2, 1>, k_kv_merge<2, 2>}};
         hipStream_t s = (hipStream_t)stream;
         const int per = 256 / (dim / 8);
+        // a dimension of a launch holds less than 2^32 threads, and more are
+        // not refused: they are cut off
+        constexpr int64_t kAcross = 1 << 23;
         const int64_t blocks = (rows + per - 1) / per;
-        if (blocks > INT32_MAX) return fail(MPT_E_INVALID, "rows = %lld", (long long)rows);
+        const dim3 grid((unsigned)(blocks < kAcross ? blocks : kAcross), (unsigned)((blocks + kAcross - 1) / kAcross));
         {
             mptlib::LaunchScope scope("k_kv_merge", (double)rows, s);
-            kernels[part_dtype][out_dtype]<<<(unsigned)blocks, 256, 0, s>>>(n_parts, rows, dim, p, out, lse);
+            kernels[part_dtype][out_dtype]<<<grid, 256, 0, s>>>(n_parts, rows, dim, p, out, lse);
         }
         MPT_HIP_TRY(hipGetLastError());
         return MPT_OK;

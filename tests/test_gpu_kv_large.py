@@ -64,3 +64,18 @@ def test_compaction_of_as_many_slots_as_there_can_be(room):
     assert c.compact(check=True) == 5
     assert [int(c.table[s, 0]) for s in used] == [0, 1, 2, 3, 4] and c.ref.tolist() == [1] * 5 + [0] * 195
     assert torch.equal(c.k[:, :5], k[:, 100:105]) and c.take_status() == []
+
+
+def test_merge_of_more_rows_than_one_launch_dimension_holds(room):
+    """2^27 rows of 256 and some, in place: 2^32 threads and more."""
+    rows = (1 << 27) + 9
+    x = torch.empty((rows, 256), dtype=torch.bfloat16, device="cuda")
+    x.copy_((torch.arange(rows, device="cuda") % 251)[:, None])
+    lse = (torch.arange(rows, device="cuda") % 7).float()
+    lse[::3] = -float("inf")
+    want = lse.clone()
+    out, total = kv.merge([x], [lse], out=x, lse=lse)
+    assert out is x and torch.equal(total, want)
+    for first in range(0, rows, 1 << 23):
+        at = torch.arange(first, min(first + (1 << 23), rows), device="cuda")
+        assert (out[first:first + (1 << 23)] == torch.where(at % 3 == 0, 0, at % 251)[:, None]).all()
