@@ -323,21 +323,27 @@ __device__ inline V load(const char *from) {
 // in registers. The instruction is written out because the compiler takes any
 // later LDS read for one of its result and would wait for the loads of the
 // next tile there; who uses it waits (arrived) before the barrier that lets
-// the tile be read.
+// the tile be read. m0, which the address goes through, is named as written:
+// the compiler, which keeps no value there, may else take two settings of its
+// own for one where a statement stands between them. It warns that it would
+// not restore a register of that kind: nothing needs it restored.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void load_lds16(const char *from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory", "m0");
 }
 // The same with 4 bytes per lane.
 __device__ inline void load_lds4(const void *from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)lds)), "v"(from) : "memory", "m0");
 }
 // The same at 32-bit offsets from one address.
 __device__ inline void load_lds16(const void *base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(uniform((int)lds)), "v"(offset), "s"(uniform((int64_t)base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(uniform((int)lds)), "v"(offset), "s"(uniform((int64_t)base)) : "memory", "m0");
 }
 __device__ inline void load_lds4(const void *base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(uniform((int)lds)), "v"(offset), "s"(uniform((int64_t)base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(uniform((int)lds)), "v"(offset), "s"(uniform((int64_t)base)) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // Waits until at most N of the wave's later loads are on their way: loads
 // arrive in order, so all before those N have.
 template <int N>
