@@ -630,9 +630,12 @@ size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_
  *     lse = log sum exp(s_t),   out = sum exp(s_t - lse) v_t.
  * Rows that see no token (or only scores of minus infinity) get out = 0 and
  * lse = minus infinity. What lies in tokens that a row does not see, NaN and
- * infinities included, has no effect on it. Bad slots count as empty, tokens on
- * bad pages as zeros or as some tokens of the pool, and tokens of no entry get
- * no output. Decoding is a chunk of one token;
+ * infinities included, has no effect on it. An infinite value that a row does
+ * see makes its output infinite however small its weight (NaN beside a NaN or the
+ * other infinity). The sums are formed with weights of up to 2^8, in 32 bits:
+ * they overflow where weights times values pass 2^128. Bad slots count as empty,
+ * tokens on bad pages as zeros or as some tokens of the pool, and tokens of no
+ * entry get no output. Decoding is a chunk of one token;
  * a prefix that several sequences share is one slot with all of their queries
  * and causal = 0, joined with their own parts (kv_begin) by mpt_kv_merge.
  *   seqs [n]       device; a slot may be listed several times

@@ -412,6 +412,87 @@ __device__ inline uint32_t odd8(s16x8 x) {
     return (((u.x & kE) + kOne) | ((u.y & kE) + kOne) | ((u.z & kE) + kOne) | ((u.w & kE) + kOne)) & 0x80008000u;
 }
 
+// Not a zero if one of a lane's sums is an infinity or NaN.
+__device__ inline float not_finite(f32x4 x) {
+    return __builtin_fmaf(x[0], 0.0f, __builtin_fmaf(x[1], 0.0f, __builtin_fmaf(x[2], 0.0f, x[3] * 0.0f)));
+}
+
+// Infinities and NaN in values. A product cannot hold them: under the weight 0
+// of a row that does not see the token, or sees it with a weight that the type
+// rounds to 0, it is NaN. So where some rows do not see a step's tokens, the
+// step's product takes zeros in their place; and a tile that has met one, or
+// whose sums came out infinite or NaN, ends here: a wave looks through the
+// values of tokens t0 .. t1 - 1 once more, and every sum that an infinity or NaN
+// belongs to becomes the sum of those alone, which is what the definition
+// gives. A lane's row sees lo .. hi - 1; its sums, groups of four dimensions
+// from d0 on, `step` apart, lie at `to`, `inc` bytes apart, in 32 bits or T.
+// l: the row's sum of weights (NaN: so are its sums). Without any weight a whole
+// row is zeros; parts keep what they saw, and their join decides.
+template <class T>
+__device__ inline void odd_values(const Attn &a, const int32_t *table, int shift, const char *values, int t0, int t1, int lo,
+                                  int hi, float l, bool whole, int d0, int step, char *to, int inc, bool f32) {
+    const int lane = threadIdx.x & 63;
+    if (whole && l == 0)
+        for (int k = 0; d0 + k * step < 8 * a.units; ++k) {
+            if (f32)
+                *(f32x4 *)(to + k * inc) = f32x4{0, 0, 0, 0};
+            else
+                *(s16x4 *)(to + k * inc) = s16x4{0, 0, 0, 0};
+        }
+    const bool mine = l > 0 || (l == 0 && !whole);
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass)                    // to zeros, then the sums
+#pragma unroll 1
+        for (int base = t0; base < t1; base += 64) {
+            const int t = base + lane, page = t < t1 ? table[t >> shift] : -1;
+            const char *row = values + row_at(page, t & (a.c.page_size - 1), a.v_page, a.v_slot);
+            uint32_t odd = 0;
+            if ((unsigned)page < (unsigned)a.c.n_pages)
+                for (int u = 0; u < a.units; ++u) odd |= odd8<T>(load<s16x8>(row + 16 * u));
+            for (uint64_t todo = __ballot(odd != 0); todo; todo &= todo - 1) {
+                const int k = __ffsll((unsigned long long)todo) - 1;
+                const char *token = (const char *)of_lane((int64_t)row, k);
+                if (!mine || base + k < lo || base + k >= hi) continue;
+                char *x = to;
+#pragma unroll 1
+                for (int d = d0; d < 8 * a.units; d += step, x += inc) {
+                    const s16x4 y = load<s16x4>(token + 2 * d);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (finite16<T>(y[i])) continue;
+                        if (f32) {
+                            volatile float *z = (float *)x + i;
+                            *z = pass ? *z + value16<T>(y[i]) : 0.0f;
+                        } else {
+                            volatile T *z = (T *)x + i;
+                            *z = (T)(pass ? (float)*z + value16<T>(y[i]) : 0.0f);
+                        }
+                    }
+                }
+            }
+        }
+}
+
+// The same in a join: a part's infinity under a factor that is too small for 32
+// bits has made the sum o NaN, and is what it should be. part(i): where part i's
+// four sums lie.
+template <class Place>
+__device__ inline f32x4 odd_parts(f32x4 o, int count, Place part) {
+    if (__builtin_expect(!__any(not_finite(o) != 0), 1)) return o;
+    f32x4 sum = {0, 0, 0, 0};
+    bool odd[4] = {};
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        const f32x4 x = *(const f32x4 *)part(i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (!(fabsf(x[k]) < INFINITY)) sum[k] += x[k], odd[k] = true;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = odd[k] ? sum[k] : o[k];
+    return o;
+}
+
 template <class T, bool F32>
 __device__ inline void put4(char *out, int64_t at, f32x4 x) {
     if constexpr (F32) {

@@ -39,6 +39,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
     __shared__ Entries ent;
     __shared__ __attribute__((aligned(1024))) char tiles[4 * 2 * N::kTile];
     __shared__ float stat[4][2][16];
+    __shared__ __attribute__((aligned(4))) char met_odd[4];
     const mpt_kv_cache &c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
     const int shift = 31 - __clz(c.page_size);
@@ -82,6 +83,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0, 0, 0, 0};
         float m = -INFINITY, l = 0;
+        bool met = false;                      // an infinity or NaN that was taken out of a product
 
         // lane t < 32 knows the page of token t of the wave's part of a step.
         // It is looked at only when it is used, a step later: a wait for it
@@ -178,24 +180,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
             }
             const s16x8 pf = __builtin_bit_cast(s16x8, w);
             if (masked) {
-                // Infinities and NaN in values: a weight of zero does not
-                // cancel them in a row that does not see them. Rows that do
-                // get them added here; then they are zeros for the product.
+                // zeros for infinities and NaN (odd_values)
                 uint32_t odd = 0;
 #pragma unroll 1
                 for (int x = lane; x < 32 * CH; x += 64) odd |= odd8<T>(*(const s16x8 *)(vw + 16 * x));
                 if (__any(odd != 0)) {
-#pragma unroll 1
-                    for (int tok = 0; tok < 32; ++tok) {
-                        const bool seen = t0 + tok >= see_lo && t0 + tok < see_hi;
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-                            const int d = dt * 16 + 4 * quad;
-                            const s16x4 x = *(const s16x4 *)(vw + tok * ROW + (((d / 8) ^ N::swizzle(tok)) << 4) + (d % 8) * 2);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[dt][i] += seen && !finite16<T>(x[i]) ? value16<T>(x[i]) : 0.0f;
-                        }
-                    }
+                    met = true;
 #pragma unroll 1
                     for (int x = lane; x < 32 * CH * 8; x += 64)
                         if (!finite16<T>(((const short *)vw)[x])) ((short *)vw)[x] = 0;
@@ -218,6 +208,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (quad == 0) stat[wave][0][col] = m, stat[wave][1][col] = l;
+        if (lane == 0) met_odd[wave] = met;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) *(f32x4 *)(vw + dt * 1024 + lane * 16) = o[dt];
         __syncthreads();
@@ -232,12 +223,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
         }
         const float scale = !(starts && ends) ? 1.0f : all_l == 0 ? 0.0f : 1.0f / all_l;
         float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (starts ? 1 : 0)) * (M * (DP + 2));
+        float odd = 0;
 #pragma unroll
         for (int k = 0; k < DT / 4; ++k) {
             const int dt = k * 4 + wave;
             f32x4 x = {0, 0, 0, 0};
 #pragma unroll
             for (int w = 0; w < 4; ++w) x += f[w] * *(const f32x4 *)(tiles + (2 * w + 1) * N::kTile + dt * 1024 + lane * 16);
+            odd += not_finite(x);
             x *= scale;
             if (starts && ends) {
                 const int d = dt * 16 + 4 * quad;
@@ -255,6 +248,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
                 const int workers = walk.second_of(range.count);
                 if (workers) a.parts[walk.worker] = Part{workers, e + walk.base, head, tile, q0, n};
             }
+        }
+        if (__builtin_expect(__any(*(const uint32_t *)met_odd | (odd != 0)), 0)) {
+            const bool whole = starts && ends, f32 = !whole || a.out_f32;
+            const int d = wave * 16 + 4 * quad, size = f32 ? 4 : 2;
+            odd_values<T>(a, table, shift, vh, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
+                          r < rows ? all_l : NAN, whole, d, 64,
+                          whole ? a.out + size * (token * a.out_token + hh * a.out_head + d) : (char *)(sums + (wave * 64 + lane) * 4),
+                          whole ? 64 * size : 4 * 64 * 16, f32);
         }
         __syncthreads();                      // the LDS is free again
         if (ends && walk.at < walk.end) walk.next(a, ent);
@@ -319,13 +320,14 @@ __global__ __launch_bounds__(256) void k_kv_join_narrow(Attn a) {
         l += f * stat[k][1][col];
         o += f * other[k][lane];
     }
+    o = odd_parts(o, part.count, [&](int i) { return sums(i) + (dt * 64 + lane) * 4; });
     const int rows = part.n * a.group, r = part.tile * M + col;
     if (r >= rows) return;
     const int j = token_of(a, r), d = dt * 16 + 4 * quad;
     const int64_t token = part.q0 + j, h = (int64_t)part.head * a.group + r - j * a.group;
     if (a.lse && dt == 0 && quad == 0)
         a.lse[token * a.heads + h] = l == 0 ? -INFINITY : 0.693147180559945f * (top + __builtin_amdgcn_logf(l));
-    if (d < 8 * a.units) store4<T>(a, token * a.out_token + h * a.out_head + d, o * (l == 0 ? 0.0f : 1.0f / l));
+    if (d < 8 * a.units) store4<T>(a, token * a.out_token + h * a.out_head + d, l == 0 ? f32x4{0, 0, 0, 0} : o * (1.0f / l));
 }
 
 template <class T, int DP>

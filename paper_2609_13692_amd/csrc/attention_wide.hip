@@ -274,48 +274,15 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
             pf[0] = __builtin_bit_cast(s16x8, packed[0]), pf[1] = __builtin_bit_cast(s16x8, packed[1]);
             __builtin_amdgcn_s_setprio(0);
         };
-        // Infinities and NaN in values of 32 tokens: a weight of zero does not
-        // cancel them in a row that does not see them. Rows that do see them
-        // get them added here, in memory, which costs the products no
-        // registers; then they are zeros for the product.
         float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (from == 0)) * (M * (DP + 2)) + wave * 32 * DP;
-        auto put_sums = [&]() INLINE {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4)
-                    *(f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4) = f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]};
-        };
-        auto odd_values = [&](int t0, char *vb) INLINE {
+        // Zeros for infinities and NaN in the values of 32 tokens (odd_values).
+        bool met = false;
+        auto take_odd = [&](char *vb) INLINE {
             uint32_t odd = 0;
 #pragma unroll 1
             for (int x = tid; x < 32 * CH; x += THREADS) odd |= odd8<T>(*(const s16x8 *)(vb + 16 * x));
             if (!__syncthreads_or(odd != 0)) return;
-            put_sums();
-#pragma unroll 1
-            for (int token = 0; token < 32; ++token) {
-                const bool seen = t0 + token >= see_lo && t0 + token < see_hi;
-#pragma unroll 1
-                for (int x = 0; x < DT * 4; ++x) {
-                    const s16x4 y = *(const s16x4 *)(vb + token * ROW + ((x ^ W::v_swizzle(token)) << 4) + 8 * half);
-                    float *z = sums + (x * 64 + lane) * 4;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (seen && !finite16<T>(y[i])) z[i] += value16<T>(y[i]);
-                }
-            }
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const f32x4 y = *(const f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4);
-                    o[dt][r] = y[0], o[dt][r + 1] = y[1], o[dt][r + 2] = y[2], o[dt][r + 3] = y[3];
-                }
-            // the wait for these loads here: where the paths meet it would
-            // hold up every step for all loads to LDS
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) asm volatile("" : "+v"(o[dt]));
-            __syncthreads();
+            met = true;
 #pragma unroll 1
             for (int x = tid; x < 32 * CH * 8; x += THREADS) {
                 short *y = (short *)vb + x;
@@ -386,7 +353,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 const int t = step * BN + 32 * h, v_before = h ? now : before + 32 * ROW;
-                if (t > first * BN && partly_seen(t - 32)) odd_values(t - 32, values + v_before);
+                if (t > first * BN && partly_seen(t - 32)) take_odd(values + v_before);
                 if (active) {
                     step32(std::false_type(), s0, s1, t, k_at + (h ? next : now + 32 * ROW), 0, v_at + v_before, 0);
                     s0 = s1;
@@ -409,7 +376,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         }
         {
             const int v_last = ((last - 1 - first) & (S - 1)) * TILE + 32 * ROW, t0 = last * BN - 32;
-            if (partly_seen(t0)) odd_values(t0, values + v_last);
+            if (partly_seen(t0)) take_odd(values + v_last);
             if (active) add(v_at + v_last, 0, nothing);
         }
 
@@ -438,13 +405,31 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide(Attn 
         } else {
             // unnormalised sums, in the order of the registers
             if (active) {
-                put_sums();
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *(f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4) = f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]};
                 (sums - wave * 32 * DP + M * DP + wave * 64)[lane] = half ? sum : m;
             }
             if (!starts && tid == 0) {
                 const int workers = walk.second_of(range.count);
                 if (workers) a.parts[walk.worker] = Part{workers, e + walk.base, head, tile, q0, n};
             }
+        }
+        float odd = 0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) odd += not_finite(f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]});
+        if (__builtin_expect(active && __any(met | (odd != 0)), 0)) {
+            const bool whole = starts && ends, f32 = !whole || a.out_f32;
+            const int size = f32 ? 4 : 2;
+            odd_values<T>(a, table, shift, vh, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
+                          r0 < rows ? sum : NAN, whole, 4 * half, 8,
+                          whole ? a.out + size * ((int64_t)(q0 + j0) * a.out_token + ((int64_t)head * a.group + rr - j0 * a.group) * a.out_head + 4 * half)
+                                : (char *)(sums + lane * 4),
+                          whole ? 8 * size : 64 * 16, f32);
         }
         if (ends && walk.at < walk.end) walk.next(a, ent);
     }
@@ -501,10 +486,17 @@ __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
         }
         m = now;
     }
+#pragma unroll
+    for (int k = 0; k < (DT + 3) / 4; ++k)
+        if (wave + 4 * k < DT)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                o[k][x] = odd_parts(o[k][x], part.count,
+                                    [&](int i) { return sums(i) + block * 32 * DP + (((wave + 4 * k) * 4 + x) * 64 + lane) * 4; });
     if (r >= rows) return;
     const int j = token_of(a, r);
     const int64_t token = part.q0 + j, h = (int64_t)part.head * a.group + r - j * a.group;
-    const float scale = l == 0 ? 0.0f : 1.0f / l;
+    const float scale = 1.0f / l;
     if (a.lse && wave == 0 && half == 0)
         a.lse[token * a.heads + h] = l == 0 ? -INFINITY : 0.693147180559945f * (m + __builtin_amdgcn_logf(l));
 #pragma unroll
@@ -513,7 +505,7 @@ __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 const int d = (wave + 4 * k) * 32 + 8 * x + 4 * half;
-                if (d < 8 * a.units) store4<T>(a, token * a.out_token + h * a.out_head + d, o[k][x] * scale);
+                if (d < 8 * a.units) store4<T>(a, token * a.out_token + h * a.out_head + d, l == 0 ? f32x4{0, 0, 0, 0} : o[k][x] * scale);
             }
 }
 
