@@ -659,8 +659,9 @@ int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, const int32_t 
 /*
  * Joins attention over disjoint parts of a context: for each row r < rows
  *     lse = log sum_p exp(lse_p),   out = sum_p exp(lse_p - lse) out_p,
- * which is attention over all parts together. Parts whose lse is minus
- * infinity are not read; without any other, out = 0 and lse = minus infinity.
+ * which is attention over all parts together. An infinity in a part stays one
+ * however small the part's weight. Parts whose lse is minus infinity are not
+ * read; without any other, out = 0 and lse = minus infinity.
  *   n_parts         1 .. MPT_KV_MAX_PARTS
  *   parts, part_lse HOST arrays [n_parts] of device pointers: [rows, dim]
  *                   (contiguous, 16-byte aligned, MPT_KV_* part_dtype) and

@@ -670,7 +670,7 @@ __global__ __launch_bounds__(256) void k_kv_merge(int n_parts, int64_t rows, int
             const float w = expf(l - top);      // NaN where l is, or where the largest is +inf
             sum += w;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += w * v[j];
+            for (int j = 0; j < 8; ++j) acc[j] += w == 0 && fabsf(v[j]) == INFINITY ? v[j] : w * v[j];   // no NaN
         }
         const float scale = sum == 0 ? 0.0f : 1.0f / sum;
 #pragma unroll

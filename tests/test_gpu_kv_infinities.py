@@ -87,3 +87,28 @@ def test_rows_of_no_weight_and_rows_of_nan(length, counts):
             assert torch.isnan(out[-1, 2]).all() and torch.isnan(lse[-1, 2])
             out[-1, 2], lse[-1, 2] = 0, -math.inf
             assert not out.any() and (lse == -math.inf).all(), how
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_merged_infinities_under_small_weights(dtype):
+    """Parts whose weights are e^-300 of the largest, or smaller than any."""
+    o = [torch.randn((6, 64)).to(dtype) for _ in range(3)]
+    lse = [torch.tensor([0.0, 300.0, 0.0, 5.0, -math.inf, math.nan]),
+           torch.tensor([300.0, 0.0, 1e30, 5.0, 0.0, 0.0]), torch.tensor([0.0, 0.0, 0.0, 0.0, 0.0, 0.0])]
+    o[0][:, 1] = math.inf
+    o[1][:, 2] = -math.inf
+    o[0][:, 3], o[1][:, 3] = math.inf, -math.inf
+    o[2][:, 4] = math.nan
+    got, total = kv.merge([x.cuda() for x in o], [x.cuda() for x in lse], out_dtype=torch.float32)
+    got, total = got.cpu(), total.cpu()
+    assert torch.isnan(got[5]).all() and torch.isnan(total[5])
+    for row in range(5):
+        there = [i for i in range(3) if lse[i][row] > -math.inf]
+        for d in range(1, 5):
+            want = sum(float(o[i][row, d]) for i in there if not math.isfinite(o[i][row, d]))
+            have = float(got[row, d])
+            if want == 0:
+                assert math.isfinite(have), (row, d)
+            else:
+                assert have == want or (math.isnan(have) and math.isnan(want)), (row, d, have, want)
+        assert torch.isfinite(got[row, 5:]).all()
