@@ -424,16 +424,23 @@ __device__ inline float not_finite(f32x4 x) {
 // whose sums came out infinite or NaN, ends here: a wave looks through the
 // values of tokens t0 .. t1 - 1 once more, and every sum that an infinity or NaN
 // belongs to becomes the sum of those alone, which is what the definition
-// gives. A lane's row sees lo .. hi - 1; its sums, groups of four dimensions
-// from d0 on, `step` apart, lie at `to`, `inc` bytes apart, in 32 bits or T.
-// l: the row's sum of weights (NaN: so are its sums). Without any weight a whole
-// row is zeros; parts keep what they saw, and their join decides.
-template <class T>
+// gives. Two bits a dimension hold it (infinities of either sign, both: NaN),
+// and the look ends where nothing can change any more. Chunks of 1024 tokens
+// over 16k as a lone call, 1.3 ms: 2.8 with one infinity among the values, 11
+// with one in every page, 1.3 with NaN everywhere, 149 with infinities
+// everywhere.
+//
+// A lane's row sees lo .. hi - 1; its sums, groups of four dimensions from d0 on,
+// `step` apart, lie at `to`, `inc` bytes apart, in 32 bits or T. l: the row's sum
+// of weights (NaN: so are its sums). Without any weight a whole row is zeros;
+// parts keep what they saw, and their join decides.
+template <class T, int GROUPS>
 __device__ inline void odd_values(const Attn &a, const int32_t *table, int shift, const char *values, int t0, int t1, int lo,
                                   int hi, float l, bool whole, int d0, int step, char *to, int inc, bool f32) {
-    const int lane = threadIdx.x & 63;
+    static_assert(GROUPS <= 16, "four bits a group");
+    const int lane = threadIdx.x & 63, dim = 8 * a.units;
     if (whole && l == 0)
-        for (int k = 0; d0 + k * step < 8 * a.units; ++k) {
+        for (int k = 0; d0 + k * step < dim; ++k) {
             if (f32)
                 *(f32x4 *)(to + k * inc) = f32x4{0, 0, 0, 0};
             else
@@ -441,36 +448,45 @@ __device__ inline void odd_values(const Attn &a, const int32_t *table, int shift
         }
     const bool mine = l > 0 || (l == 0 && !whole);
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass)                    // to zeros, then the sums
+    for (; __any(d0 < dim); d0 += GROUPS * step, to += GROUPS * inc) {          // GROUPS at a time
+        uint64_t up = 0, down = 0, all = 0;
+        for (int k = 0; k < GROUPS && d0 + k * step < dim; ++k) all |= 15ull << 4 * k;
 #pragma unroll 1
-        for (int base = t0; base < t1; base += 64) {
+        for (int base = t0; base < t1 && !__all(!mine || (up & down) == all); base += 64) {
             const int t = base + lane, page = t < t1 ? table[t >> shift] : -1;
             const char *row = values + row_at(page, t & (a.c.page_size - 1), a.v_page, a.v_slot);
             uint32_t odd = 0;
             if ((unsigned)page < (unsigned)a.c.n_pages)
                 for (int u = 0; u < a.units; ++u) odd |= odd8<T>(load<s16x8>(row + 16 * u));
-            for (uint64_t todo = __ballot(odd != 0); todo; todo &= todo - 1) {
-                const int k = __ffsll((unsigned long long)todo) - 1;
-                const char *token = (const char *)of_lane((int64_t)row, k);
-                if (!mine || base + k < lo || base + k >= hi) continue;
-                char *x = to;
 #pragma unroll 1
-                for (int d = d0; d < 8 * a.units; d += step, x += inc) {
-                    const s16x4 y = load<s16x4>(token + 2 * d);
+            for (uint64_t todo = __ballot(odd != 0); todo; todo &= todo - 1) {
+                const int at = __ffsll((unsigned long long)todo) - 1;
+                const char *token = (const char *)of_lane((int64_t)row, at) + 2 * d0;
+                if (!mine || base + at < lo || base + at >= hi || (up & down) == all) continue;
+#pragma unroll 4
+                for (int k = 0; k < GROUPS; ++k) {
+                    if (d0 + k * step >= dim) break;
+                    const s16x4 y = load<s16x4>(token + 2 * k * step);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (finite16<T>(y[i])) continue;
-                        if (f32) {
-                            volatile float *z = (float *)x + i;
-                            *z = pass ? *z + value16<T>(y[i]) : 0.0f;
-                        } else {
-                            volatile T *z = (T *)x + i;
-                            *z = (T)(pass ? (float)*z + value16<T>(y[i]) : 0.0f);
-                        }
+                        const float x = value16<T>(y[i]);
+                        up |= (uint64_t)(!finite16<T>(y[i]) && !(x < 0)) << (4 * k + i);
+                        down |= (uint64_t)(!finite16<T>(y[i]) && !(x > 0)) << (4 * k + i);
                     }
                 }
             }
         }
+#pragma unroll 1
+        for (uint64_t set = up | down; set; set &= set - 1) {
+            const int b = __ffsll((unsigned long long)set) - 1;
+            const float x = !(down >> b & 1) ? INFINITY : up >> b & 1 ? NAN : -INFINITY;
+            char *z = to + (b >> 2) * inc;
+            if (f32)
+                ((float *)z)[b & 3] = x;
+            else
+                ((T *)z)[b & 3] = (T)x;
+        }
+    }
 }
 
 // The same in a join: a part's infinity under a factor that is too small for 32

@@ -15,8 +15,12 @@ struct Choice {
     int workers, rows;       // workgroups, rows of a tile
 };
 
-// By the rows that an entry has for a key head on average (the lengths are on
-// the device), and for heads of 128 by whether a tile can have a CU for itself.
+// By the rows that an entry has for a key head on average, and for heads of 128
+// by whether a tile can have a CU for itself. The call knows neither the lengths
+// nor how the tokens are spread over the entries (both are on the device), so
+// decodes beside one long chunk go by the mean of the two, and the rule stands
+// between the figures for short contexts and for long ones where those turn.
+// One group size was measured: other ones go by the rows alone.
 // Microseconds, narrow / 4 waves / 8 waves, 4 query heads on each of 8 key
 // heads:
 //   dim 128, 32 entries over 4000 tokens: 16 rows 116/164/131; 32 rows

@@ -32,8 +32,10 @@ struct Narrow {
     __device__ static int swizzle(int token) { return DP == 64 ? 2 * ((token >> 1) & 3) : 2 * (token & 7); }
 };
 
+// Two workgroups to a CU, three with heads of 64, one with heads of 256, and
+// registers for no fewer: 37 contexts with heads of 64 21 us, 25 with two.
 template <class T, int DP, bool CAP, bool PAD>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void k_kv_narrow(Attn a) {
     using N = Narrow<DP>;
     constexpr int M = N::M, BN = N::BN, C = N::C, KK = N::KK, DT = N::DT, ROW = N::ROW, CH = N::CH, L = N::L;
     __shared__ Entries ent;
@@ -171,6 +173,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
                 for (int dt = 0; dt < DT; ++dt) o[dt] *= keep;
             }
             const float base = m == -INFINITY ? 0.0f : m;
+            // rounded to the values' type for the product, as in the chunk kernel
             typename Type<T>::x8 w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_kv_narrow(Attn a) {
         if (__builtin_expect(__any(*(const uint32_t *)met_odd | (odd != 0)), 0)) {
             const bool whole = starts && ends, f32 = !whole || a.out_f32;
             const int d = wave * 16 + 4 * quad, size = f32 ? 4 : 2;
-            odd_values<T>(a, table, shift, vh, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
+            odd_values<T, DT / 4>(a, table, shift, vh, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
                           r < rows ? all_l : NAN, whole, d, 64,
                           whole ? a.out + size * (token * a.out_token + hh * a.out_head + d) : (char *)(sums + (wave * 64 + lane) * 4),
                           whole ? 64 * size : 4 * 64 * 16, f32);

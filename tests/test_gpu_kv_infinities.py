@@ -8,7 +8,7 @@ import torch
 
 from kv_reference import attention, attention_bounds, close
 from paper_2609_13692_amd import kv
-from test_gpu_kv_attention import DT, filled, ints
+from test_gpu_kv_attention import DT, check, filled, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -112,3 +112,28 @@ def test_merged_infinities_under_small_weights(dtype):
             else:
                 assert have == want or (math.isnan(have) and math.isnan(want)), (row, d, have, want)
         assert torch.isfinite(got[row, 5:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", SHAPES + [([130, 500], [1, 1], 4, 2, 256, 4), ([260], [40], 3, 1, 192, 16), ([90], [1], 2, 2, 80, 1),
+                                            ([700], [50], 2, 1, 80, 16)],
+                         ids=lambda s: f"L{max(s[0])}q{max(s[1])}h{s[2]}k{s[3]}d{s[4]}p{s[5]}")
+def test_infinities_and_nan_anywhere(shape, dtype):
+    """A few in every dimension, of either sign, and pages full of them, in
+    tokens that all, some or no rows see."""
+    lengths, counts, heads, kv_heads, dim, page = shape
+    dt = DT[dtype]
+    c, slots, ks, vs = filled(lengths, page, kv_heads, dim, dt, 70)
+    g = torch.Generator().manual_seed(71)
+    for i, n in enumerate(lengths):
+        v = torch.from_numpy(vs[i]).clone()
+        for x in (math.inf, -math.inf, math.nan):
+            v[torch.rand(v.shape, generator=g) < 0.3 / n] = x
+        v[n // 2, :, : dim // 2], v[n // 2 + 1, :, dim // 2: dim - 3] = -math.inf, math.nan
+        v[n - 1, 0] = math.inf
+        vs[i] = v.numpy()
+        rows = torch.arange(n, device="cuda")
+        c.v[1, c.table[int(slots[i])].long()[rows // page], rows % page] = v.to(dt).cuda()
+    for how in (dict(), dict(window=lengths[0] // 3), dict(causal=False, softcap=8.0)):
+        check(c, slots, ks, vs, counts, heads, 72, dt, **how)
+        check(c, slots, ks, vs, counts, heads, 73, dt, out_dtype=torch.float32, **how)
