@@ -19,21 +19,23 @@ struct Choice {
 // by whether a tile can have a CU for itself. The call knows neither the lengths
 // nor how the tokens are spread over the entries (both are on the device), so
 // decodes beside one long chunk go by the mean of the two, and the rule stands
-// between the figures for short contexts and for long ones where those turn.
-// One group size was measured: other ones go by the rows alone.
+// between the figures for short contexts and for long ones.
 // Microseconds, narrow / 4 waves / 8 waves, 4 query heads on each of 8 key
-// heads:
-//   dim 128, 32 entries over 4000 tokens: 16 rows 116/164/131; 32 rows
-//   122/164/131; 48 rows 302/173/132; 128 rows 452/192/139; 160 rows
-//   573/214/148; 256 rows 895/233/181. 32 over 300: 48 rows 33/32/28; 128 rows
-//   50/38/34. 8 over 4000: 48 rows 75/57/48; 128 rows 81/77/55; over 300 22/31/33
-//   dim 128, 128 entries over 300: 16 rows 39/54/69; 32 rows 62/52/70; 48 rows
-//   85/57/73; 128 rows 208/76/98; 256 rows 444/136/137. 128 over 4000, where it
-//   turns (the call does not know): 48 rows 1086/505/428; 128 rows 2863/547/471
-//   dim 64, 32 entries over 4000: 16 rows 54/61/62; 20 rows 95/62/65; 128 rows
-//   325/74/73; 256 rows 632/106/102. 128 over 4000: 128 rows 1459/219/293; 160
-//   rows 1840/421/355
-//   dim 256, 32 entries over 2000: 16 rows 105/132; 20 rows 198/135
+// heads (other groups go by the rows alone):
+//   dim 128, 32 entries over 4000 tokens: 16 rows 115/130/122; 32 rows
+//   123/131/122; 48 rows 297/138/122; 128 rows 444/149/124; 160 rows
+//   555/159/145; 256 rows 890/219/170. 32 over 300: 48 rows 32/28/26; 128 rows
+//   48/33/31. 8 over 4000: 48 rows 73/50/45; 128 rows 76/67/52; over 300 20/23/23
+//   dim 128, 128 entries over 300: 16 rows 36/43/66; 32 rows 60/44/66; 48 rows
+//   86/47/69; 128 rows 205/65/92; 256 rows 436/118/130. 128 over 4000: 48 rows
+//   1049/401/398; 128 rows 2733/416/447
+//   dim 64, 32 entries over 4000: 16 rows 53/62/67; 20 rows 94/61/65; 128 rows
+//   327/73/75; 256 rows 633/111/105. 128 over 4000: 128 rows 1445/250/292; 160
+//   rows 1817/425/349
+//   dim 256, 32 entries over 2000: 16 rows 105/121; 20 rows 195/119
+// The limit of 32 rows for heads of 128 was drawn when 4 waves took 164 us where
+// they now take 131 and 52 where they take 44: at 17 to 32 rows narrow tiles no
+// longer gain.
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);

@@ -28,8 +28,8 @@
 // chunks over up to 4099 tokens with a window from 101 to 92 us, 25 ragged
 // chunks over up to 8400 from 816 to 775 (797 TFLOP/s), the chunks above to
 // 1031 (1021 TFLOP/s; a library product of 8192^3 reaches 1210 on this card).
-// Infinities among the values at the tile's end instead of at its steps: 45 and
-// 44 KB with fewer registers put into memory; 91.9 to 86.5, 781 to 756 and 1039 to
+// Infinities among the values at the tile's end instead of at its steps: 46 and
+// 43 KB with fewer registers put into memory; 91.9 to 86.5, 781 to 756 and 1039 to
 // 1021 us, both sides on one card.
 
 #include "attention.h"

@@ -7,7 +7,9 @@ off its parent: the parent's pages are shared, only the node's own chunk is
 computed (its keys and values appended, its queries attended over the whole
 prefix), so the tokens computed are the layout's trie cost (Eq. 1), which
 ``mpt_layout_cost`` bills. Nodes that no request ends at are freed once their
-children exist; their pages live on in the children.
+children exist, unless the prefill is told to keep their depth; their pages live
+on in the children. It is a demonstration of the cache's calls: one layer, and a
+decode step whose tokens are not appended.
 
 ``python -m paper_2609_13692_amd.serve`` runs a small retrieval-shaped instance
 through the exact solver, the cache and a decode step in which each first
