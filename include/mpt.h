@@ -483,9 +483,10 @@ int mpt_pinned_assemble(int m, int64_t nnz, const int64_t *req_off, const int32_
  * dimensions are free (heads inside or outside the slots, layers or keys and
  * values interleaved). Rows must not overlap.
  *
- * Errors in device data: a call that finds one changes nothing in tables and
- * pages and ORs MPT_KV_* bits into *status, where they stay until
- * mpt_kv_status reads them. The page calls take a nullable HOST output; with
+ * Errors in device data: a call that finds one ORs MPT_KV_* bits into *status,
+ * where they stay until mpt_kv_status reads them. The page calls (forks to
+ * copies below) then change nothing in tables and pages, appends write the
+ * tokens that are in order. The page calls take a nullable HOST output; with
  * it they synchronise `stream` and return the error of this call
  * (MPT_E_RANGE, MPT_E_DUP, MPT_E_STATE or MPT_E_PAGES). Without it, and in
  * mpt_kv_append, mpt_kv_attention and mpt_kv_merge, nothing synchronises, and
