@@ -501,6 +501,8 @@ int mpt_pinned_assemble(int m, int64_t nnz, const int64_t *req_off, const int32_
 #define MPT_KV_BF16 0
 #define MPT_KV_F16 1
 #define MPT_KV_F32 2              /* outputs and merged parts only */
+#define MPT_KV_BF16_MX4 3         /* rows in 4 bits whose elements bfloat16 holds exactly, */
+#define MPT_KV_F16_MX4 4          /* and float16: a cache of mpt_kv_cache_mx4 */
 #define MPT_KV_MAX_DIM 256
 #define MPT_KV_MAX_PAGE_SIZE 1024
 #define MPT_KV_MAX_PAGES (1 << 26)
@@ -524,12 +526,41 @@ typedef struct mpt_kv_cache {
     int32_t *ref;                 /* device [n_pages] */
     uint64_t *free_bits;          /* device [(n_pages + 63) / 64] */
     uint32_t *status;             /* device: MPT_KV_* bits */
-    int dtype;                    /* MPT_KV_BF16 or MPT_KV_F16 */
+    int dtype;                    /* MPT_KV_BF16 or MPT_KV_F16 (4 bits: below) */
     int n_layers, n_pages;
     int page_size;                /* a power of two, 1 .. MPT_KV_MAX_PAGE_SIZE */
     int n_heads, head_dim;        /* key/value heads; a multiple of 8, 8 .. MPT_KV_MAX_DIM */
     int max_seqs, max_pages;      /* max_pages * page_size <= 2^30 */
 } mpt_kv_cache;
+
+/*
+ * A cache in 4 bits: its descriptor is the `c` of an mpt_kv_cache_mx4, dtype one
+ * of the MX4 types, and every call below takes &x.c. head_dim is a multiple of
+ * 32. Each 32 consecutive elements of a row share a byte E; an element has a
+ * code of 4 bits, a sign (8) and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3, 4,
+ * 6 (0 .. 7), and stands for its code's value times 2^(E - 127). E = 255: all 32
+ * are NaN. (This is the 4-bit type of the Open Compute microscaling formats,
+ * which the matrix cores' conversions read: 4.25 bits an element.)
+ *
+ * k and v hold the codes, two to a byte, the lower bits first: rows of
+ * head_dim / 2 bytes, and k_stride and v_stride count bytes, multiples of 16.
+ * k_scale and v_scale hold the E of a row, head_dim / 32 consecutive bytes;
+ * their addresses and strides (in bytes) are multiples of the largest power of
+ * two that divides head_dim / 32, as they are in an array without gaps.
+ *
+ * Appends write for each 32 elements x the smallest exponent e = E - 127 with
+ * max |x| <= 7 * 2^e in -125 .. 125 (bfloat16) or -23 .. 13 (float16), where every
+ * value is finite and exact in the 16-bit type, and the codes nearest to x / 2^e:
+ * of two as near the even one, 6 for all that is larger. With a NaN or an
+ * infinity among the 32, E = 255. What a cache holds in other bytes E is read as
+ * far as the 16-bit type holds it.
+ */
+typedef struct mpt_kv_cache_mx4 {
+    mpt_kv_cache c;
+    void *k_scale, *v_scale;      /* device */
+    int64_t k_scale_stride[4];    /* bytes from one layer, page, slot, head to the next */
+    int64_t v_scale_stride[4];
+} mpt_kv_cache_mx4;
 
 /* Empties the cache: every page free, every length 0, status 0. Does not
  * synchronise. */
@@ -600,9 +631,9 @@ int mpt_kv_copy(const mpt_kv_cache *cache, int n, const int32_t *src, const int3
  * they go to positions length - (q_off[i+1] - q_off[i]) .. length - 1.
  *   seqs [n]             device; distinct
  *   q_off [n+1]          device; q_off[0] = 0, non-decreasing, q_off[n] = n_tokens
- *   k_new, v_new         device, the cache's type, [n_tokens, n_heads,
- *                        head_dim]; strides in elements, multiples of 8;
- *                        16-byte aligned
+ *   k_new, v_new         device, the cache's type (of one in 4 bits its 16-bit
+ *                        type), [n_tokens, n_heads, head_dim]; strides in
+ *                        elements, multiples of 8; 16-byte aligned
  * Tokens before position 0, in bad slots or pages, or in pages that other
  * sequences refer to are not written (and set status bits).
  */
@@ -610,6 +641,62 @@ int mpt_kv_append(const mpt_kv_cache *cache, int layer, int n, const int32_t *se
                   const int32_t *q_off, int64_t n_tokens, const void *k_new,
                   int64_t k_token_stride, int64_t k_head_stride, const void *v_new,
                   int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/*
+ * The rotation of keys and queries to their positions. Of each row the first
+ * `dim` elements are dim / 2 pairs (x1, x2): elements i and i + dim / 2, or
+ * 2i and 2i + 1 if interleaved. At position p pair i becomes
+ *     y1 = x1 c - x2 s,   y2 = x2 c + x1 s
+ * with c = factor cos(p freq[i]), s = factor sin(p freq[i]), the angle and its
+ * cosine formed in 64 bits. Further elements stay as they are.
+ */
+typedef struct mpt_kv_rotation {
+    const float *freq;            /* device [dim / 2]: radians per position */
+    const int32_t *position;      /* device [n_tokens], nullable: each token's place in its sequence */
+    int dim;                      /* a multiple of 16, 16 .. head_dim */
+    int interleaved;
+    float factor;
+} mpt_kv_rotation;
+
+/*
+ * mpt_kv_append with the new keys rotated on the way, and the queries of the
+ * same tokens rotated beside them: row (token, head) of q to that of q_out.
+ * In a cache of 16 bits the sums above are formed in 32 bits and rounded to its
+ * type, as q_out is; in one of 4 bits keys are rotated in 64 bits and rounded once.
+ * Queries of tokens that are not written are rotated all the same, at
+ * length - (q_off[i+1] - q_off[i]) + j, which may be negative; where there is no
+ * such place (bad slots, tokens of no entry) and no position is given, q_out is
+ * left as it was.
+ *   q, q_out   device, the cache's 16-bit type, [n_tokens, n_q_heads, head_dim];
+ *              both nullable (no queries); q_out may be q with equal strides
+ *   k_new      nullable with v_new: queries alone; then, with positions, n may
+ *              be 0
+ *   rotation   HOST
+ */
+int mpt_kv_append_rotated(const mpt_kv_cache *cache, int layer, int n, const int32_t *seqs,
+                          const int32_t *q_off, int64_t n_tokens, const void *k_new,
+                          int64_t k_token_stride, int64_t k_head_stride, const void *v_new,
+                          int64_t v_token_stride, int64_t v_head_stride,
+                          const mpt_kv_rotation *rotation, int n_q_heads, const void *q,
+                          int64_t q_token_stride, int64_t q_head_stride, void *q_out,
+                          int64_t out_token_stride, int64_t out_head_stride, void *stream);
+
+/*
+ * Reads tokens of one layer out in the cache's 16-bit type: entry i < n has the
+ * rows off[i] .. off[i+1] - 1 of k_out and v_out, for the tokens from first[i] on
+ * of the sequence in slot seqs[i] (first NULL: its newest). Rows of tokens that
+ * are not there (before the first, past the last, on bad pages, in bad slots)
+ * are zeros, and set status bits; rows of no entry are left as they were.
+ *   seqs [n]        device; a slot may be listed several times
+ *   off [n+1]       device; off[0] = 0, non-decreasing, off[n] = n_tokens
+ *   first [n]       device, nullable
+ *   k_out, v_out    device [n_tokens, n_heads, head_dim], either nullable;
+ *                   strides in elements, multiples of 8; 16-byte aligned
+ */
+int mpt_kv_read(const mpt_kv_cache *cache, int layer, int n, const int32_t *seqs,
+                const int32_t *off, const int32_t *first, int64_t n_tokens, void *k_out,
+                int64_t k_token_stride, int64_t k_head_stride, void *v_out,
+                int64_t v_token_stride, int64_t v_head_stride, void *stream);
 
 /* Bytes of device workspace (256-byte aligned) for mpt_kv_attention of n
  * entries and n_tokens tokens with n_q_heads query heads: at most 68 MiB, the
@@ -643,12 +730,13 @@ size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_
  *   q_off [n+1]    device; q_off[0] = 0, non-decreasing, q_off[n] = n_tokens
  *   q, out         device [n_tokens, n_q_heads, head_dim]; strides in
  *                  elements, multiples of 8; 16-byte aligned. q has the
- *                  cache's type, out that type or MPT_KV_F32 (out_dtype)
+ *                  cache's type (of one in 4 bits its 16-bit type), out that
+ *                  type or MPT_KV_F32 (out_dtype)
  *   lse            device out, nullable: float [n_tokens * n_q_heads],
  *                  natural logarithms
  *   kv_begin [n]   device, nullable (0): first visible token
  * Scores, statistics and sums are held in 32 bits; the weights exp(s_t - max)
- * are rounded to the cache's type for the product with the values.
+ * are rounded to the cache's (16-bit) type for the product with the values.
  */
 int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, const int32_t *seqs,
                      const int32_t *q_off, int64_t n_tokens, int n_q_heads, const void *q,

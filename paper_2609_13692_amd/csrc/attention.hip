@@ -76,6 +76,7 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
             return fail(MPT_E_INVALID, "n = %d, n_tokens = %lld", n, (long long)n_tokens);
         if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % cache->n_heads)
             return fail(MPT_E_INVALID, "n_q_heads = %d is no multiple of the cache's %d", n_q_heads, cache->n_heads);
+        if (is_mx4(*cache)) return fail(MPT_E_INVALID, "no attention over 4 bits");
         if (out_dtype != cache->dtype && out_dtype != MPT_KV_F32)
             return fail(MPT_E_INVALID, "out_dtype = %d is neither the cache's type nor MPT_KV_F32", out_dtype);
         if (n_tokens * (n_q_heads / cache->n_heads) > (1 << 30))

@@ -77,8 +77,6 @@ __device__ inline int pages_of(const mpt_kv_cache &c, int tokens) {
     return (int)(((int64_t)tokens + c.page_size - 1) >> (31 - __clz(c.page_size)));
 }
 
-__device__ inline bool slot_ok(const mpt_kv_cache &c, int s) { return s >= 0 && s < c.max_seqs; }
-__device__ inline bool page_ok(const mpt_kv_cache &c, int p) { return p >= 0 && p < c.n_pages; }
 // A page of the pool that a table can refer to: one with references.
 __device__ inline bool page_held(const mpt_kv_cache &c, int p) { return page_ok(c, p) && c.ref[p] > 0; }
 
@@ -295,6 +293,39 @@ __device__ inline void copy_rows(char *base, const int64_t *stride, int64_t laye
     }
 }
 
+// The bytes E of the same rows, in words W that divide a row. Rows without gaps
+// go as one run, of 16 bytes where its ends are aligned to that.
+template <class W>
+__device__ inline void copy_words(char *base, int64_t from, int64_t to, int64_t s_slot, int64_t s_head, int tokens, int heads,
+                                  int words) {
+    const int total = tokens * heads * words;
+    for (int x = threadIdx.x; x < total; x += blockDim.x) {
+        const int row = x / words, head = row / tokens;
+        const int64_t off = head * s_head + (row - head * tokens) * s_slot + (x - row * words) * (int)sizeof(W);
+        *(W *)(base + to + off) = *(const W *)(base + from + off);
+    }
+}
+__device__ inline void copy_scales(char *base, const int64_t *stride, int64_t layer, int a, int b, int tokens, int page_size,
+                                   int heads, int bytes) {
+    const int64_t from = layer * stride[0] + (int64_t)a * stride[1], to = layer * stride[0] + (int64_t)b * stride[1];
+    const int64_t run = (int64_t)tokens * heads * bytes;
+    if (((stride[2] == bytes && stride[3] == (int64_t)page_size * bytes && tokens == page_size) ||
+         (stride[3] == bytes && stride[2] == (int64_t)heads * bytes)) &&
+        (((uintptr_t)base | (uint64_t)from | (uint64_t)to | (uint64_t)run) & 15) == 0) {
+        for (int64_t x = 16 * (int)threadIdx.x; x < run; x += 16 * (int)blockDim.x)
+            *(uint4 *)(base + to + x) = *(const uint4 *)(base + from + x);
+        return;
+    }
+    if (bytes % 8 == 0)
+        copy_words<uint64_t>(base, from, to, stride[2], stride[3], tokens, heads, bytes / 8);
+    else if (bytes % 4 == 0)
+        copy_words<uint32_t>(base, from, to, stride[2], stride[3], tokens, heads, bytes / 4);
+    else if (bytes % 2 == 0)
+        copy_words<uint16_t>(base, from, to, stride[2], stride[3], tokens, heads, bytes / 2);
+    else
+        copy_words<uint8_t>(base, from, to, stride[2], stride[3], tokens, heads, bytes);
+}
+
 // A reference less. A page that counts fewer than the tables have, which no
 // look at one entry shows, stays at none.
 __device__ inline void drop(const mpt_kv_cache &c, int page) {
@@ -309,7 +340,7 @@ __device__ inline void drop(const mpt_kv_cache &c, int page) {
 // Forks and growth as planned: workgroup (i, 0) writes entry i's row of the
 // table and the references, workgroups (i, y) copy the keys or the values of
 // a partial page's tokens in a layer.
-__global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t *src, const int32_t *dst,
+__global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, Scales e, const int32_t *src, const int32_t *dst,
                                                   const int32_t *new_len, Plan p) {
     if (p.head->err) return;
     const int i = blockIdx.x, tid = threadIdx.x, d = dst[i], first = p.start[i], from = p.from[i];
@@ -322,6 +353,9 @@ __global__ __launch_bounds__(256) void k_kv_apply(mpt_kv_cache c, const int32_t 
                 copy_rows((char *)c.v, c.v_stride, y >> 1, from, to, part, c.page_size, c.n_heads, units);
             else
                 copy_rows((char *)c.k, c.k_stride, y >> 1, from, to, part, c.page_size, c.n_heads, units);
+            if (e.bytes)
+                copy_scales(y & 1 ? e.v : e.k, y & 1 ? e.v_stride : e.k_stride, y >> 1, from, to, part, c.page_size, c.n_heads,
+                            e.bytes);
         }
     }
     if (blockIdx.y) return;
@@ -472,7 +506,7 @@ __global__ __launch_bounds__(1024) void k_kv_plan_moves(mpt_kv_cache c, Plan p) 
 // a load a thread, which was not measured. Used
 // pages that move are found from their number by a search in a, which
 // ascends; no table entry below n_live changes.
-__global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Plan p, int tables) {
+__global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Scales e, Plan p, int tables) {
     const int moves = p.head->moves, units = c.head_dim / 8;
     if (p.head->err || moves == 0) return;
     for (int64_t x = blockIdx.x; x < 2ll * moves * c.n_layers; x += gridDim.x) {
@@ -482,6 +516,9 @@ __global__ __launch_bounds__(256) void k_kv_move(mpt_kv_cache c, Plan p, int tab
             copy_rows((char *)c.v, c.v_stride, rest >> 1, a, b, c.page_size, c.page_size, c.n_heads, units);
         else
             copy_rows((char *)c.k, c.k_stride, rest >> 1, a, b, c.page_size, c.page_size, c.n_heads, units);
+        if (e.bytes)
+            copy_scales(rest & 1 ? e.v : e.k, rest & 1 ? e.v_stride : e.k_stride, rest >> 1, a, b, c.page_size, c.page_size,
+                        c.n_heads, e.bytes);
         if (tables && rest == 0 && threadIdx.x == 0) {
             c.ref[b] = c.ref[a];
             c.ref[a] = 0;
@@ -562,22 +599,6 @@ __global__ __launch_bounds__(256) void k_kv_reset(mpt_kv_cache c) {
 }
 
 __global__ void k_kv_clear_status(mpt_kv_cache c, uint32_t bits) { atomicAnd(c.status, ~bits); }
-
-// Index of the last entry of off[0 .. n] that is <= x (off ascends), found by
-// the 64 lanes of a wave together, 64 places a step.
-__device__ inline int wave_find(const int32_t *off, int n, int x) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, len = n + 1;
-    while (len > 1) {
-        const int step = (len + 63) / 64, at = lo + lane * step;
-        const uint64_t le = __ballot(lane * step < len && off[at] <= x);
-        if (!le) return -1;
-        const int k = 63 - __clzll(le);
-        lo += k * step;
-        len = min(step, len - k * step);
-    }
-    return off[lo] <= x ? lo : -1;
-}
 
 // One wave per token: the row of keys and the row of values, 16 bytes per lane.
 // Bound by memory: 15763 tokens of 8 heads of 128 in 21 us (6 TB/s read and
@@ -693,7 +714,8 @@ using mptlib::fail;
 
 int check_cache(const mpt_kv_cache *c) {
     if (!c) return fail(MPT_E_INVALID, "cache is NULL");
-    if (c->dtype != MPT_KV_BF16 && c->dtype != MPT_KV_F16) return fail(MPT_E_INVALID, "cache: dtype = %d", c->dtype);
+    if (c->dtype < MPT_KV_BF16 || c->dtype > MPT_KV_F16_MX4 || c->dtype == MPT_KV_F32)
+        return fail(MPT_E_INVALID, "cache: dtype = %d", c->dtype);
     if (c->n_layers < 1 || c->n_pages < 1 || c->n_pages > MPT_KV_MAX_PAGES)
         return fail(MPT_E_INVALID, "cache: n_layers = %d, n_pages = %d", c->n_layers, c->n_pages);
     if (c->page_size < 1 || c->page_size > MPT_KV_MAX_PAGE_SIZE || (c->page_size & (c->page_size - 1)))
@@ -710,7 +732,31 @@ int check_cache(const mpt_kv_cache *c) {
     for (int i = 0; i < 4; ++i)
         if (c->k_stride[i] < 0 || c->v_stride[i] < 0 || c->k_stride[i] % 8 || c->v_stride[i] % 8)
             return fail(MPT_E_INVALID, "cache: strides must be multiples of 8, not negative");
+    if (!is_mx4(*c)) return MPT_OK;
+    if (c->head_dim % 32) return fail(MPT_E_INVALID, "cache: head_dim = %d in 4 bits is no multiple of 32", c->head_dim);
+    const Scales e = scales_of(*c);
+    if (!e.k || !e.v) return fail(MPT_E_INVALID, "cache: an array is NULL");
+    const int word = e.bytes & -e.bytes;              // the largest power of two that divides a row
+    if (((uintptr_t)e.k | (uintptr_t)e.v) & (word - 1))
+        return fail(MPT_E_INVALID, "cache: k_scale and v_scale must be aligned to %d bytes", word);
+    for (int i = 0; i < 4; ++i) {
+        if (c->k_stride[i] % 16 || c->v_stride[i] % 16)
+            return fail(MPT_E_INVALID, "cache: strides of codes must be multiples of 16 bytes");
+        if (e.k_stride[i] < 0 || e.v_stride[i] < 0 || e.k_stride[i] % word || e.v_stride[i] % word)
+            return fail(MPT_E_INVALID, "cache: strides of scales must be multiples of %d, not negative", word);
+    }
     return MPT_OK;
+}
+
+// A cache as the page calls' launches take it: elements of two bytes. In 4 bits a
+// row of head_dim / 2 bytes is one of head_dim / 4 of them.
+static mpt_kv_cache in_two_bytes(const mpt_kv_cache &c) {
+    mpt_kv_cache x = c;
+    if (is_mx4(c)) {
+        x.head_dim /= 4;
+        for (int i = 0; i < 4; ++i) x.k_stride[i] /= 2, x.v_stride[i] /= 2;
+    }
+    return x;
 }
 
 // Entries that a list of sequences can have: distinct slots, a workgroup each of
@@ -762,7 +808,8 @@ static int grow(const mpt_kv_cache *c, int n, const int32_t *src, const int32_t 
     }
     if (n) {
         mptlib::LaunchScope scope("k_kv_apply", n, s);
-        k_kv_apply<<<dim3(n, c->n_layers < 32 ? 2 * c->n_layers : 64), 256, 0, s>>>(*c, src, dst, new_len, p);
+        k_kv_apply<<<dim3(n, c->n_layers < 32 ? 2 * c->n_layers : 64), 256, 0, s>>>(in_two_bytes(*c), scales_of(*c), src, dst, new_len,
+                                                                                       p);
     }
     if (free_pages && !src) {                  // copies of shared pages may have left some without references
         mptlib::LaunchScope scope("k_kv_count", c->n_pages, s);
@@ -878,7 +925,7 @@ extern "C" int mpt_kv_compact(const mpt_kv_cache *cache, int64_t *live_pages, vo
         }
         {
             mptlib::LaunchScope scope("k_kv_move", cache->n_pages, s);
-            k_kv_move<<<2048, 256, 0, s>>>(*cache, p, 1);
+            k_kv_move<<<2048, 256, 0, s>>>(in_two_bytes(*cache), scales_of(*cache), p, 1);
         }
         return report(p, live_pages, "mpt_kv_compact", s);
     });
@@ -898,7 +945,7 @@ extern "C" int mpt_kv_copy(const mpt_kv_cache *cache, int n, const int32_t *src,
         }
         if (n) {
             mptlib::LaunchScope scope("k_kv_move", n, s);
-            k_kv_move<<<2048, 256, 0, s>>>(*cache, p, 0);
+            k_kv_move<<<2048, 256, 0, s>>>(in_two_bytes(*cache), scales_of(*cache), p, 0);
         }
         return report(p, checked, "mpt_kv_copy", s);
     });
@@ -910,15 +957,16 @@ extern "C" int mpt_kv_append(const mpt_kv_cache *cache, int layer, int n, const 
     mptlib::clear_error();
     return mptlib::guarded(__func__, [&]() -> int {
         if (int rc = check_cache(cache)) return rc;
-        if (layer < 0 || layer >= cache->n_layers) return fail(MPT_E_INVALID, "layer = %d", layer);
-        if (n < 0 || n_tokens < 0 || n_tokens > INT32_MAX)
-            return fail(MPT_E_INVALID, "n = %d, n_tokens = %lld", n, (long long)n_tokens);
+        if (int rc = check_append(cache, layer, n, n_tokens)) return rc;
         if (n == 0 || n_tokens == 0) return MPT_OK;
         if (!seqs || !q_off || !k_new || !v_new) return fail(MPT_E_INVALID, "an array is NULL");
         if (!aligned16(k_new) || !aligned16(v_new)) return fail(MPT_E_INVALID, "k_new and v_new must be 16-byte aligned");
         if ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) % 8)
             return fail(MPT_E_INVALID, "strides must be multiples of 8");
         hipStream_t s = (hipStream_t)stream;
+        if (is_mx4(*cache))
+            return append_mx4(cache, layer, n, seqs, q_off, n_tokens, k_new, k_token_stride, k_head_stride, v_new,
+                              v_token_stride, v_head_stride, s);
         {
             mptlib::LaunchScope scope("k_kv_append", (double)n_tokens, s);
             k_kv_append<<<mptlib::grid_for(n_tokens, 4, 4096), 256, 0, s>>>(

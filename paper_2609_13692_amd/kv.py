@@ -1,6 +1,7 @@
-"""The paged key/value cache of include/mpt.h: pages that the sequences of a
-layout share, appends, attention of new tokens over the pages, and the join of
-attention over parts of a context.
+"""The paged key/value cache of include/mpt.h, in 16 bits or in 4: pages that the
+sequences of a layout share, appends (with the rotation to positions on the
+way, if asked), attention of new tokens over the pages, tokens read back, and
+the join of attention over parts of a context.
 
 As :mod:`.mpt` this only marshals arguments: every step runs in the HIP kernels
 of ``libmpt.so``. Calls enqueue on the current stream (or ``stream``) and
@@ -15,9 +16,9 @@ import struct
 
 import torch
 
-from .mpt import KvDescriptor, MptError, _check, load
+from .mpt import KvDescriptor, KvDescriptorMx4, KvRotation, MptError, _check, load
 
-BF16, F16, F32 = 0, 1, 2
+BF16, F16, F32, MX4 = 0, 1, 2, 3                # MX4: added to a 16-bit type
 _KIND = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 MAX_PARTS = 16
 _POINTERS = [struct.Struct(f"{n}P").pack for n in range(MAX_PARTS + 1)]      # host arrays of device pointers
@@ -78,41 +79,64 @@ class KvCache:
     per page: together the state described at ``mpt_kv_cache``.
     :meth:`create` allocates and empties one.
 
+    In 4 bits (``mpt_kv_cache_mx4``) ``k`` and ``v`` are uint8 [layers, pages,
+    slots per page, heads, dim / 2], of strides that are multiples of 16, with
+    ``k_scale`` and ``v_scale`` uint8 [layers, pages, slots per page, heads,
+    dim / 32], and ``dtype`` (bfloat16 or float16) is the type that tokens come
+    in and are read as.
+
     The cache holds the workspaces of its calls: of attention one for each size
     that its calls need (at most three), all of them for as long as the cache
     lives, so that graphs captured earlier stay valid. Calls on one cache must
     be ordered (one stream, or events between streams).
     """
 
-    def __init__(self, k, v, table, length, ref, free_bits, status):
+    def __init__(self, k, v, table, length, ref, free_bits, status, k_scale=None, v_scale=None, dtype=None):
         if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must be [layers, pages, slots, heads, dim] of one shape and type")
-        if k.dtype not in (torch.bfloat16, torch.float16):
+        four = k_scale is not None or v_scale is not None
+        if four:
+            if k.dtype is not torch.uint8:
+                raise TypeError(f"k and v with scales must be uint8, got {k.dtype}")
+            if dtype not in (torch.bfloat16, torch.float16):
+                raise TypeError(f"a cache in 4 bits needs dtype bfloat16 or float16, got {dtype}")
+            for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+                if t is None or t.dtype is not torch.uint8 or t.device != k.device or \
+                        t.shape != (*k.shape[:4], k.shape[4] // 16) or k.shape[4] % 16 or t.stride(4) != 1:
+                    raise ValueError(f"{name} must be uint8 [layers, pages, slots, heads, dim / 32] on {k.device}, with contiguous rows")
+        elif k.dtype not in (torch.bfloat16, torch.float16) or dtype not in (None, k.dtype):
             raise TypeError(f"k and v must be bfloat16 or float16, got {k.dtype}")
         if not k.is_cuda:
             raise ValueError("k must be a device tensor")
         if k.stride(4) != 1 or v.stride(4) != 1:
             raise ValueError("the elements of a row must be contiguous")
         layers, pages, size, heads, dim = k.shape
-        for name, t, dtype, n in (("ref", ref, torch.int32, pages), ("free_bits", free_bits, torch.int64, -(-pages // 64)),
+        dim, kind = (2 * dim, _KIND[dtype] + MX4) if four else (dim, _KIND[k.dtype])
+        for name, t, want, n in (("ref", ref, torch.int32, pages), ("free_bits", free_bits, torch.int64, -(-pages // 64)),
                                   ("status", status, torch.int32, 1), ("length", length, torch.int32, 1),
                                   ("table", table, torch.int32, 1), ("v", v, v.dtype, 0)):
-            if t.dtype != dtype or t.device != k.device or t.numel() < n or (name != "v" and not t.is_contiguous()):
-                raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on {k.device}")
+            if t.dtype != want or t.device != k.device or t.numel() < n or (name != "v" and not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous {want} tensor of at least {n} elements on {k.device}")
         if table.dim() != 2 or table.shape[0] != length.numel():
             raise ValueError("table must be [slots, pages of a sequence], length [slots]")
         self.k, self.v, self.table, self.length, self.ref = k, v, table, length, ref
         self.free_bits, self.status = free_bits, status
-        self.device, self.dtype, self.page_size, self.n_heads, self.head_dim = k.device, k.dtype, size, heads, dim
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.device, self.dtype = k.device, dtype if four else k.dtype
+        self.page_size, self.n_heads, self.head_dim = size, heads, dim
         self.max_seqs, self._index = table.shape[0], k.get_device()
-        d = KvDescriptor()
+        whole = KvDescriptorMx4()
+        d = whole.c
         d.k, d.v = k.data_ptr(), v.data_ptr()
         d.k_stride[:], d.v_stride[:] = k.stride()[:4], v.stride()[:4]
         d.table, d.length, d.ref = table.data_ptr(), length.data_ptr(), ref.data_ptr()
         d.free_bits, d.status = free_bits.data_ptr(), status.data_ptr()
-        d.dtype, d.n_layers, d.n_pages, d.page_size = _KIND[k.dtype], layers, pages, size
+        d.dtype, d.n_layers, d.n_pages, d.page_size = kind, layers, pages, size
         d.n_heads, d.head_dim, d.max_seqs, d.max_pages = heads, dim, table.shape[0], table.shape[1]
-        self._d = d
+        if four:
+            whole.k_scale, whole.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+            whole.k_scale_stride[:], whole.v_scale_stride[:] = k_scale.stride()[:4], v_scale.stride()[:4]
+        self._whole, self._d = whole, d
         self._p = ctypes.addressof(d)
         self._lib = load()
         n = self._lib.mpt_kv_workspace_bytes(self._p)
@@ -125,17 +149,32 @@ class KvCache:
 
     @classmethod
     def create(cls, n_layers, n_pages, page_size, n_heads, head_dim, max_seqs, max_len, dtype=torch.bfloat16,
-               device="cuda", heads_first=False):
-        """An empty cache; ``heads_first`` puts a page's heads outside its slots."""
-        shape = (n_layers, n_pages) + ((n_heads, page_size) if heads_first else (page_size, n_heads)) + (head_dim,)
-        # zeros: a page is copied whole, tokens that were never written included
-        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
-        if heads_first:
-            k, v = k.transpose(2, 3), v.transpose(2, 3)
+               device="cuda", heads_first=None, bits=16):
+        """An empty cache of 16 or 4 bits; ``heads_first`` puts a page's heads
+        outside its slots (None: in 4 bits, where a head's row alone is a part
+        of what memory hands out at a time)."""
+        if bits not in (16, 4):
+            raise ValueError(f"a cache has 16 bits or 4, got {bits}")
+        if bits == 4 and head_dim % 32:
+            raise ValueError(f"head_dim in 4 bits must be a multiple of 32, got {head_dim}")
+        if heads_first is None:
+            heads_first = bits == 4
+        shape = (n_layers, n_pages) + ((n_heads, page_size) if heads_first else (page_size, n_heads))
+
+        def pool(row, dtype):
+            # zeros: a page is copied whole, tokens that were never written included
+            x = torch.zeros((*shape, row), dtype=dtype, device=device)
+            return x.transpose(2, 3) if heads_first else x
+        how = {}
+        if bits == 4:
+            k, v = (pool(head_dim // 2, torch.uint8) for _ in range(2))
+            how = dict(k_scale=pool(head_dim // 32, torch.uint8), v_scale=pool(head_dim // 32, torch.uint8), dtype=dtype)
+        else:
+            k, v = (pool(head_dim, dtype) for _ in range(2))
         i32 = dict(dtype=torch.int32, device=device)
         c = cls(k, v, torch.full((max_seqs, max(1, -(-max_len // page_size))), -1, **i32), torch.zeros(max_seqs, **i32),
                 torch.zeros(n_pages, **i32), torch.zeros(-(-n_pages // 64), dtype=torch.int64, device=device),
-                torch.zeros(1, **i32))
+                torch.zeros(1, **i32), **how)
         c.reset()
         return c
 
@@ -214,6 +253,71 @@ class KvCache:
                   *self._rows(v_new, self.n_heads, "v_new", self.dtype), _on(stream, index)[0])
         if rc:
             _check(rc, "mpt_kv_append")
+
+    def append_rotated(self, layer, k_new, v_new, q_off, seqs, freq, q=None, q_out=None, interleaved=False, positions=None,
+                       factor=1.0, stream=None):
+        """As append, with the keys (and the queries q [tokens, heads, dim])
+        rotated to their positions: pair i of a row by position * freq[i], its
+        first 2 len(freq) elements in all (see mpt_kv_append_rotated). Returns
+        the rotated queries, in q_out (which may be q) or a new tensor; None
+        without any. positions [tokens] int32 in the place of the tokens' own in
+        their sequences; with k_new and v_new None nothing is written, and then,
+        with positions, q_off and seqs may be None."""
+        index = self._index
+        at, under = _on(stream, index)
+        if freq.dtype is not torch.float32 or freq.get_device() != index or freq.dim() != 1 or not freq.is_contiguous():
+            raise ValueError(f"freq must be a contiguous float32 vector on GPU {index}")
+        if (k_new is None) != (v_new is None) or (k_new is None and q is None):
+            raise ValueError("needs k_new and v_new, or q, or all three")
+        if q is None and q_out is not None:
+            raise ValueError("q_out without q")
+        tokens = (q if k_new is None else k_new).shape[0]
+        for name, t in (("v_new", v_new), ("q", q), ("q_out", q_out)):
+            if t is not None and t.shape[0] != tokens:
+                raise ValueError(f"{name} must have one row per token")
+        n = 0 if seqs is None else seqs.numel()
+        if seqs is None and (k_new is not None or positions is None or q_off is not None):
+            raise ValueError("needs q_off and seqs, but for queries alone with positions")
+        heads, rows = 1, [None, 0, 0]
+        if q is not None:
+            heads = q.shape[1]
+            rows = self._rows(q, heads, "q", self.dtype)
+            if q_out is None:
+                q_out = _new(q.shape, self.dtype, self.device, under)
+        r = KvRotation()
+        r.freq, r.dim, r.interleaved, r.factor = freq.data_ptr(), 2 * freq.numel(), bool(interleaved), factor
+        r.position = None if positions is None else _list(positions, tokens, "positions", index)
+        rc = _run(index, self._lib.mpt_kv_append_rotated, self._p, layer, n, *((None, None) if seqs is None else (
+                  _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index))), tokens,
+                  *((None, 0, 0) if k_new is None else self._rows(k_new, self.n_heads, "k_new", self.dtype)),
+                  *((None, 0, 0) if v_new is None else self._rows(v_new, self.n_heads, "v_new", self.dtype)),
+                  ctypes.addressof(r), heads, *rows,
+                  *((None, 0, 0) if q is None else self._rows(q_out, heads, "q_out", self.dtype)), at)
+        if rc:
+            _check(rc, "mpt_kv_append_rotated")
+        return q_out
+
+    def read(self, layer, off, seqs, tokens, first=None, k_out=None, v_out=None, stream=None):
+        """(keys, values) [tokens, heads, dim] of one layer in the cache's 16-bit
+        type: of entry i those from first[i] on (None: the newest) of the
+        sequence in slot seqs[i], off[i + 1] - off[i] of them, in rows off[i] on.
+        Tokens that are not there are zeros (see mpt_kv_read)."""
+        n, index = seqs.numel(), self._index
+        at, under = _on(stream, index)
+        shape = (tokens, self.n_heads, self.head_dim)
+        rows = []
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            if t is None:
+                t = _new(shape, self.dtype, self.device, under)
+            elif t.shape[0] != tokens:
+                raise ValueError(f"{name} must have one row per token")
+            rows.append((t, self._rows(t, self.n_heads, name, self.dtype)))
+        rc = _run(index, self._lib.mpt_kv_read, self._p, layer, n, _list(seqs, n, "seqs", index),
+                  _list(off, n + 1, "off", index), None if first is None else _list(first, n, "first", index), tokens,
+                  *rows[0][1], *rows[1][1], at)
+        if rc:
+            _check(rc, "mpt_kv_read")
+        return rows[0][0], rows[1][0]
 
     def attend(self, layer, q, q_off, seqs, causal=True, window=0, softcap=0.0, scale=None, kv_begin=None, out=None,
                lse=None, out_dtype=None, stream=None):

@@ -44,7 +44,7 @@ EXPORTED = ("mpt_workspace_bytes", "mpt_build_weights", "mpt_solve_exact", "mpt_
             "mpt_copy_table", "mpt_table_device", "mpt_solve_exact_noalloc", "mpt_ctx_optimum",
             "mpt_profile_begin_prefix", "mpt_kv_reset", "mpt_kv_status", "mpt_kv_workspace_bytes", "mpt_kv_fork",
             "mpt_kv_extend", "mpt_kv_free", "mpt_kv_compact", "mpt_kv_copy", "mpt_kv_append",
-            "mpt_kv_attention_workspace_bytes", "mpt_kv_attention", "mpt_kv_merge")
+            "mpt_kv_append_rotated", "mpt_kv_read", "mpt_kv_attention_workspace_bytes", "mpt_kv_attention", "mpt_kv_merge")
 
 
 class MptError(RuntimeError):
@@ -67,6 +67,18 @@ class KvDescriptor(ctypes.Structure):
                 ("dtype", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_pages", ctypes.c_int),
                 ("page_size", ctypes.c_int), ("n_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
                 ("max_seqs", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+
+class KvDescriptorMx4(ctypes.Structure):
+    """mpt_kv_cache_mx4: of a cache in 4 bits."""
+    _fields_ = [("c", KvDescriptor), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("k_scale_stride", ctypes.c_int64 * 4), ("v_scale_stride", ctypes.c_int64 * 4)]
+
+
+class KvRotation(ctypes.Structure):
+    """mpt_kv_rotation."""
+    _fields_ = [("freq", ctypes.c_void_p), ("position", ctypes.c_void_p), ("dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("factor", ctypes.c_float)]
 
 
 _lib = None
@@ -152,6 +164,9 @@ def load() -> ctypes.CDLL:
                        ("free", [P, i32, P, P, P, P, sz, P]), ("compact", [P, P, P, sz, P]),
                        ("copy", [P, i32, P, P, P, P, sz, P]),
                        ("append", [P, i32, i32, P, P, i64, P, i64, i64, P, i64, i64, P]),
+                       ("append_rotated", [P, i32, i32, P, P, i64, P, i64, i64, P, i64, i64, P, i32, P, i64, i64, P, i64,
+                                           i64, P]),
+                       ("read", [P, i32, i32, P, P, P, i64, P, i64, i64, P, i64, i64, P]),
                        ("attention", [P, i32, i32, P, P, i64, i32, P, i64, i64, P, i64, i64, i32, P, P, i32, i32, f32,
                                       f32, P, sz, P]),
                        ("merge", [i32, i64, i32, P, P, i32, P, i32, P, P])):
