@@ -11,7 +11,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SRCS = [os.path.join(CSRC, f) for f in ("mpt.hip", "ctx.hip", "greedy.hip", "layout.hip", "pinned.hip")]
-KV_SRCS = [os.path.join(CSRC, f) for f in ("attention_wide.hip", "attention_narrow.hip", "attention.hip", "rows.hip", "kv.hip")]
+KV_SRCS = [os.path.join(CSRC, f) for f in ("attention_wide.hip", "attention_narrow.hip", "attention_wide_mx4.hip",
+                                               "attention_narrow_mx4.hip", "attention.hip", "rows.hip", "kv.hip")]
 LIB = os.path.join(PKG, "libmpt.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -525,8 +525,10 @@ __device__ inline void store4(const Attn &a, int64_t at, f32x4 x) {
 
 inline int pad_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
-// Launch of a kernel and of its join.
+// Launch of a kernel and of its join; the joins alone.
 void launch_wide(const Attn &a, int waves, hipStream_t s);
 void launch_narrow(const Attn &a, hipStream_t s);
+void join_wide(const Attn &a, int waves, hipStream_t s);
+void join_narrow(const Attn &a, hipStream_t s);
 
 }  // namespace mptkv

@@ -1,7 +1,7 @@
 // Attention of new tokens over the paged key/value cache: checks, the choice
 // of a kernel and its workspace.
 
-#include "attention.h"
+#include "attention_mx4.h"
 
 #include <cmath>
 
@@ -40,7 +40,10 @@ static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_hea
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
     const bool own_cu = dim == 128 && (int64_t)n * c.n_heads <= 256;
-    if (rows <= (dim == 128 ? 32 : 16)) return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
+    if (rows <= (dim == 128 ? 32 : 16)) {
+        if (is_mx4(c)) return {0, dim == 256 ? 256 : dim == 128 ? 768 : 1024, 16};
+        return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
+    }
     if ((rows <= 128 && !own_cu) || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
     return {8, 256, 256};
 }
@@ -76,8 +79,7 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
             return fail(MPT_E_INVALID, "n = %d, n_tokens = %lld", n, (long long)n_tokens);
         if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % cache->n_heads)
             return fail(MPT_E_INVALID, "n_q_heads = %d is no multiple of the cache's %d", n_q_heads, cache->n_heads);
-        if (is_mx4(*cache)) return fail(MPT_E_INVALID, "no attention over 4 bits");
-        if (out_dtype != cache->dtype && out_dtype != MPT_KV_F32)
+        if (out_dtype != value_type(*cache) && out_dtype != MPT_KV_F32)
             return fail(MPT_E_INVALID, "out_dtype = %d is neither the cache's type nor MPT_KV_F32", out_dtype);
         if (n_tokens * (n_q_heads / cache->n_heads) > (1 << 30))
             return fail(MPT_E_INVALID, "%lld tokens with %d query heads a key head", (long long)n_tokens,
@@ -95,7 +97,7 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
                         workspace_bytes, need);
         hipStream_t s = (hipStream_t)stream;
         const Choice ch = choose(*cache, n, n_tokens, n_q_heads);
-        Attn a = {};
+        Attn4 a = {};
         a.c = *cache;
         a.layer = layer, a.n = n, a.n_tokens = (int)n_tokens, a.heads = n_q_heads, a.group = n_q_heads / cache->n_heads;
         a.units = cache->head_dim / 8;
@@ -114,24 +116,38 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
         if (!std::isfinite(a.factor) || !std::isfinite(softcap * log2e))
             return fail(MPT_E_INVALID, "scale = %g, softcap = %g", scale, softcap);
         a.cap = softcap * log2e;
-        for (int i = 1; i < 3; ++i)
-            if (cache->k_stride[i] / 8 * (i == 2 ? cache->page_size : 1) > UINT32_MAX ||
-                cache->v_stride[i] / 8 * (i == 2 ? cache->page_size : 1) > UINT32_MAX)
+        const bool mx4 = is_mx4(*cache);
+        const int piece = mx4 ? 16 : 8, size = mx4 ? 1 : 2;        // strides of 16 bytes; bytes of what strides count
+        const Scales e = scales_of(*cache);
+        for (int i = 1; i < 3; ++i) {
+            const int64_t times = i == 2 ? cache->page_size : 1;
+            if (cache->k_stride[i] / piece * times > UINT32_MAX || cache->v_stride[i] / piece * times > UINT32_MAX)
                 return fail(MPT_E_INVALID, "cache: a page, or the stride of pages, of 64 GiB or more");
-        a.k_page = (uint32_t)(cache->k_stride[1] / 8), a.k_slot = (uint32_t)(cache->k_stride[2] / 8);
-        a.v_page = (uint32_t)(cache->v_stride[1] / 8), a.v_slot = (uint32_t)(cache->v_stride[2] / 8);
+            if (e.k_stride[i] * times > UINT32_MAX || e.v_stride[i] * times > UINT32_MAX)
+                return fail(MPT_E_INVALID, "cache: a page's scales, or the stride of pages, of 4 GiB or more");
+        }
+        a.k_page = (uint32_t)(cache->k_stride[1] / piece), a.k_slot = (uint32_t)(cache->k_stride[2] / piece);
+        a.v_page = (uint32_t)(cache->v_stride[1] / piece), a.v_slot = (uint32_t)(cache->v_stride[2] / piece);
         const auto near = [&](uint64_t page, uint64_t slot) {
             return cache->n_pages <= 1 << 24 && page < 1 << 24 &&
                    (cache->n_pages - 1) * page + (cache->page_size - 1) * slot + a.units <= 1 << 28;
         };
         a.near = near(a.k_page, a.k_slot) && near(a.v_page, a.v_slot);
-        a.k = (const char *)cache->k + 2 * layer * cache->k_stride[0];
-        a.v = (const char *)cache->v + 2 * layer * cache->v_stride[0];
-        a.k_head = 2 * cache->k_stride[3], a.v_head = 2 * cache->v_stride[3];
+        a.k = (const char *)cache->k + size * layer * cache->k_stride[0];
+        a.v = (const char *)cache->v + size * layer * cache->v_stride[0];
+        a.k_head = size * cache->k_stride[3], a.v_head = size * cache->v_stride[3];
+        if (mx4) {
+            a.ke = e.k + layer * e.k_stride[0], a.ve = e.v + layer * e.v_stride[0];
+            a.ke_head = e.k_stride[3], a.ve_head = e.v_stride[3];
+            a.ke_page = (uint32_t)e.k_stride[1], a.ke_slot = (uint32_t)e.k_stride[2];
+            a.ve_page = (uint32_t)e.v_stride[1], a.ve_slot = (uint32_t)e.v_stride[2];
+        }
         a.workers = ch.workers;
         a.parts = (Part *)workspace;
         a.sums = (float *)((char *)workspace + mptlib::align256(sizeof(Part) * ch.workers));
-        if (ch.waves)
+        if (mx4)
+            ch.waves ? launch_wide_mx4(a, ch.waves, s) : launch_narrow_mx4(a, s);
+        else if (ch.waves)
             launch_wide(a, ch.waves, s);
         else
             launch_narrow(a, s);

@@ -334,6 +334,12 @@ __global__ __launch_bounds__(256) void k_kv_join_narrow(Attn a) {
 }
 
 template <class T, int DP>
+static void launch_join(const Attn &a, hipStream_t s) {
+    mptlib::LaunchScope scope("k_kv_join_narrow", a.workers, s);
+    k_kv_join_narrow<T, DP><<<dim3(a.workers, (a.units + 1) / 2), 256, 0, s>>>(a);
+}
+
+template <class T, int DP>
 static void launch(const Attn &a, hipStream_t s) {
     {
         mptlib::LaunchScope scope("k_kv_narrow", (double)a.n_tokens * a.heads, s);
@@ -342,14 +348,21 @@ static void launch(const Attn &a, hipStream_t s) {
                                        : (pad ? k_kv_narrow<T, DP, false, true> : k_kv_narrow<T, DP, false, false>);
         kernel<<<a.workers, 256, 0, s>>>(a);
     }
-    mptlib::LaunchScope scope("k_kv_join_narrow", a.workers, s);
-    k_kv_join_narrow<T, DP><<<dim3(a.workers, (a.units + 1) / 2), 256, 0, s>>>(a);
+    launch_join<T, DP>(a, s);
 }
 
 template <class T>
 static void launch_dim(const Attn &a, hipStream_t s) {
     const int dim = pad_dim(8 * a.units);
     dim == 64 ? launch<T, 64>(a, s) : dim == 128 ? launch<T, 128>(a, s) : launch<T, 256>(a, s);
+}
+
+void join_narrow(const Attn &a, hipStream_t s) {
+    const int dim = pad_dim(8 * a.units);
+    if (value_type(a.c) == MPT_KV_BF16)
+        dim == 64 ? launch_join<__bf16, 64>(a, s) : dim == 128 ? launch_join<__bf16, 128>(a, s) : launch_join<__bf16, 256>(a, s);
+    else
+        dim == 64 ? launch_join<_Float16, 64>(a, s) : dim == 128 ? launch_join<_Float16, 128>(a, s) : launch_join<_Float16, 256>(a, s);
 }
 
 void launch_narrow(const Attn &a, hipStream_t s) {

@@ -519,6 +519,12 @@ __global__ __launch_bounds__(256) void k_kv_join_wide(Attn a) {
 }
 
 template <class T, int DP, int WAVES>
+static void launch_join(const Attn &a, hipStream_t s) {
+    mptlib::LaunchScope scope("k_kv_join_wide", a.workers, s);
+    k_kv_join_wide<T, DP, WAVES><<<dim3(a.workers, WAVES), 256, 0, s>>>(a);
+}
+
+template <class T, int DP, int WAVES>
 static void launch(const Attn &a, hipStream_t s) {
     {
         mptlib::LaunchScope scope("k_kv_wide", (double)a.n_tokens * a.heads, s);
@@ -527,8 +533,7 @@ static void launch(const Attn &a, hipStream_t s) {
         else
             k_kv_wide<T, DP, WAVES, false><<<a.workers, 64 * WAVES, 0, s>>>(a);
     }
-    mptlib::LaunchScope scope("k_kv_join_wide", a.workers, s);
-    k_kv_join_wide<T, DP, WAVES><<<dim3(a.workers, WAVES), 256, 0, s>>>(a);
+    launch_join<T, DP, WAVES>(a, s);
 }
 
 template <class T>
@@ -540,6 +545,21 @@ static void launch_dim(const Attn &a, int waves, hipStream_t s) {
         waves == 8 ? launch<T, 128, 8>(a, s) : launch<T, 128, 4>(a, s);
     else
         launch<T, 256, 4>(a, s);
+}
+
+template <class T>
+static void join_dim(const Attn &a, int waves, hipStream_t s) {
+    const int dim = pad_dim(8 * a.units);
+    if (dim == 64)
+        waves == 8 ? launch_join<T, 64, 8>(a, s) : launch_join<T, 64, 4>(a, s);
+    else if (dim == 128)
+        waves == 8 ? launch_join<T, 128, 8>(a, s) : launch_join<T, 128, 4>(a, s);
+    else
+        launch_join<T, 256, 4>(a, s);
+}
+
+void join_wide(const Attn &a, int waves, hipStream_t s) {
+    value_type(a.c) == MPT_KV_BF16 ? join_dim<__bf16>(a, waves, s) : join_dim<_Float16>(a, waves, s);
 }
 
 void launch_wide(const Attn &a, int waves, hipStream_t s) {
