@@ -2,10 +2,10 @@
 // the rotation of keys and queries to their positions, rows in 4 bits, and
 // tokens read back.
 //
-// A wave takes a token, or a part of one where there are few: pieces of 8
-// elements, 64 at a time, of its keys, its values and its queries. The angles of
-// a token are formed once per wave, in 64 bits (an angle of position 10^6 in 32
-// bits would be off by 0.06), and handed out through LDS.
+// A wave takes a run of tokens, whose places its lanes find together, or a part of
+// one token where there are few. Of each it forms the angles, in 64 bits (an angle
+// of position 10^6 in 32 bits would be off by 0.06), and hands them out through LDS;
+// its keys, values and queries go 64 units of 8 or 16 elements at a time.
 
 #include "kv.h"
 
@@ -19,7 +19,7 @@ using mptlib::fail;
 struct Append {
     mpt_kv_cache c;
     Scales e;
-    int layer, n, n_tokens, heads, parts;            // parts: waves of a token
+    int layer, n, n_tokens, heads, run, parts;       // run: tokens of a wave; parts: waves that share them
     const int32_t *seqs, *q_off, *position;
     const char *k, *v, *q;
     char *q_out;
@@ -29,6 +29,49 @@ struct Append {
     int pairs, dim, e_min, e_max;                    // rotated pairs of a row; head_dim
     uint32_t turn_mul, copy_mul;                     // of divisions by a row's units
 };
+
+// Where a token goes: lane l knows it of the l-th of the wave's tokens.
+struct Place {
+    int page, slot;          // page -1: nowhere
+    int pos;                 // place in its sequence
+    bool known;              // it has one
+    uint32_t bad;            // MPT_KV_* bits
+};
+
+// Places of tokens x0 + lane, lane < count, cut into entries by off. first: where an
+// entry's tokens begin (NULL: they are the sequence's newest).
+__device__ inline Place locate(const mpt_kv_cache &c, int n, const int32_t *seqs, const int32_t *off, const int32_t *first, int x0,
+                               int count) {
+    const int lane = threadIdx.x & 63, shift = 31 - __clz(c.page_size);
+    Place p = {-1, 0, 0, false, 0};
+    int i = n > 0 ? wave_find(off, n, x0) : -1;
+    if (lane >= count) return p;
+    const int x = x0 + lane;
+    if (i >= 0 && i < n && x >= off[i + 1]) {            // a later entry's
+        int lo = i + 1, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (off[mid] <= x)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        i = lo;
+    }
+    p.bad = MPT_KV_BAD_SLOT;
+    if (i < 0 || i >= n || !slot_ok(c, seqs[i])) return p;
+    const int s = seqs[i];
+    const int length = max(0, (int)min((int64_t)c.length[s], (int64_t)c.max_pages << shift));
+    p.pos = first ? (int)min((int64_t)first[i] + (x - off[i]), (int64_t)INT32_MAX) : length - (off[i + 1] - x);
+    p.known = true;
+    p.bad = MPT_KV_BAD_LENGTH;
+    if (p.pos < 0 || p.pos >= length) return p;
+    p.bad = MPT_KV_BAD_PAGE;
+    const int page = c.table[(int64_t)s * c.max_pages + (p.pos >> shift)];
+    if (!page_ok(c, page)) return p;
+    p.page = page, p.slot = p.pos & (c.page_size - 1), p.bad = 0;
+    return p;
+}
 
 struct Turn64 { double c, s; };
 struct Turn32 { float c, s; };
@@ -48,7 +91,19 @@ __device__ inline uint4 narrow(const float *y) {
     return v.u;
 }
 
-// x / units by a product: mul = ceil(2^32 / units), x below 2^21, units up to 32.
+// The wave's number in its launch, and a launch of so many waves, four to a
+// workgroup: a dimension of it holds less than 2^32 threads.
+__device__ inline int64_t wave_number() {
+    return ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + uniform((int)threadIdx.x >> 6);
+}
+static dim3 grid_of(int64_t waves) {
+    constexpr int64_t kAcross = 1 << 23;
+    const int64_t blocks = (waves + 3) / 4;
+    return dim3((unsigned)(blocks < kAcross ? blocks : kAcross), (unsigned)((blocks + kAcross - 1) / kAcross));
+}
+
+// x / units by a product: mul = ceil(2^32 / units), x units below 2^32 (and so the
+// product's error below one part in units).
 __device__ inline int divided(int x, uint32_t mul) { return mul ? (int)__umulhi((uint32_t)x, mul) : x; }
 
 // Units of a row that is rotated in 16 bits: with pairs apart a unit is the two
@@ -59,37 +114,46 @@ __host__ __device__ inline int turn_units(int dim, int pairs) {
     return NEIGHBOURS ? dim / 8 : pairs / 8 + (dim - 2 * pairs) / 8;
 }
 
+// Where a unit's one or two pieces lie in a row of 16 bits, in bytes, and whether it
+// is rotated.
+template <bool NEIGHBOURS>
+__device__ inline void unit_at(int pairs, int u, int &first, int &second, bool &turns) {
+    turns = NEIGHBOURS ? 4 * u < pairs : 8 * u < pairs;
+    first = NEIGHBOURS || turns ? 16 * u : 4 * pairs + 16 * (u - pairs / 8);
+    second = NEIGHBOURS || !turns ? first : 16 * u + 2 * pairs;
+}
+
 // One unit of a row of queries or of 16-bit keys.
 template <class T, bool NEIGHBOURS>
-__device__ inline void turn_row(const Append &a, const char *in, char *out, int u, const Turn32 *turns) {
-    if (NEIGHBOURS ? 4 * u < a.pairs : 8 * u < a.pairs) {
-        float x[8], y[8];
-        if (NEIGHBOURS) {
-            widen<T>(*(const uint4 *)(in + 16 * u), x);
+__device__ inline void turn_unit(int pairs, uint4 a, uint4 b, char *out, int u, const Turn32 *table) {
+    int first, second;
+    bool turns;
+    unit_at<NEIGHBOURS>(pairs, u, first, second, turns);
+    if (!turns) {
+        *(uint4 *)(out + first) = a;
+        return;
+    }
+    float x[8], y[8];
+    widen<T>(a, x);
+    if (NEIGHBOURS) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Turn32 t = turns[4 * u + i];
-                y[2 * i] = x[2 * i] * t.c - x[2 * i + 1] * t.s;
-                y[2 * i + 1] = x[2 * i + 1] * t.c + x[2 * i] * t.s;
-            }
-            *(uint4 *)(out + 16 * u) = narrow<T>(y);
-        } else {
-            float z[8], w[8];
-            widen<T>(*(const uint4 *)(in + 16 * u), x);
-            widen<T>(*(const uint4 *)(in + 2 * a.pairs + 16 * u), z);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const Turn32 t = turns[8 * u + i];
-                y[i] = x[i] * t.c - z[i] * t.s;
-                w[i] = z[i] * t.c + x[i] * t.s;
-            }
-            *(uint4 *)(out + 16 * u) = narrow<T>(y);
-            *(uint4 *)(out + 2 * a.pairs + 16 * u) = narrow<T>(w);
+        for (int i = 0; i < 4; ++i) {
+            const Turn32 t = table[4 * u + i];
+            y[2 * i] = x[2 * i] * t.c - x[2 * i + 1] * t.s;
+            y[2 * i + 1] = x[2 * i + 1] * t.c + x[2 * i] * t.s;
         }
     } else {
-        const int at = NEIGHBOURS ? 16 * u : 4 * a.pairs + 16 * (u - a.pairs / 8);
-        *(uint4 *)(out + at) = *(const uint4 *)(in + at);
+        float z[8], w[8];
+        widen<T>(b, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const Turn32 t = table[8 * u + i];
+            y[i] = x[i] * t.c - z[i] * t.s;
+            w[i] = z[i] * t.c + x[i] * t.s;
+        }
+        *(uint4 *)(out + second) = narrow<T>(w);
     }
+    *(uint4 *)(out + first) = narrow<T>(y);
 }
 
 // y rounded to 24 bits so that a later rounding to fewer gives what y itself
@@ -103,154 +167,241 @@ __device__ inline float to_odd(double y) {
 
 __device__ inline uint32_t umax(uint32_t x, uint32_t y) { return x > y ? x : y; }
 
-// Eight elements of a row in 4 bits, with those of the three lanes beside it that
-// have the rest of their 32: the codes, and the byte E that belongs to them.
-__device__ inline uint32_t to_codes(const float *y, int e_min, int e_max, int &scale) {
+// 32 elements in 4 bits: the codes, and the byte E that belongs to them.
+__device__ inline uint4 to_codes(const float *y, int e_min, int e_max, int &scale) {
     uint32_t top = 0;                                // by their bits: a NaN is above all numbers
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = umax(top, __builtin_bit_cast(uint32_t, y[i]) & 0x7fffffffu);
-    top = umax(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xb1, 0xf, 0xf, true));    // lanes 1 0 3 2
-    top = umax(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4e, 0xf, 0xf, true));    // lanes 2 3 0 1
+    for (int i = 0; i < 32; ++i) top = umax(top, __builtin_bit_cast(uint32_t, y[i]) & 0x7fffffffu);
     // max <= 7 2^e: 7 = 1.75 2^2
     int e = (int)(top >> 23) - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
     e = min(max(e, e_min), e_max);
     const float unit = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
-    uint32_t codes = 0;
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], unit, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], unit, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], unit, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], unit, 3);
     const bool odd = top >= 0x7f800000u;
     scale = odd ? 255 : e + 127;
-    return odd ? 0 : codes;
+    uint32_t codes[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float *z = y + 8 * w;
+        codes[w] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, z[0], z[1], unit, 0);
+        codes[w] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes[w], z[2], z[3], unit, 1);
+        codes[w] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes[w], z[4], z[5], unit, 2);
+        codes[w] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes[w], z[6], z[7], unit, 3);
+        if (odd) codes[w] = 0;
+    }
+    return uint4{codes[0], codes[1], codes[2], codes[3]};
 }
 
-// One piece of a row of keys in 64 bits, rotated, as the sums' 24 odd bits.
-template <class T, bool NEIGHBOURS>
-__device__ inline void turn_piece(const Append &a, const char *in, int u, const Turn64 *turns, float *y) {
-    float x[8];
-    widen<T>(*(const uint4 *)(in + 16 * u), x);
-    if (4 * u >= a.pairs) {
+// How keys are rotated: not at all, pairs of neighbours, pairs half the rotated
+// elements apart.
+enum Keys { kWhole, kNeighbours, kApart };
+
+// The 32 elements from 32 b on of a row of keys, rotated in 64 bits and cut so that
+// they round as they are.
+template <class T, int KEYS>
+__device__ inline void turn_block(int pairs, const char *row, int b, const Turn64 *table, float *y) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[i];
-    } else if (NEIGHBOURS) {
+    for (int w = 0; w < 4; ++w) widen<T>(*(const uint4 *)(row + 64 * b + 16 * w), y + 8 * w);
+    if (KEYS == kWhole || 16 * b >= pairs) return;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const Turn64 t = turns[4 * u + i];
-            const double p = x[2 * i], r = x[2 * i + 1];
-            y[2 * i] = to_odd(p * t.c - r * t.s);
-            y[2 * i + 1] = to_odd(r * t.c + p * t.s);
-        }
-    } else {
-        float z[8];
-        const bool upper = 8 * u >= a.pairs;
-        const int first = 8 * u - (upper ? a.pairs : 0);
-        widen<T>(*(const uint4 *)(in + 16 * u + (upper ? -2 : 2) * a.pairs), z);
+    for (int w = 0; w < 4; ++w) {
+        const int u = 4 * b + w;
+        float *x = y + 8 * w;
+        if (4 * u >= pairs) continue;
+        if (KEYS == kNeighbours) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const Turn64 t = turns[first + i];
-            y[i] = to_odd((double)x[i] * t.c + (double)z[i] * (upper ? t.s : -t.s));
+            for (int i = 0; i < 4; ++i) {
+                const Turn64 t = table[4 * u + i];
+                const double p = x[2 * i], r = x[2 * i + 1];
+                x[2 * i] = to_odd(p * t.c - r * t.s);
+                x[2 * i + 1] = to_odd(r * t.c + p * t.s);
+            }
+        } else {
+            const bool upper = 8 * u >= pairs;
+            const int first = 8 * u - (upper ? pairs : 0);
+            float z[8];
+            widen<T>(*(const uint4 *)(row + 16 * u + (upper ? -2 : 2) * pairs), z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const Turn64 t = table[first + i];
+                x[i] = to_odd((double)x[i] * t.c + (double)z[i] * (upper ? t.s : -t.s));
+            }
         }
     }
 }
 
-template <class T, bool FOUR, bool NEIGHBOURS>
-__global__ __launch_bounds__(256) void k_kv_append_rotated(Append a) {
-    __shared__ Turn32 turns32[4][MPT_KV_MAX_DIM / 2];
-    __shared__ Turn64 turns64[FOUR ? 4 : 1][FOUR ? MPT_KV_MAX_DIM / 2 : 1];
+enum Role { kKeys, kValues, kQueries };              // rows that a chunk of 64 units belongs to
+
+// How the rows of a role are cut into units, in 16 bits.
+template <class T, bool NEIGHBOURS, int ROLE>
+struct Units {
+    const Append &a;
+    int pairs, units, all, chunks;
+    uint32_t mul;
+
+    __device__ explicit Units(const Append &a, bool any) : a(a) {
+        pairs = ROLE == kValues ? 0 : a.pairs;
+        units = ROLE == kValues ? a.dim / 8 : turn_units<NEIGHBOURS>(a.dim, a.pairs);
+        mul = ROLE == kValues ? a.copy_mul : a.turn_mul;
+        all = any ? (ROLE == kQueries ? a.heads : a.c.n_heads) * units : 0;
+        chunks = (all + 63) / 64;
+    }
+
+    // The pieces of unit y: lanes past the last read that one.
+    __device__ void load(int64_t token, int y, uint4 &one, uint4 &two) const {
+        y = min(y, all - 1);
+        const int h = divided(y, mul), u = y - h * units;
+        int first, second;
+        bool turns;
+        unit_at<NEIGHBOURS>(pairs, u, first, second, turns);
+        const char *row = ROLE == kKeys     ? a.k + 2 * (token * a.k_token + h * a.k_head)
+                          : ROLE == kValues ? a.v + 2 * (token * a.v_token + h * a.v_head)
+                                            : a.q + 2 * (token * a.q_token + h * a.q_head);
+        one = *(const uint4 *)(row + first);
+        if (ROLE != kValues && !NEIGHBOURS) two = *(const uint4 *)(row + second);
+    }
+
+    __device__ void put(int64_t token, int page, int slot, int y, uint4 one, uint4 two, const Turn32 *table) const {
+        const mpt_kv_cache &c = a.c;
+        const int h = divided(y, mul), u = y - h * units;
+        if (y >= all) return;
+        if (ROLE == kQueries) {
+            turn_unit<T, NEIGHBOURS>(pairs, one, two, a.q_out + 2 * (token * a.out_token + h * a.out_head), u, table);
+            return;
+        }
+        const int64_t *st = ROLE == kKeys ? c.k_stride : c.v_stride;
+        char *to = (char *)(ROLE == kKeys ? c.k : c.v) + 2 * (a.layer * st[0] + page * st[1] + slot * st[2] + h * st[3]);
+        if (ROLE == kKeys)
+            turn_unit<T, NEIGHBOURS>(pairs, one, two, to, u, table);
+        else
+            *(uint4 *)(to + 16 * u) = one;
+    }
+};
+
+constexpr int kRun4 = 4;                             // tokens of a wave, at most, in a cache of 4 bits
+
+// In a cache of 4 bits a lane takes 32 elements of a row, of any of the wave's
+// tokens: no two lanes need to agree on an E, and 16 bytes of codes go out at a time.
+template <class T, bool FOUR, int KEYS>
+__global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
+    constexpr bool NEIGHBOURS = KEYS == kNeighbours;
+    extern __shared__ char tables[];                 // of each wave
     const mpt_kv_cache &c = a.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int shift = 31 - __clz(c.page_size), units = turn_units<NEIGHBOURS>(a.dim, a.pairs);
-    const int pieces = c.n_heads * (a.dim / 8);
-    const int k_all = a.k ? FOUR ? pieces : c.n_heads * units : 0, q_all = a.q ? a.heads * units : 0;
-    const int kc = (k_all + 63) / 64, vc = a.k ? (pieces + 63) / 64 : 0, qc = (q_all + 63) / 64;
-    Turn32 *t32 = turns32[wave];
-    Turn64 *t64 = turns64[FOUR ? wave : 0];
-    const int64_t all = (int64_t)a.n_tokens * a.parts;
-    for (int64_t at = blockIdx.x * 4 + wave; at < all; at += gridDim.x * 4) {
-        const int token = uniform((int)(a.parts == 1 ? at : at / a.parts)), part = uniform((int)(at - (int64_t)token * a.parts));
-        // where the token stands and goes
-        int slot = -1, length = 0;
-        int64_t pos = 0;
-        const int i = a.n > 0 ? uniform(wave_find(a.q_off, a.n, token)) : -1;
-        bool known = false, write = false;
-        if (i >= 0 && i < a.n && slot_ok(c, a.seqs[i])) {
-            slot = a.seqs[i], length = c.length[slot];
-            pos = (int64_t)length - a.q_off[i + 1] + token;
-            known = true;
-            if (pos < 0 || pos >= length || (pos >> shift) >= c.max_pages) {
-                if (a.k && lane == 0 && part == 0) flag(c, MPT_KV_BAD_LENGTH);
-            } else {
-                write = a.k != nullptr;
-            }
-        } else if (lane == 0 && part == 0 && (a.k || !a.position)) {
-            flag(c, MPT_KV_BAD_SLOT);
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const Units<T, NEIGHBOURS, kKeys> keys(a, !FOUR && a.k);
+    const Units<T, NEIGHBOURS, kValues> values(a, !FOUR && a.k);
+    const Units<T, NEIGHBOURS, kQueries> queries(a, a.q);
+    const int of_run = FOUR ? a.run : 1;             // tokens whose angles are there at a time
+    Turn32 *t32 = (Turn32 *)(tables + (FOUR ? 4 * of_run * a.pairs * sizeof(Turn64) : 0)) + wave * of_run * a.pairs;
+    Turn64 *t64 = (Turn64 *)tables + wave * of_run * a.pairs;
+    const int64_t at = wave_number(), group = a.parts == 1 ? at : at / a.parts;
+    const int part = (int)(at - group * a.parts);
+    if (group * a.run >= a.n_tokens) return;
+    const int x0 = (int)(group * a.run), count = min(a.run, a.n_tokens - x0);
+    Place place = locate(c, a.n, a.seqs, a.q_off, nullptr, x0, count);
+    if (a.k) {
+        if (place.page >= 0 && c.ref[place.page] != 1) {
+            place.bad = c.ref[place.page] > 1 ? MPT_KV_SHARED : MPT_KV_BAD_PAGE;
+            place.page = -1;
         }
-        int page = 0;
-        if (write) {
-            page = c.table[(int64_t)slot * c.max_pages + (pos >> shift)];
-            if (!page_ok(c, page) || c.ref[page] != 1) {
-                if (lane == 0 && part == 0) flag(c, page_ok(c, page) && c.ref[page] > 1 ? MPT_KV_SHARED : MPT_KV_BAD_PAGE);
-                write = false;
+    } else {
+        place.bad = a.position || place.known ? 0 : place.bad;      // nothing is written
+    }
+    if (part == 0 && place.bad) flag(c, place.bad);
+    if (a.position && lane < count) place.pos = a.position[x0 + lane], place.known = true;
+    auto turn = [&](int x, Turn32 *to32, Turn64 *to64) {
+        const double pos = __builtin_amdgcn_readlane(place.pos, x);
+        for (int p = lane; p < a.pairs; p += 64) {
+            double s, co;
+            sincos(pos * (double)a.freq[p], &s, &co);
+            co *= a.factor, s *= a.factor;
+            if (FOUR) to64[p] = Turn64{co, s};
+            to32[p] = Turn32{(float)co, (float)s};
+        }
+    };
+    auto handed_out = [&]() {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    // all roles' chunks in turn over the parts
+    int before = 0;
+    auto first_of = [&](int chunks) {
+        const int x = a.parts == 1 ? 0 : (int)((uint32_t)(part + a.parts * 65536 - before) % (uint32_t)a.parts);
+        before += chunks;
+        return x;
+    };
+    if constexpr (FOUR) {
+        for (int x = 0; x < count; ++x) turn(x, t32 + x * a.pairs, t64 + x * a.pairs);
+        handed_out();
+        const int blocks = a.dim / 32, units = c.n_heads * blocks, all = a.k ? count * units : 0, chunks = (all + 63) / 64;
+        auto put = [&](auto role, int y) {
+            constexpr bool KEY = decltype(role)::value == kKeys;
+            const int x = (y >= units) + (y >= 2 * units) + (y >= 3 * units), z = y - x * units, h = divided(z, a.copy_mul), b = z - h * blocks;
+            const int page = __shfl(place.page, x);
+            const int64_t slot = __shfl(place.slot, x), token = x0 + x;
+            if (y >= all || page < 0) return;
+            const int64_t *st = KEY ? c.k_stride : c.v_stride, *es = KEY ? a.e.k_stride : a.e.v_stride;
+            float f[32];
+            if (KEY)
+                turn_block<T, KEYS>(a.pairs, a.k + 2 * (token * a.k_token + h * a.k_head), b, t64 + x * a.pairs, f);
+            else
+                turn_block<T, kWhole>(0, a.v + 2 * (token * a.v_token + h * a.v_head), b, nullptr, f);
+            int scale;
+            const uint4 codes = to_codes(f, a.e_min, a.e_max, scale);
+            *(uint4 *)((char *)(KEY ? c.k : c.v) + (a.layer * st[0] + page * st[1] + slot * st[2] + h * st[3]) + 16 * b) = codes;
+            *(uint8_t *)((KEY ? a.e.k : a.e.v) + (a.layer * es[0] + page * es[1] + slot * es[2] + h * es[3]) + b) = (uint8_t)scale;
+        };
+        for (int j = first_of(chunks); j < chunks; j += a.parts) put(std::integral_constant<int, kKeys>(), j * 64 + lane);
+        for (int j = first_of(chunks); j < chunks; j += a.parts) put(std::integral_constant<int, kValues>(), j * 64 + lane);
+        const int q0 = first_of(0);
+        for (int x = 0; x < count; ++x) {
+            if (!__builtin_amdgcn_readlane(place.known, x)) continue;
+            for (int j = q0; j < queries.chunks; j += 2 * a.parts) {
+                uint4 one[2], two[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) queries.load(x0 + x, (j + i * a.parts) * 64 + lane, one[i], two[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    queries.put(x0 + x, 0, 0, (j + i * a.parts) * 64 + lane, one[i], two[i], t32 + x * a.pairs);
             }
         }
-        const int64_t in_page = pos & (c.page_size - 1);
-        if (a.position) pos = a.position[token], known = true;
-        if (a.pairs && known) {
-            __builtin_amdgcn_wave_barrier();                 // the last token's are read
-            for (int p = lane; p < a.pairs; p += 64) {
-                double s, co;
-                sincos((double)pos * (double)a.freq[p], &s, &co);
-                co *= a.factor, s *= a.factor;
-                if (FOUR) t64[p] = Turn64{co, s};
-                t32[p] = Turn32{(float)co, (float)s};
+    } else {
+        const int k0 = first_of(keys.chunks), v0 = first_of(values.chunks), q0 = first_of(0);
+        for (int x = 0; x < count; ++x) {
+            const int64_t token = x0 + x;
+            const int page = __builtin_amdgcn_readlane(place.page, x), slot = __builtin_amdgcn_readlane(place.slot, x);
+            const bool known = __builtin_amdgcn_readlane(place.known, x);
+            uint4 k1, k2, q1[2], q2[2], none;
+            auto load_queries = [&](int j) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) queries.load(token, (j + i * a.parts) * 64 + lane, q1[i], q2[i]);
+            };
+            if (k0 < keys.chunks) keys.load(token, k0 * 64 + lane, k1, k2);
+            if (q0 < queries.chunks) load_queries(q0);
+            if (known) {
+                __builtin_amdgcn_wave_barrier();             // the last token's are read
+                turn(x, t32, nullptr);
+                handed_out();
             }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        }
-        for (int j = part; j < kc + vc + qc; j += a.parts) {
-            if (j >= kc + vc) {
-                const int x = (j - kc - vc) * 64 + lane, h = divided(x, a.turn_mul);
-                if (known && x < q_all)
-                    turn_row<T, NEIGHBOURS>(a, a.q + 2 * (token * a.q_token + h * a.q_head),
-                                            a.q_out + 2 * (token * a.out_token + h * a.out_head), x - h * units, t32);
-                continue;
-            }
-            if (!write) continue;
-            if constexpr (FOUR) {
-                const bool keys = j < kc;
-                const int x = (keys ? j : j - kc) * 64 + lane, h = divided(x, a.copy_mul), u = x - h * (a.dim / 8);
-                float y[8] = {};
-                if (x < pieces) {
-                    if (keys)
-                        turn_piece<T, NEIGHBOURS>(a, a.k + 2 * (token * a.k_token + h * a.k_head), u, t64, y);
-                    else
-                        widen<T>(*(const uint4 *)(a.v + 2 * (token * a.v_token + h * a.v_head) + 16 * u), y);
+            if (page >= 0) {
+                for (int j = k0; j < keys.chunks;) {
+                    keys.put(token, page, slot, j * 64 + lane, k1, k2, t32);
+                    if ((j += a.parts) < keys.chunks) keys.load(token, j * 64 + lane, k1, k2);
                 }
-                int scale;
-                const uint32_t codes = to_codes(y, a.e_min, a.e_max, scale);
-                if (x < pieces) {
-                    const int64_t *st = keys ? c.k_stride : c.v_stride, *es = keys ? a.e.k_stride : a.e.v_stride;
-                    char *to = (char *)(keys ? c.k : c.v) + a.layer * st[0] + page * st[1] + in_page * st[2] + h * st[3];
-                    char *e = (keys ? a.e.k : a.e.v) + a.layer * es[0] + page * es[1] + in_page * es[2] + h * es[3];
-                    *(uint32_t *)(to + 4 * u) = codes;
-                    if (u % 4 == 0) e[u / 4] = (char)scale;
+                for (int j = v0; j < values.chunks; j += 2 * a.parts) {
+                    uint4 v[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) values.load(token, (j + i * a.parts) * 64 + lane, v[i], none);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) values.put(token, page, slot, (j + i * a.parts) * 64 + lane, v[i], none, t32);
                 }
-            } else if (j < kc) {
-                const int x = j * 64 + lane, h = divided(x, a.turn_mul);
-                if (x < k_all)
-                    turn_row<T, NEIGHBOURS>(a, a.k + 2 * (token * a.k_token + h * a.k_head),
-                                            (char *)c.k + 2 * (a.layer * c.k_stride[0] + page * c.k_stride[1] +
-                                                               in_page * c.k_stride[2] + h * c.k_stride[3]),
-                                            x - h * units, t32);
-            } else {
-                const int x = (j - kc) * 64 + lane, h = divided(x, a.copy_mul), u = x - h * (a.dim / 8);
-                if (x < pieces)
-                    *(uint4 *)((char *)c.v + 2 * (a.layer * c.v_stride[0] + page * c.v_stride[1] + in_page * c.v_stride[2] +
-                                                  h * c.v_stride[3]) + 16 * u) =
-                        *(const uint4 *)(a.v + 2 * (token * a.v_token + h * a.v_head) + 16 * u);
             }
+            if (known)
+                for (int j = q0; j < queries.chunks;) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) queries.put(token, 0, 0, (j + i * a.parts) * 64 + lane, q1[i], q2[i], t32);
+                    if ((j += 2 * a.parts) < queries.chunks) load_queries(j);
+                }
         }
     }
 }
@@ -258,7 +409,7 @@ __global__ __launch_bounds__(256) void k_kv_append_rotated(Append a) {
 struct Read {
     mpt_kv_cache c;
     Scales e;
-    int layer, n, n_tokens, dim;
+    int layer, n, n_tokens, dim, run;
     const int32_t *seqs, *off, *first;
     char *k, *v;
     int64_t k_token, k_head, v_token, v_head;
@@ -283,51 +434,60 @@ __device__ inline uint4 from_codes(uint32_t codes, uint32_t scale) {
                  two(std::integral_constant<int, 2>()), two(std::integral_constant<int, 3>())};
 }
 
-// One wave per token, a piece of 8 elements per lane.
+// A wave per run of tokens, a piece of 8 elements per lane.
 template <class T, bool FOUR>
 __global__ __launch_bounds__(256) void k_kv_read(Read a) {
     const mpt_kv_cache &c = a.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, shift = 31 - __clz(c.page_size);
+    const int lane = threadIdx.x & 63;
     const int units = a.dim / 8, pieces = c.n_heads * units;
-    for (int64_t at = blockIdx.x * 4 + wave; at < a.n_tokens; at += gridDim.x * 4) {
-        const int token = uniform((int)at), i = uniform(wave_find(a.off, a.n, token));
-        if (i < 0 || i >= a.n) {
-            if (lane == 0) flag(c, MPT_KV_BAD_SLOT);
-            continue;
-        }
-        int page = -1;
-        int64_t pos = 0;
-        uint32_t bad = 0;
-        if (slot_ok(c, a.seqs[i])) {
-            const int slot = a.seqs[i], length = c.length[slot];
-            pos = a.first ? (int64_t)a.first[i] + token - a.off[i] : (int64_t)length - a.off[i + 1] + token;
-            if (pos < 0 || pos >= length || (pos >> shift) >= c.max_pages) {
-                bad = MPT_KV_BAD_LENGTH;
-            } else {
-                page = c.table[(int64_t)slot * c.max_pages + (pos >> shift)];
-                if (!page_ok(c, page)) page = -1, bad = MPT_KV_BAD_PAGE;
-            }
-        } else {
-            bad = MPT_KV_BAD_SLOT;
-        }
-        if (bad && lane == 0) flag(c, bad);
-        const int64_t in_page = pos & (c.page_size - 1);
-        for (int x = lane; x < pieces; x += 64) {
-            const int h = divided(x, a.copy_mul), u = x - h * units;
-            auto one = [&](const void *base, const int64_t *st, const char *e, const int64_t *es) -> uint4 {
-                if (page < 0) return uint4{0, 0, 0, 0};
-                const int64_t row = a.layer * st[0] + page * st[1] + in_page * st[2] + h * st[3];
+    const int64_t group = wave_number();
+    if (group * a.run >= a.n_tokens) return;
+    const int x0 = (int)(group * a.run), count = min(a.run, a.n_tokens - x0);
+    const Place place = locate(c, a.n, a.seqs, a.off, a.first, x0, count);
+    if (place.bad) flag(c, place.bad);
+    // tokens of no entry keep their rows: off[n] on, or before off[0]
+    const int begin = a.off[0], end = a.off[a.n];
+    for (int z0 = 0; z0 < pieces; z0 += 64) {
+        const int z = z0 + lane, h = divided(z, a.copy_mul), u = z - h * units;
+        const int64_t k_from = h * c.k_stride[3] * (FOUR ? 1 : 2) + (FOUR ? 4 : 16) * u;
+        const int64_t v_from = h * c.v_stride[3] * (FOUR ? 1 : 2) + (FOUR ? 4 : 16) * u;
+        const int64_t ke_from = FOUR ? h * a.e.k_stride[3] + u / 4 : 0, ve_from = FOUR ? h * a.e.v_stride[3] + u / 4 : 0;
+        const int64_t k_to = 2 * h * a.k_head + 16 * u, v_to = 2 * h * a.v_head + 16 * u;
+        if (z >= pieces) break;
+        constexpr int U = 4;
+        for (int x = 0; x < count; x += U) {
+            uint4 k[U], v[U];
+            uint32_t kc[U], vc[U], ks[U], vs[U];
+#pragma unroll
+            for (int y = 0; y < U; ++y) {
+                const int page = __builtin_amdgcn_readlane(place.page, min(x + y, count - 1));
+                const int64_t slot = __builtin_amdgcn_readlane(place.slot, min(x + y, count - 1));
+                k[y] = v[y] = uint4{0, 0, 0, 0};
+                kc[y] = vc[y] = 0, ks[y] = vs[y] = 0;
+                if (page < 0) continue;
+                const int64_t k_row = a.layer * c.k_stride[0] + page * c.k_stride[1] + slot * c.k_stride[2];
+                const int64_t v_row = a.layer * c.v_stride[0] + page * c.v_stride[1] + slot * c.v_stride[2];
                 if constexpr (FOUR) {
-                    const uint8_t scale = *(const uint8_t *)(e + a.layer * es[0] + page * es[1] + in_page * es[2] + h * es[3] + u / 4);
-                    return from_codes<T>(*(const uint32_t *)((const char *)base + row + 4 * u), scale);
+                    const int64_t *ek = a.e.k_stride, *ev = a.e.v_stride;
+                    if (a.k) kc[y] = *(const uint32_t *)((const char *)c.k + k_row + k_from);
+                    if (a.k) ks[y] = *(const uint8_t *)(a.e.k + (a.layer * ek[0] + page * ek[1] + slot * ek[2]) + ke_from);
+                    if (a.v) vc[y] = *(const uint32_t *)((const char *)c.v + v_row + v_from);
+                    if (a.v) vs[y] = *(const uint8_t *)(a.e.v + (a.layer * ev[0] + page * ev[1] + slot * ev[2]) + ve_from);
+                } else {
+                    if (a.k) k[y] = *(const uint4 *)((const char *)c.k + 2 * k_row + k_from);
+                    if (a.v) v[y] = *(const uint4 *)((const char *)c.v + 2 * v_row + v_from);
                 }
-                return *(const uint4 *)((const char *)base + 2 * row + 16 * u);
-            };
-            uint4 k, v;
-            if (a.k) k = one(c.k, c.k_stride, a.e.k, a.e.k_stride);
-            if (a.v) v = one(c.v, c.v_stride, a.e.v, a.e.v_stride);
-            if (a.k) *(uint4 *)(a.k + 2 * (token * a.k_token + h * a.k_head) + 16 * u) = k;
-            if (a.v) *(uint4 *)(a.v + 2 * (token * a.v_token + h * a.v_head) + 16 * u) = v;
+            }
+#pragma unroll
+            for (int y = 0; y < U; ++y) {
+                const int64_t token = x0 + x + y;
+                if (x + y >= count || token < begin || token >= end) continue;
+                if (FOUR) k[y] = from_codes<T>(kc[y], ks[y]), v[y] = from_codes<T>(vc[y], vs[y]);
+                typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+                // past the caches: 983 MB and 261 MB of codes 241 us, 253 through them
+                if (a.k) __builtin_nontemporal_store(__builtin_bit_cast(u4, k[y]), (u4 *)(a.k + 2 * token * a.k_token + k_to));
+                if (a.v) __builtin_nontemporal_store(__builtin_bit_cast(u4, v[y]), (u4 *)(a.v + 2 * token * a.v_token + v_to));
+            }
         }
     }
 }
@@ -336,22 +496,36 @@ __global__ __launch_bounds__(256) void k_kv_read(Read a) {
 
 static uint32_t reciprocal(int units) { return units == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + units - 1) / units); }
 
+// Tokens of a wave of a launch over n_tokens, at most `most`: what makes `waves`.
+static int run_of(int n_tokens, int waves, int most) {
+    const int64_t run = ((int64_t)n_tokens + waves - 1) / waves;
+    return run < 1 ? 1 : run < most ? (int)run : most;
+}
+
 static void launch_append(Append &a, bool neighbours, hipStream_t s) {
     const mpt_kv_cache &c = a.c;
+    const bool mx4 = is_mx4(c), bf16 = value_type(c) == MPT_KV_BF16;
     a.dim = c.head_dim;
-    a.copy_mul = reciprocal(a.dim / 8);
     a.turn_mul = reciprocal(neighbours ? turn_units<true>(a.dim, a.pairs) : turn_units<false>(a.dim, a.pairs));
-    const bool bf16 = value_type(c) == MPT_KV_BF16;
+    a.copy_mul = reciprocal(mx4 ? a.dim / 32 : a.dim / 8);
     a.e_min = bf16 ? -125 : -23, a.e_max = bf16 ? 125 : 13;
-    a.parts = 1;
+    const int lanes = c.n_heads * (a.dim / 32);          // of a token's keys, in 4 bits
+    a.run = mx4 ? run_of(a.n_tokens, 4096, lanes >= 64 ? 1 : lanes >= 32 ? 2 : kRun4) : run_of(a.n_tokens, 16384, 16);
+    a.parts = a.n_tokens <= 1024 ? 4 : 1;
     using Kernel = void (*)(Append);
-    static constexpr Kernel kernels[2][2][2] = {
-        {{k_kv_append_rotated<__bf16, false, false>, k_kv_append_rotated<__bf16, false, true>},
-         {k_kv_append_rotated<__bf16, true, false>, k_kv_append_rotated<__bf16, true, true>}},
-        {{k_kv_append_rotated<_Float16, false, false>, k_kv_append_rotated<_Float16, false, true>},
-         {k_kv_append_rotated<_Float16, true, false>, k_kv_append_rotated<_Float16, true, true>}}};
+    static constexpr Kernel wide[2][2] = {
+        {k_kv_append_rotated<__bf16, false, kApart>, k_kv_append_rotated<__bf16, false, kNeighbours>},
+        {k_kv_append_rotated<_Float16, false, kApart>, k_kv_append_rotated<_Float16, false, kNeighbours>}};
+    static constexpr Kernel four[2][3] = {
+        {k_kv_append_rotated<__bf16, true, kWhole>, k_kv_append_rotated<__bf16, true, kNeighbours>,
+         k_kv_append_rotated<__bf16, true, kApart>},
+        {k_kv_append_rotated<_Float16, true, kWhole>, k_kv_append_rotated<_Float16, true, kNeighbours>,
+         k_kv_append_rotated<_Float16, true, kApart>}};
+    const Kernel kernel = mx4 ? four[!bf16][a.pairs == 0 ? kWhole : neighbours ? kNeighbours : kApart] : wide[!bf16][neighbours];
+    const size_t lds = 4 * (size_t)a.pairs * (mx4 ? a.run * (sizeof(Turn32) + sizeof(Turn64)) : sizeof(Turn32));
+    const int64_t waves = ((int64_t)a.n_tokens + a.run - 1) / a.run * a.parts;
     mptlib::LaunchScope scope("k_kv_append_rotated", (double)a.n_tokens, s);
-    kernels[bf16 ? 0 : 1][is_mx4(c)][neighbours]<<<mptlib::grid_for((int64_t)a.n_tokens * a.parts, 4, 4096), 256, 0, s>>>(a);
+    kernel<<<grid_of(waves), 256, lds, s>>>(a);
 }
 
 int check_append(const mpt_kv_cache *c, int layer, int n, int64_t n_tokens) {
@@ -434,13 +608,15 @@ extern "C" int mpt_kv_read(const mpt_kv_cache *cache, int layer, int n, const in
         a.seqs = seqs, a.off = off, a.first = first, a.k = (char *)k_out, a.v = (char *)v_out;
         a.k_token = k_token_stride, a.k_head = k_head_stride, a.v_token = v_token_stride, a.v_head = v_head_stride;
         a.copy_mul = reciprocal(a.dim / 8);
+        a.run = run_of(a.n_tokens, 8192, 4);
         using Kernel = void (*)(Read);
         static constexpr Kernel kernels[2][2] = {{k_kv_read<__bf16, false>, k_kv_read<__bf16, true>},
                                                  {k_kv_read<_Float16, false>, k_kv_read<_Float16, true>}};
         hipStream_t s = (hipStream_t)stream;
         {
             mptlib::LaunchScope scope("k_kv_read", (double)n_tokens, s);
-            kernels[value_type(*cache)][is_mx4(*cache)]<<<mptlib::grid_for(n_tokens, 4, 4096), 256, 0, s>>>(a);
+            const int64_t waves = ((int64_t)a.n_tokens + a.run - 1) / a.run;
+            kernels[value_type(*cache)][is_mx4(*cache)]<<<grid_of(waves), 256, 0, s>>>(a);
         }
         MPT_HIP_TRY(hipGetLastError());
         return MPT_OK;

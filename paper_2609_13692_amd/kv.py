@@ -16,11 +16,12 @@ import struct
 
 import torch
 
-from .mpt import KvDescriptor, KvDescriptorMx4, KvRotation, MptError, _check, load
+from .mpt import KvDescriptor, KvDescriptorMx4, MptError, _check, load
 
 BF16, F16, F32, MX4 = 0, 1, 2, 3                # MX4: added to a 16-bit type
 _KIND = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 MAX_PARTS = 16
+_ROTATION = struct.Struct("PPiif").pack         # mpt_kv_rotation
 _POINTERS = [struct.Struct(f"{n}P").pack for n in range(MAX_PARTS + 1)]      # host arrays of device pointers
 STATUS_BITS = {1: "slot", 2: "length", 4: "page", 8: "duplicate", 16: "not empty", 32: "no pages", 64: "shared page"}
 
@@ -269,30 +270,32 @@ class KvCache:
             raise ValueError(f"freq must be a contiguous float32 vector on GPU {index}")
         if (k_new is None) != (v_new is None) or (k_new is None and q is None):
             raise ValueError("needs k_new and v_new, or q, or all three")
-        if q is None and q_out is not None:
-            raise ValueError("q_out without q")
         tokens = (q if k_new is None else k_new).shape[0]
-        for name, t in (("v_new", v_new), ("q", q), ("q_out", q_out)):
-            if t is not None and t.shape[0] != tokens:
-                raise ValueError(f"{name} must have one row per token")
-        n = 0 if seqs is None else seqs.numel()
-        if seqs is None and (k_new is not None or positions is None or q_off is not None):
-            raise ValueError("needs q_off and seqs, but for queries alone with positions")
-        heads, rows = 1, [None, 0, 0]
+        k = v = q_in = out = (None, 0, 0)
+        heads = 1
+        if k_new is not None:
+            if v_new.shape[0] != tokens:
+                raise ValueError("v_new must have one row per token")
+            k, v = self._rows(k_new, self.n_heads, "k_new", self.dtype), self._rows(v_new, self.n_heads, "v_new", self.dtype)
         if q is not None:
             heads = q.shape[1]
-            rows = self._rows(q, heads, "q", self.dtype)
+            q_in = self._rows(q, heads, "q", self.dtype)
             if q_out is None:
                 q_out = _new(q.shape, self.dtype, self.device, under)
-        r = KvRotation()
-        r.freq, r.dim, r.interleaved, r.factor = freq.data_ptr(), 2 * freq.numel(), bool(interleaved), factor
-        r.position = None if positions is None else _list(positions, tokens, "positions", index)
-        rc = _run(index, self._lib.mpt_kv_append_rotated, self._p, layer, n, *((None, None) if seqs is None else (
-                  _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index))), tokens,
-                  *((None, 0, 0) if k_new is None else self._rows(k_new, self.n_heads, "k_new", self.dtype)),
-                  *((None, 0, 0) if v_new is None else self._rows(v_new, self.n_heads, "v_new", self.dtype)),
-                  ctypes.addressof(r), heads, *rows,
-                  *((None, 0, 0) if q is None else self._rows(q_out, heads, "q_out", self.dtype)), at)
+            if q.shape[0] != tokens or q_out.shape[0] != tokens:
+                raise ValueError("q and q_out must have one row per token")
+            out = q_in if q_out is q else self._rows(q_out, heads, "q_out", self.dtype)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        n, lists = 0, (None, None)
+        if seqs is not None:
+            n = seqs.numel()
+            lists = _list(seqs, n, "seqs", index), _list(q_off, n + 1, "q_off", index)
+        elif k_new is not None or positions is None or q_off is not None:
+            raise ValueError("needs q_off and seqs, but for queries alone with positions")
+        rotation = _ROTATION(freq.data_ptr(), 0 if positions is None else _list(positions, tokens, "positions", index),
+                             2 * freq.numel(), bool(interleaved), factor)
+        rc = _run(index, self._lib.mpt_kv_append_rotated, self._p, layer, n, *lists, tokens, *k, *v, rotation, heads, *q_in, *out, at)
         if rc:
             _check(rc, "mpt_kv_append_rotated")
         return q_out
