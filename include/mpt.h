@@ -552,8 +552,8 @@ typedef struct mpt_kv_cache {
  * max |x| <= 7 * 2^e in -125 .. 125 (bfloat16) or -23 .. 13 (float16), where every
  * value is finite and exact in the 16-bit type, and the codes nearest to x / 2^e:
  * of two as near the even one, 6 for all that is larger. With a NaN or an
- * infinity among the 32, E = 255. What a cache holds in other bytes E is read as
- * far as the 16-bit type holds it.
+ * infinity among the 32, E = 255. Calls that read take a byte E above that range
+ * for 255; below it, values are read as far as the 16-bit type holds them.
  */
 typedef struct mpt_kv_cache_mx4 {
     mpt_kv_cache c;

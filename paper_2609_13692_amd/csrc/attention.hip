@@ -41,7 +41,7 @@ static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_hea
     const int dim = pad_dim(c.head_dim);
     const bool own_cu = dim == 128 && (int64_t)n * c.n_heads <= 256;
     if (rows <= (dim == 128 ? 32 : 16)) {
-        if (is_mx4(c)) return {0, dim == 256 ? 256 : dim == 128 ? 768 : 1024, 16};
+        if (is_mx4(c)) return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
         return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
     }
     if ((rows <= 128 && !own_cu) || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
@@ -117,12 +117,12 @@ extern "C" int mpt_kv_attention(const mpt_kv_cache *cache, int layer, int n, con
             return fail(MPT_E_INVALID, "scale = %g, softcap = %g", scale, softcap);
         a.cap = softcap * log2e;
         const bool mx4 = is_mx4(*cache);
-        const int piece = mx4 ? 16 : 8, size = mx4 ? 1 : 2;        // strides of 16 bytes; bytes of what strides count
+        const int piece = mx4 ? 1 : 8, size = mx4 ? 1 : 2;         // strides go in bytes, or 16 of them; bytes of what they count
         const Scales e = scales_of(*cache);
         for (int i = 1; i < 3; ++i) {
             const int64_t times = i == 2 ? cache->page_size : 1;
             if (cache->k_stride[i] / piece * times > UINT32_MAX || cache->v_stride[i] / piece * times > UINT32_MAX)
-                return fail(MPT_E_INVALID, "cache: a page, or the stride of pages, of 64 GiB or more");
+                return fail(MPT_E_INVALID, "cache: a page, or the stride of pages, of %d GiB or more", mx4 ? 4 : 64);
             if (e.k_stride[i] * times > UINT32_MAX || e.v_stride[i] * times > UINT32_MAX)
                 return fail(MPT_E_INVALID, "cache: a page's scales, or the stride of pages, of 4 GiB or more");
         }

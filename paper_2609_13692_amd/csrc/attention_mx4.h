@@ -6,19 +6,22 @@
 
 namespace mptkv {
 
-// In 4 bits k_page and the like count 16-byte pieces of codes, k_head bytes.
+// Strides of pages and slots are in bytes here, those of Attn too.
 struct Attn4 : Attn {
     const char *ke, *ve;                              // the layer's bytes E
-    int64_t ke_head, ve_head;                         // all in bytes
+    int64_t ke_head, ve_head;
     uint32_t ke_page, ke_slot, ve_page, ve_slot;
 };
 
-inline __device__ uint64_t scale_at(uint32_t page, uint32_t slot, uint32_t page_stride, uint32_t slot_stride) {
-    return (uint64_t)page * page_stride + (uint64_t)slot * slot_stride;
-}
+// x at index i of so many bytes: one instruction.
+inline __device__ const char *at(const char *x, uint32_t i, uint32_t bytes) { return x + (uint64_t)i * bytes; }
+
+// The largest E that appends write; all above count as 255, which is NaN.
+template <class T>
+constexpr uint32_t kMaxScale = __is_same(T, __bf16) ? 127 + 125 : 127 + 13;
 
 // What a byte E multiplies codes by, as the conversions take it: the exponent
-// of a 32-bit number. E = 255 has no such number; who uses it looks for it.
+// of a 32-bit number.
 inline __device__ float unit_of(uint32_t scale) { return __builtin_bit_cast(float, scale << 23); }
 
 // Eight codes as eight elements of the 16-bit type, exactly.
@@ -46,7 +49,7 @@ __device__ inline s16x8 nans() {
     return s16x8{n, n, n, n, n, n, n, n};
 }
 
-// NaN in values (blocks with E = 255; there are no infinities). Products take
+// NaN in values (there are no infinities). Products take
 // zeros in their place, for under the weight 0 of a row that does not see the
 // token they would spread, and a tile that has met one ends here: the E of the
 // values of tokens t0 .. t1 - 1 are looked through once more, and the sums of the
@@ -62,8 +65,8 @@ __device__ inline void nan_values(const Attn4 &a, const int32_t *table, int shif
         const int t = base + lane, page = t < t1 ? table[t >> shift] : -1;
         uint32_t odd = 0;
         if ((unsigned)page < (unsigned)a.c.n_pages) {
-            const uint8_t *e = (const uint8_t *)scales + scale_at(page, t & (a.c.page_size - 1), a.ve_page, a.ve_slot);
-            for (int b = 0; b < blocks; ++b) odd |= (uint32_t)(e[b] == 255) << b;
+            const uint8_t *e = (const uint8_t *)at(at(scales, page, a.ve_page), t & (a.c.page_size - 1), a.ve_slot);
+            for (int b = 0; b < blocks; ++b) odd |= (uint32_t)(e[b] > kMaxScale<T>) << b;
         }
 #pragma unroll 1
         for (uint64_t todo = __ballot(odd != 0); todo; todo &= todo - 1) {

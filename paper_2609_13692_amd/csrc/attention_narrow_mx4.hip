@@ -2,14 +2,34 @@
 // tiles of 16 rows, the four waves of a workgroup 32 tokens each of a step of 128,
 // as over 16 bits.
 //
-// Codes go to LDS as they come, keys as codes: a lane reads back a quarter of a
-// token's row, which is one E (heads of 128), as the operand of S' = K Q', whose
-// dimensions may come in any order if the queries agree on it. Values become 16-bit
-// rows on their way into LDS, where they are read by columns.
+// Codes of keys go to LDS as they come: a lane reads back a quarter of a token's
+// row, which is one E (heads of 128), as the operand of S' = K Q', whose dimensions
+// may come in any order if the queries agree on it. Values become 16-bit rows on
+// their way into LDS, where they are read by columns. What a load brings costs the
+// same in the address units whether its lanes take one byte or 16, so the bytes E of
+// a step's keys and values are one load of a row a lane, and its page ids another;
+// lanes ask each other for them.
+//
+// What bounds it is a step's own instructions and the LDS it fills (8 KiB of 16-bit
+// values for 2 KiB of codes), not memory: with three workgroups to a CU instead of two
+// it is no faster, and with registers put into memory to make room for them slower
+// (64 contexts of 700 to 9000, 32 heads on 8 of 128: 79 us, 88 with 5 of them in
+// memory), and so with steps loaded two ahead instead of one (84).
 
 #include "attention_mx4.h"
 
+#include <type_traits>
+
+#define INLINE __attribute__((always_inline))
+
 namespace mptkv {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <class V>
+__device__ inline void to_lds(uint32_t at, V x) {
+    *(__attribute__((address_space(3))) V *)(uintptr_t)at = x;
+}
 
 template <int DP>
 struct Narrow4 {
@@ -19,19 +39,21 @@ struct Narrow4 {
     static constexpr int E = DP == 256 ? 2 : 1;                        // bytes E of a quarter of a row
     static constexpr int kKeys = 32 * CODES, kValues = 32 * ROW;       // of a wave
 
-    // 16 tokens' pieces fall on different banks.
-    __device__ static int k_swizzle(int t) { return DP == 64 ? (t >> 3) & 1 : DP == 128 ? (t >> 2) & 3 : (t >> 1) & 7; }
-    // Eight tokens' 32 bytes fall on different banks, and so do the first (second,
-    // ...) quarters of four tokens' pieces, which are written at a time.
-    __device__ static int v_swizzle(int t) {
-        return DP == 64 ? 2 * ((t >> 1) & 3) + ((t >> 2) & 1) : 2 * (t & 7) + ((t >> 1) & 1);
-    }
+    static constexpr int EW = DP == 256 ? 2 : 1;                       // words of E a row
+
+    // Where the 16-byte pieces of a token's row of codes lie: those that eight lanes
+    // read at a time (a quarter of eight tokens each) on different banks.
+    __device__ static int k_swizzle(int t) { return DP == 64 ? (t >> 2) & 1 : DP == 128 ? (t >> 1) & 3 : t & 7; }
+    // And of a row of values: those that eight lanes write at a time (the same
+    // quarter of eight pieces) and that 16 read (32 bytes of four tokens each).
+    __host__ __device__ static constexpr int v_fold(int u) { return DP == 64 ? u : DP == 128 ? u ^ ((u >> 3) & 1) : u ^ ((u >> 3) & 3); }
+    __device__ static int v_swizzle(int t) { return DP == 64 ? 2 * (t & 3) + ((t >> 1) & 1) : 2 * (t & 7); }
 };
 
 template <class T, int DP, bool CAP, bool PAD>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 3 : 4) void k_kv_narrow_mx4(Attn4 a) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void k_kv_narrow_mx4(Attn4 a) {
     using N = Narrow4<DP>;
-    constexpr int M = N::M, BN = N::BN, C = N::C, KK = N::KK, DT = N::DT, ROW = N::ROW, CP = N::CP, L = N::L, E = N::E;
+    constexpr int M = N::M, BN = N::BN, C = N::C, KK = N::KK, DT = N::DT, ROW = N::ROW, CP = N::CP, L = N::L, E = N::E, EW = N::EW;
     __shared__ Entries ent;
     __shared__ __attribute__((aligned(1024))) char tiles[4 * (N::kKeys + N::kValues)];
     __shared__ float stat[4][2][16];
@@ -40,6 +62,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 3 : 4) void k_kv_n
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
     const int shift = 31 - __clz(c.page_size), pieces = a.units / 4;
     char *vw = tiles + wave * N::kValues, *kw = tiles + 4 * N::kValues + wave * N::kKeys;
+    // Where a lane writes and reads: swizzles are the same 8 tokens on, so all other
+    // places are these with bits turned over, and constants from there.
+    const int put_t = lane / CP, put_p = lane & (CP - 1), own_row = lane >> 2;   // own_row: 4 quad + col / 4
+    const uint32_t k_put = lds_address(kw) + put_t * N::CODES + ((put_p ^ N::k_swizzle(put_t)) << 4);
+    const uint32_t v_put = lds_address(vw) + put_t * ROW + ((N::v_fold(4 * put_p) ^ N::v_swizzle(put_t)) << 4);
+    const uint32_t k_get = lds_address(kw) + col * N::CODES +
+                           (DP == 64 ? ((quad / 2 ^ N::k_swizzle(col)) << 4) + (quad & 1) * 8 : (E * quad ^ N::k_swizzle(col)) << 4);
+    const uint32_t v_get = lds_address(vw) + own_row * ROW + (((lane & 3) / 2 ^ N::v_swizzle(own_row)) << 4) + (lane & 1) * 8;
+    bool lost = false;                         // a page id outside the pool
 
     Walk<M, BN, C> walk;
     if (!walk.begin(a, ent, 1)) return;
@@ -81,122 +112,159 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 3 : 4) void k_kv_n
         float m = -INFINITY, l = 0;
         bool met = false;                      // a NaN that was taken out of a product
 
-        // lane t < 32 knows the page of token t of the wave's part of a step,
-        // looked at a step later
-        auto find_page = [&](int step) {
-            const int t = step * BN + wave * 32 + (lane & 31);
-            return t >= range.lo && t < range.hi ? table[t >> shift] : -1;
-        };
-        const char *kh = a.k + head * a.k_head, *vh = a.v + head * a.v_head;
-        const char *keh = a.ke + head * a.ke_head, *veh = a.ve + head * a.ve_head;
+        // Tokens of a step that the tile does not reach are read as others of it
+        // (their scores are masked, and a weight of 0 times a finite value is 0),
+        // and so are pieces past the row's end (their queries are 0). A page id
+        // outside the pool becomes the last page, and is reported.
+        // A step's tokens are 32 slots of a page, or pages are of the step: a lane's
+        // places in them are the same for all steps but for what is uniform.
+        constexpr int T16 = 64 / CP;                               // tokens of a load: 8, 16 or 32
+        const int piece = min(put_p, pieces - 1);
+        const uint32_t own_slot = put_t & (c.page_size - 1);
+        const char *kx = at(a.k + head * a.k_head + 16 * piece, own_slot, a.k_slot), *vx = at(a.v + head * a.v_head + 16 * piece, own_slot, a.v_slot);
+        // Bytes E: of the step's 32 tokens, keys' in the lower half of the wave, values' in
+        // the upper, a row a lane.
+        const uint32_t e_slot = (lane & 31) & (c.page_size - 1);
+        const char *ex = lane < 32 ? at(a.ke + head * a.ke_head, e_slot, a.ke_slot) : at(a.ve + head * a.ve_head, e_slot, a.ve_slot);
+        const uint32_t e_page = lane < 32 ? a.ke_page : a.ve_page, e_stride = lane < 32 ? a.ke_slot : a.ve_slot;
+        // The next step is on its way while one is worked on, and the page ids of the one
+        // after it: loads arrive in order, so ids have to be asked for before the codes
+        // that are waited for when they are used. Lane l and l + 32 have the page of token
+        // l of the wave's 32. Every load costs the address units the same whether its
+        // lanes take one byte or 16.
         u32x4 kr[L], vr[L];
-        uint8_t ks[2][E], vs[L];
-        auto load = [&](int step, int pages) __attribute__((always_inline)) {
-            const int t0 = step * BN + wave * 32, ln = renewed(lane), piece = ln & (CP - 1);
-            if ((unsigned)pages >= (unsigned)c.n_pages) {
-                if (t0 + (ln & 31) >= range.lo && t0 + (ln & 31) < range.hi) flag(c, MPT_KV_BAD_PAGE);
-                pages = -1;
-            }
+        uint32_t er[EW];
+        uint8_t eb[PAD ? CP : 1];
+        int ids;
+        auto find_pages = [&](int step) INLINE {
+            const int t = step * BN + wave * 32 + (lane & 31);
+            return table[max(range.lo, min(range.hi - 1, t)) >> shift];
+        };
+        struct Pages { uint32_t of[L], e; };
+        auto pages_of = [&](int ids) INLINE {
+            const uint32_t page = min((uint32_t)ids, (uint32_t)c.n_pages - 1);
+            lost |= page != (uint32_t)ids;
+            Pages p;
+#pragma unroll
+            for (int i = 0; i < L; ++i) p.of[i] = __shfl((int)page, i * T16 + put_t);
+            p.e = page;
+            return p;
+        };
+        auto load = [&](const Pages &p, int step) INLINE {
+            const uint32_t slot0 = (uint32_t)(step * BN + wave * 32) & (c.page_size - 1);
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                const int t = i * (64 / CP) + ln / CP, page = __shfl(pages, t);
-                const uint32_t slot = (t0 + t) & (c.page_size - 1);
-                const bool there = page >= 0 && (!PAD || piece < pieces);
-                kr[i] = mptkv::load<u32x4>(or_zeros(there, kh + 16 * piece + row_at(page, slot, a.k_page, a.k_slot)));
-                vr[i] = mptkv::load<u32x4>(or_zeros(there, vh + 16 * piece + row_at(page, slot, a.v_page, a.v_slot)));
-                vs[i] = mptkv::load<uint8_t>(or_zeros(there, veh + piece + scale_at(page, slot, a.ve_page, a.ve_slot)));
+                const uint64_t slot = slot0 + (i * T16 & (c.page_size - 1));
+                kr[i] = mptkv::load<u32x4>(at(kx, p.of[i], a.k_page) + slot * a.k_slot);
+                vr[i] = mptkv::load<u32x4>(at(vx, p.of[i], a.v_page) + slot * a.v_slot);
             }
+            const char *e = at(at(ex, p.e, e_page), slot0, e_stride);
+            if constexpr (PAD) {
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-                const int t = mt * 16 + (ln & 15), page = __shfl(pages, t);
-                const uint32_t slot = (t0 + t) & (c.page_size - 1);
-#pragma unroll
-                for (int x = 0; x < E; ++x) {
-                    const int block = DP == 64 ? (ln >> 4) / 2 : (ln >> 4) * E + x;
-                    const bool there = page >= 0 && (!PAD || block < pieces);
-                    ks[mt][x] = mptkv::load<uint8_t>(or_zeros(there, keh + block + scale_at(page, slot, a.ke_page, a.ke_slot)));
-                }
+                for (int x = 0; x < CP; ++x) eb[x] = mptkv::load<uint8_t>(e + min(x, pieces - 1));
+            } else if constexpr (DP == 64) {
+                er[0] = mptkv::load<uint16_t>(e);
+            } else if constexpr (DP == 128) {
+                er[0] = mptkv::load<uint32_t>(e);
+            } else {
+                const u32x2 x = mptkv::load<u32x2>(e);
+                er[0] = x[0], er[1] = x[1];
             }
         };
-
-        int pages = find_page(first);
-        load(first, pages);
-        pages = find_page(first + 1);
-        for (int step = first; step < last; ++step) {
-            const int t0 = step * BN + wave * 32, ln = renewed(lane);
-            float ku[2][E];
+        auto one_step = [&](int step) INLINE {
+            const int t0 = step * BN + wave * 32;
+            if constexpr (PAD) {
+#pragma unroll
+                for (int x = 0; x < EW; ++x) er[x] = 0;
+#pragma unroll
+                for (int x = 0; x < CP; ++x) er[x / 4] |= (uint32_t)eb[x] << 8 * (x % 4);
+            }
+            // E from the lanes that have them: of block b of the row that lane `from` holds
+            auto scale_of = [&](int from, int b) INLINE -> uint32_t {
+                uint32_t x = __shfl((int)er[0], from);
+                if constexpr (EW == 2) {
+                    const uint32_t y = __shfl((int)er[1], from);
+                    x = b >= 4 ? y : x;
+                }
+                return __builtin_amdgcn_ubfe(x, 8 * (b & 3), 8);
+            };
+            uint32_t vs[L];
             bool k_odd = false, v_odd = false;
+#pragma unroll
+            for (int i = 0; i < L; ++i) vs[i] = scale_of(32 + i * T16 + put_t, piece), v_odd |= vs[i] > kMaxScale<T>;
+            float ku[2][E];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                for (int x = 0; x < E; ++x) ku[mt][x] = unit_of(ks[mt][x]), k_odd |= ks[mt][x] == 255;
+                for (int x = 0; x < E; ++x) {
+                    const uint32_t y = scale_of(mt * 16 + col, DP == 64 ? quad / 2 : quad * E + x);
+                    k_odd |= y > kMaxScale<T>;
+                    ku[mt][x] = unit_of(y);
+                }
+            if (__builtin_expect(__any(v_odd), 0)) {               // NaN: zeros (nan_values)
+                met = true;
+#pragma unroll
+                for (int i = 0; i < L; ++i)
+                    if (vs[i] > kMaxScale<T>) vr[i] = u32x4{0, 0, 0, 0}, vs[i] = 0;
+            }
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                const int t = i * (64 / CP) + ln / CP, piece = ln & (CP - 1);
-                *(u32x4 *)(kw + t * N::CODES + ((piece ^ N::k_swizzle(t)) << 4)) = kr[i];
-                const bool odd = vs[i] == 255;
-                v_odd |= odd;
+                to_lds(k_put + i * T16 * N::CODES, kr[i]);
                 const float unit = unit_of(vs[i]);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t codes = odd ? 0 : vr[i][w];
-                    *(s16x8 *)(vw + t * ROW + (((4 * piece + w) ^ N::v_swizzle(t)) << 4)) = from_codes<T>(codes, odd ? 1.0f : unit);
-                }
+                for (int w = 0; w < 4; ++w) to_lds((v_put ^ w << 4) + i * T16 * ROW, from_codes<T>(vr[i][w], unit));
             }
-            met |= __any(v_odd);
-            if (step + 1 < last) {
-                load(step + 1, pages);
-                pages = find_page(step + 2);
-            }
-            if (t0 >= range.hi || t0 + 32 <= range.lo) continue;   // nothing for this wave
+            // past the last step too, whose tokens are then others of the range: what is on
+            // its way has to be the same on all ways here, or a step would wait for all of it
+            const Pages p = pages_of(ids);
+            ids = find_pages(step + 2);
+            load(p, step + 1);
+            if (t0 >= range.hi || t0 + 32 <= range.lo) return;     // nothing for this wave
             float s[8];
-            s16x8 kf[2][KK];
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
-                const int t = mt * 16 + (ln & 15);
-                const char *row = kw + t * N::CODES;
                 uint32_t codes[KK];
                 if constexpr (DP == 64) {
-                    const uint2 x = *(const uint2 *)(row + (((ln >> 5) ^ N::k_swizzle(t)) << 4) + ((ln >> 4) & 1) * 8);
-                    codes[0] = x.x, codes[1] = x.y;
+                    const u32x2 x = from_lds<u32x2>(k_get + mt * 16 * N::CODES);
+                    codes[0] = x[0], codes[1] = x[1];
                 } else {
 #pragma unroll
                     for (int x = 0; x < E; ++x) {
-                        const u32x4 y = *(const u32x4 *)(row + (((E * (ln >> 4) + x) ^ N::k_swizzle(t)) << 4));
+                        const u32x4 y = from_lds<u32x4>((k_get ^ x << 4) + mt * 16 * N::CODES);
 #pragma unroll
                         for (int w = 0; w < 4; ++w) codes[4 * x + w] = y[w];
                     }
                 }
+                s16x8 kf[KK];
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) kf[mt][kk] = from_codes<T>(codes[kk], ku[mt][kk * E / KK]);
-            }
-            if (__builtin_expect(__any(k_odd), 0)) {               // scores that are NaN
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                for (int kk = 0; kk < KK; ++kk) kf[kk] = from_codes<T>(codes[kk], ku[mt][kk * E / KK]);
+                if (__builtin_expect(__any(k_odd), 0)) {           // scores that are NaN
 #pragma unroll
                     for (int kk = 0; kk < KK; ++kk)
-                        if (ku[mt][kk * E / KK] == unit_of(255)) kf[mt][kk] = nans<T>();
-            }
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
+                        if (ku[mt][kk * E / KK] > unit_of(kMaxScale<T>)) kf[kk] = nans<T>();
+                }
                 f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) x = Type<T>::mfma16(kf[mt][kk], qf[kk], x);
+                for (int kk = 0; kk < KK; ++kk) x = Type<T>::mfma16(kf[kk], qf[kk], x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[mt * 4 + i] = x[i];
             }
             const bool masked = t0 < all_lo || t0 + 32 > all_hi;
+            if constexpr (CAP) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = score<true>(a, s[i]);
+            }
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = t0 + 16 * (i / 4) + 4 * quad + i % 4;
+                    s[i] = t >= see_lo && t < see_hi ? s[i] : -INFINITY;
+                }
+            }
             float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float x = score<CAP>(a, s[i]);
-                if (masked) {
-                    const int t = t0 + 16 * (i / 4) + 4 * quad + i % 4;
-                    x = t >= see_lo && t < see_hi ? x : -INFINITY;
-                }
-                s[i] = x;
-                top = fmaxf(top, x);
-            }
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, s[i]);
+            if constexpr (!CAP) top *= a.factor;
             if (__any(top > m + 8.0f)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -208,25 +276,36 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 3 : 4) void k_kv_n
             }
             const float base = m == -INFINITY ? 0.0f : m;
             // rounded to the 16-bit type for the product, as over 16 bits
-            typename Type<T>::x8 w;
+            u32x4 packed;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = __builtin_amdgcn_exp2f(s[i] - base);
-                l += x;
-                w[i] = (T)x;
+            for (int i = 0; i < 8; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(CAP ? s[i] - base : __builtin_fmaf(s[i], a.factor, -base));
+                const float y = __builtin_amdgcn_exp2f(CAP ? s[i + 1] - base : __builtin_fmaf(s[i + 1], a.factor, -base));
+                l += x + y;
+                packed[i / 2] = pack<T>(x, y);
             }
-            const s16x8 pf = __builtin_bit_cast(s16x8, w);
-            const int row = ln >> 2;                               // 4 quad + col / 4
-            s16x8 vf[DT];
+            const s16x8 pf = __builtin_bit_cast(s16x8, packed);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const char *q = vw + row * ROW + (((dt * 2 + (ln & 3) / 2) ^ N::v_swizzle(row)) << 4) + (ln & 1) * 8;
-                const s16x4 x = read_column4(q), y = read_column4(q + 16 * ROW);
-                vf[dt] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            for (int g = 0; g < DT; g += 4) {
+                s16x8 vf[4];
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) {
+                    const uint32_t q = v_get ^ N::v_fold(2 * (g + dt)) << 4;
+                    const s16x4 x = read_column4(q), y = read_column4(q + 16 * ROW);
+                    vf[dt] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) o[g + dt] = Type<T>::mfma16(vf[dt], pf, o[g + dt]);
             }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[dt] = Type<T>::mfma16(vf[dt], pf, o[dt]);
+        };
+        if (range.hi > range.lo) {
+            ids = find_pages(first);
+            const Pages p = pages_of(ids);
+            ids = find_pages(first + 1);
+            load(p, first);
+#pragma unroll 1
+            for (int step = first; step < last; ++step) one_step(step);
         }
 
         // the waves' parts: each in its own LDS, DT vectors of 1 KiB
@@ -275,7 +354,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 3 : 4) void k_kv_n
         if (__builtin_expect(*(const uint32_t *)met_odd != 0, 0)) {
             const bool whole = starts && ends, f32 = !whole || a.out_f32;
             const int d = wave * 16 + 4 * quad, size = f32 ? 4 : 2;
-            nan_values<T>(a, table, shift, veh, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
+            nan_values<T>(a, table, shift, a.ve + head * a.ve_head, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
                           r < rows ? all_l : NAN, whole, d, 64,
                           whole ? a.out + size * (token * a.out_token + hh * a.out_head + d) : (char *)(sums + (wave * 64 + lane) * 4),
                           whole ? 64 * size : 4 * 64 * 16, f32);
@@ -283,6 +362,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 3 : 4) void k_kv_n
         __syncthreads();                      // the LDS is free again
         if (ends && walk.at < walk.end) walk.next(a, ent);
     }
+    if (lost) flag(c, MPT_KV_BAD_PAGE);
 }
 
 template <class T, int DP>

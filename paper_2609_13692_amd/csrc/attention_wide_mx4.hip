@@ -96,14 +96,14 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             for (int i = 0; i < L; ++i) {
                 int tj, t, piece;
                 piece_of(i, j, tj, t, piece);
-                const int at = tj * BN + t, id = ids[i];
-                const bool see = tj >= first && tj < last && at >= range.lo && at < range.hi && i * THREADS + tid < 2 * W::kPieces;
+                const int token = tj * BN + t, id = ids[i];
+                const bool see = tj >= first && tj < last && token >= range.lo && token < range.hi && i * THREADS + tid < 2 * W::kPieces;
                 const bool in_pool = (unsigned)id < (unsigned)c.n_pages, there = see && in_pool && piece < pieces;
                 lost |= see && !in_pool;
-                const uint32_t slot = (uint32_t)at & (c.page_size - 1);
+                const uint32_t slot = (uint32_t)token & (c.page_size - 1);
                 const bool key = is_key(i);
-                const char *rows0 = (key ? kh : vh) + 16 * piece + row_at(id, slot, key ? a.k_page : a.v_page, key ? a.k_slot : a.v_slot);
-                const char *e0 = (key ? keh : veh) + piece + scale_at(id, slot, key ? a.ke_page : a.ve_page, key ? a.ke_slot : a.ve_slot);
+                const char *rows0 = at(at((key ? kh : vh) + 16 * piece, id, key ? a.k_page : a.v_page), slot, key ? a.k_slot : a.v_slot);
+                const char *e0 = at(at((key ? keh : veh) + piece, id, key ? a.ke_page : a.ve_page), slot, key ? a.ke_slot : a.ve_slot);
                 codes[i] = mptkv::load<u32x4>(or_zeros(there, rows0));
                 scale[i] = mptkv::load<uint8_t>(or_zeros(there, e0));
             }
@@ -121,8 +121,8 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
                 s16x8 x[4];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) x[w] = from_codes<T>(codes[i][w], unit);
-                if (__builtin_expect(__any(scale[i] == 255), 0)) {
-                    if (scale[i] == 255) {
+                if (__builtin_expect(__any(scale[i] > kMaxScale<T>), 0)) {
+                    if (scale[i] > kMaxScale<T>) {
                         const s16x8 y = key ? nans<T>() : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
                         for (int w = 0; w < 4; ++w) x[w] = y;

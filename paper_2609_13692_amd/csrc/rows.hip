@@ -429,7 +429,7 @@ __device__ inline uint4 from_codes(uint32_t codes, uint32_t scale) {
             return __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, unit, which));
     };
     const uint32_t nan = __is_same(T, __bf16) ? 0x7fc07fc0u : 0x7e007e00u;
-    if (scale == 255) return uint4{nan, nan, nan, nan};
+    if (scale > (__is_same(T, __bf16) ? 127 + 125 : 127 + 13)) return uint4{nan, nan, nan, nan};
     return uint4{two(std::integral_constant<int, 0>()), two(std::integral_constant<int, 1>()),
                  two(std::integral_constant<int, 2>()), two(std::integral_constant<int, 3>())};
 }

@@ -238,10 +238,10 @@ class KvCache:
         shape = t.shape
         if len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim or t.dtype is not dtype:
             raise ValueError(f"{name} must be [tokens, {heads}, {self.head_dim}] of {dtype}, got {tuple(shape)} of {t.dtype}")
-        stride = t.stride()
-        if t.get_device() != self._index or stride[2] != 1:
+        by_token, by_head, by_element = t.stride()
+        if by_element != 1 or t.get_device() != self._index:
             raise ValueError(f"{name} must be on {self.device}, with contiguous rows")
-        return t.data_ptr(), stride[0], stride[1]
+        return t.data_ptr(), by_token, by_head
 
     def append(self, layer, k_new, v_new, q_off, seqs, stream=None):
         """Writes the newest tokens' keys and values of one layer; q_off [n + 1]
@@ -281,10 +281,18 @@ class KvCache:
             heads = q.shape[1]
             q_in = self._rows(q, heads, "q", self.dtype)
             if q_out is None:
-                q_out = _new(q.shape, self.dtype, self.device, under)
-            if q.shape[0] != tokens or q_out.shape[0] != tokens:
-                raise ValueError("q and q_out must have one row per token")
-            out = q_in if q_out is q else self._rows(q_out, heads, "q_out", self.dtype)
+                q_out = _like(q, self.dtype, under)
+                by_token, by_head, by_element = q_out.stride()
+                if by_element != 1:                        # q's rows overlap, or are a column each
+                    q_out = _new(q.shape, self.dtype, self.device, under)
+                    by_token, by_head, _ = q_out.stride()
+                out = q_out.data_ptr(), by_token, by_head
+            elif q_out.shape[0] != tokens:
+                raise ValueError("q_out must have one row per token")
+            else:
+                out = q_in if q_out is q else self._rows(q_out, heads, "q_out", self.dtype)
+            if q.shape[0] != tokens:
+                raise ValueError("q must have one row per token")
         elif q_out is not None:
             raise ValueError("q_out without q")
         n, lists = 0, (None, None)
@@ -305,22 +313,22 @@ class KvCache:
         type: of entry i those from first[i] on (None: the newest) of the
         sequence in slot seqs[i], off[i + 1] - off[i] of them, in rows off[i] on.
         Tokens that are not there are zeros (see mpt_kv_read)."""
-        n, index = seqs.numel(), self._index
+        n, index, heads = seqs.numel(), self._index, self.n_heads
         at, under = _on(stream, index)
-        shape = (tokens, self.n_heads, self.head_dim)
-        rows = []
-        for name, t in (("k_out", k_out), ("v_out", v_out)):
-            if t is None:
-                t = _new(shape, self.dtype, self.device, under)
-            elif t.shape[0] != tokens:
-                raise ValueError(f"{name} must have one row per token")
-            rows.append((t, self._rows(t, self.n_heads, name, self.dtype)))
+        if k_out is None:
+            k_out = _new((tokens, heads, self.head_dim), self.dtype, self.device, under)
+            if v_out is None:
+                v_out = _like(k_out, self.dtype, under)
+        elif v_out is None:
+            v_out = _new((tokens, heads, self.head_dim), self.dtype, self.device, under)
+        if k_out.shape[0] != tokens or v_out.shape[0] != tokens:
+            raise ValueError("k_out and v_out must have one row per token")
         rc = _run(index, self._lib.mpt_kv_read, self._p, layer, n, _list(seqs, n, "seqs", index),
                   _list(off, n + 1, "off", index), None if first is None else _list(first, n, "first", index), tokens,
-                  *rows[0][1], *rows[1][1], at)
+                  *self._rows(k_out, heads, "k_out", self.dtype), *self._rows(v_out, heads, "v_out", self.dtype), at)
         if rc:
             _check(rc, "mpt_kv_read")
-        return rows[0][0], rows[1][0]
+        return k_out, v_out
 
     def attend(self, layer, q, q_off, seqs, causal=True, window=0, softcap=0.0, scale=None, kv_begin=None, out=None,
                lse=None, out_dtype=None, stream=None):

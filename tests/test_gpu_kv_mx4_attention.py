@@ -15,7 +15,7 @@ from test_gpu_kv_attention import DT, check, ints
 pytestmark = pytest.mark.gpu
 
 
-def filled(lengths, page, kv_heads, dim, dtype, seed, heads_first=True, extra_pages=5):
+def filled(lengths, page, kv_heads, dim, dtype, seed, heads_first=True, extra_pages=5, poison=255):
     """A cache of two layers whose bytes start out as 0xff (NaN), sequences in
     slots in a mixed order, written into layer 1; and their values in 64 bits."""
     g = torch.Generator().manual_seed(seed)
@@ -23,7 +23,7 @@ def filled(lengths, page, kv_heads, dim, dtype, seed, heads_first=True, extra_pa
     pages = sum(-(-l // page) for l in lengths) + extra_pages
     c = kv.KvCache.create(2, pages, page, kv_heads, dim, n + 2, max(max(lengths), 1) + 2 * page, dtype, heads_first=heads_first, bits=4)
     for x in (c.k, c.v, c.k_scale, c.v_scale):
-        x.fill_(255)
+        x.fill_(poison)
     slots = torch.randperm(n + 2, generator=g)[:n].int().cuda()
     c.fork(ints([-1] * n), slots, ints([0] * n), ints(lengths), check=True)
     total = sum(lengths)
@@ -165,7 +165,7 @@ def test_nan(dim, count, length):
 def test_bad_pages_and_slots(count):
     """Pages outside the pool count as tokens of zeros or of the pool, and are
     reported; slots outside the table as empty."""
-    c, slots, ks, vs = filled([200, 100], 16, 1, 128, torch.float16, 15)
+    c, slots, ks, vs = filled([200, 100], 16, 1, 128, torch.float16, 15, poison=100)
     q = torch.randn((2 * count, 4, 128), device="cuda").half()
     clean, _ = c.attend(1, q, ints([0, count, 2 * count]), slots)
     for page in (-1, 10 ** 9, c.k.shape[1], -2 ** 31):
