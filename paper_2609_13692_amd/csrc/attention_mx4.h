@@ -16,6 +16,11 @@ struct Attn4 : Attn {
 // x at index i of so many bytes: one instruction.
 inline __device__ const char *at(const char *x, uint32_t i, uint32_t bytes) { return x + (uint64_t)i * bytes; }
 
+template <class V>
+__device__ inline void to_lds(uint32_t at, V x) {
+    *(__attribute__((address_space(3))) V *)(uintptr_t)at = x;
+}
+
 // The largest E that appends write; all above count as 255, which is NaN.
 template <class T>
 constexpr uint32_t kMaxScale = __is_same(T, __bf16) ? 127 + 125 : 127 + 13;

@@ -26,10 +26,6 @@ namespace mptkv {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-template <class V>
-__device__ inline void to_lds(uint32_t at, V x) {
-    *(__attribute__((address_space(3))) V *)(uintptr_t)at = x;
-}
 
 template <int DP>
 struct Narrow4 {

@@ -47,6 +47,17 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
     const int v_of = 4 * half + (lane & 15) / 4;
     const uint32_t v_at = lds_address(values) + v_of * ROW + (lane & 1) * 8 + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ W::v_swizzle(v_of));
     bool lost = false;                         // a page id outside the pool
+    // A thread's pieces, and where their elements go: the first quarter of each.
+    auto is_key = [&](int i) INLINE { return i * THREADS + wave * 64 < W::kPieces; };
+    auto has_piece = [&](int i) INLINE { return i * THREADS + wave * 64 < 2 * W::kPieces; };
+    auto piece_of = [&](int i) INLINE { return (i * THREADS + renewed(tid)) & (CP - 1); };
+    auto token_of_piece = [&](int i) INLINE { return (int)((uint32_t)((i * THREADS + renewed(tid)) & (W::kPieces - 1)) / CP); };
+    uint32_t put_at[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const int t = token_of_piece(i), swizzle = is_key(i) ? W::k_swizzle(t) : W::v_swizzle(t);
+        put_at[i] = lds_address(is_key(i) ? keys : values) + t * ROW + ((4 * piece_of(i) ^ swizzle) << 4);
+    }
 
     Walk<M, BN, C> walk;
     if (!walk.begin(a, ent, 4)) return;
@@ -67,56 +78,54 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         const bool active = row_base < rows;
 
         // Turn j, between the barriers in tiles j - 1 and j, makes the keys of tile
-        // j + 1 and the values of tile j: of each thread L pieces, keys first. Their
-        // codes are loaded a turn before, their pages' ids one before that.
-        const char *kh = a.k + head * a.k_head, *vh = a.v + head * a.v_head;
-        const char *keh = a.ke + head * a.ke_head, *veh = a.ve + head * a.ve_head;
+        // j + 1 and the values of tile j: of each thread L pieces, keys first, a wave's
+        // all of one kind. Their codes are loaded a turn before, their pages' ids one
+        // before that.
+        // Tokens that the tile does not reach are read as others of it (their scores are
+        // masked, and a weight of 0 times a finite value is 0), and so are pieces past the
+        // row's end (their queries are 0). A page id outside the pool becomes the last
+        // page, and is reported.
+        // A tile's tokens are 64 slots of a page, or pages are of the tile: a thread's
+        // places in them are the same for all tiles but for what is uniform.
+        const char *from_codes_of[L], *from_scales_of[L];
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const bool key = is_key(i);
+            const int piece = min(piece_of(i), pieces - 1);
+            const uint32_t slot = token_of_piece(i) & (c.page_size - 1);
+            from_codes_of[i] = at((key ? a.k + head * a.k_head : a.v + head * a.v_head) + 16 * piece, slot, key ? a.k_slot : a.v_slot);
+            from_scales_of[i] = at((key ? a.ke + head * a.ke_head : a.ve + head * a.ve_head) + piece, slot, key ? a.ke_slot : a.ve_slot);
+        }
         u32x4 codes[L];
         uint8_t scale[L];
         int ids[L];
         bool met = false;                      // a NaN among the values
-        auto is_key = [&](int i) INLINE { return i * THREADS + tid < W::kPieces; };
-        auto piece_of = [&](int i, int j, int &tile_j, int &t, int &piece) INLINE {
-            const int x = i * THREADS + renewed(tid);
-            const bool key = x < W::kPieces;
-            tile_j = key ? j + 1 : j;
-            t = (x & (W::kPieces - 1)) / CP;
-            piece = x & (CP - 1);
-        };
         auto fetch_ids = [&](int j) INLINE {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                int tj, t, piece;
-                piece_of(i, j, tj, t, piece);
-                ids[i] = table[max(0, max(range.lo, min(range.hi - 1, tj * BN + t))) >> shift];
+                const int t = (j + is_key(i)) * BN + token_of_piece(i);
+                ids[i] = table[max(0, max(range.lo, min(range.hi - 1, t))) >> shift];
             }
         };
         auto fetch = [&](int j) INLINE {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                int tj, t, piece;
-                piece_of(i, j, tj, t, piece);
-                const int token = tj * BN + t, id = ids[i];
-                const bool see = tj >= first && tj < last && token >= range.lo && token < range.hi && i * THREADS + tid < 2 * W::kPieces;
-                const bool in_pool = (unsigned)id < (unsigned)c.n_pages, there = see && in_pool && piece < pieces;
-                lost |= see && !in_pool;
-                const uint32_t slot = (uint32_t)token & (c.page_size - 1);
+                if (!has_piece(i)) break;
                 const bool key = is_key(i);
-                const char *rows0 = at(at((key ? kh : vh) + 16 * piece, id, key ? a.k_page : a.v_page), slot, key ? a.k_slot : a.v_slot);
-                const char *e0 = at(at((key ? keh : veh) + piece, id, key ? a.ke_page : a.ve_page), slot, key ? a.ke_slot : a.ve_slot);
-                codes[i] = mptkv::load<u32x4>(or_zeros(there, rows0));
-                scale[i] = mptkv::load<uint8_t>(or_zeros(there, e0));
+                const uint32_t id = min((uint32_t)ids[i], (uint32_t)c.n_pages - 1);
+                lost |= id != (uint32_t)ids[i] && range.hi > 0;
+                const uint64_t slot = (uint32_t)((j + key) * BN) & (c.page_size - 1);
+                codes[i] = mptkv::load<u32x4>(at(from_codes_of[i], id, key ? a.k_page : a.v_page) + slot * (key ? a.k_slot : a.v_slot));
+                scale[i] = mptkv::load<uint8_t>(at(from_scales_of[i], id, key ? a.ke_page : a.ve_page) + slot * (key ? a.ke_slot : a.ve_slot));
             }
         };
-        auto make = [&](int j) INLINE {
+        // odd: whether the values' tile, j, is of odd number from `first` on (the keys' is the other kind)
+        auto make = [&](int odd) INLINE {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                int tj, t, piece;
-                piece_of(i, j, tj, t, piece);
+                if (!has_piece(i)) break;
                 const bool key = is_key(i);
-                if (i * THREADS + tid >= 2 * W::kPieces) break;
-                char *row = (key ? keys : values) + ((tj - first) & 1) * TILE + t * ROW;
-                const int swizzle = key ? W::k_swizzle(t) : W::v_swizzle(t);
+                const uint32_t to = put_at[i] + (odd ^ key ? TILE : 0);
                 const float unit = unit_of(scale[i]);
                 s16x8 x[4];
 #pragma unroll
@@ -130,7 +139,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
                     }
                 }
 #pragma unroll
-                for (int w = 0; w < 4; ++w) *(s16x8 *)(row + (((4 * piece + w) ^ swizzle) << 4)) = x[w];
+                for (int w = 0; w < 4; ++w) to_lds(to ^ w << 4, x[w]);
             }
         };
         fetch_ids(first - 1);
@@ -148,9 +157,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             // wide heads: in the registers that only products read, where they stay
             if constexpr (DP == 256) asm volatile("" : "+a"(qf[kk]));
         }
-        // tokens that all rows of the wave see
-        int wave_lo, wave_hi;
+        // tokens that all rows of the wave, and of the tile, see
+        int wave_lo, wave_hi, tile_lo, tile_hi;
         seen_by_all(a, n, len, begin, min(row_base, rows - 1), min(row_base + 31, rows - 1), wave_lo, wave_hi);
+        seen_by_all(a, n, len, begin, tile * M, min(tile * M + M, rows) - 1, tile_lo, tile_hi);
 
         f32x16 o[DT], s0, s1;
         s16x8 pf[2];
@@ -164,10 +174,11 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         // The products of a step, in groups that the compiler keeps in order:
         // an operand from LDS (read some groups ahead), its product, and beside
         // it a share of the step's other work.
-        // S' = K Q' of 32 tokens
-        auto multiply = [&](uint32_t base, f32x16 &s, auto beside) INLINE {
+        // S' = K Q' of 32 tokens (base: where the lane's first operand lies; kb, vb: bytes
+        // from there, constants)
+        auto multiply = [&](uint32_t base, int kb, f32x16 &s, auto beside) INLINE {
             s16x8 kf[AHEAD + 1];
-            auto read = [&](int kk) INLINE { kf[kk % (AHEAD + 1)] = from_lds<s16x8>(base ^ 32 * kk); };
+            auto read = [&](int kk) INLINE { kf[kk % (AHEAD + 1)] = from_lds<s16x8>((base ^ 32 * kk) + kb); };
 #pragma unroll
             for (int kk = 0; kk < AHEAD; ++kk) read(kk);
 #pragma unroll
@@ -179,10 +190,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             }
         };
         // O' += V' P' of 32 tokens
-        auto add = [&](uint32_t base, auto beside) INLINE {
+        auto add = [&](uint32_t base, int vb, auto beside) INLINE {
             s16x8 vf[AHEAD + 1];
             auto read = [&](int i) INLINE {
-                const uint32_t x = (base ^ 64 * (i % DT)) + (i / DT) * 16 * ROW;
+                const uint32_t x = (base ^ 64 * (i % DT)) + vb + (i / DT) * 16 * ROW;
                 const s16x4 y = read_column4(x), z = read_column4(x + 8 * ROW);
                 vf[i % (AHEAD + 1)] = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
             };
@@ -200,12 +211,12 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         // One step of 32 tokens from t0 with scores x: products with the values
         // of the step before beside this step's maximum, scores of the next
         // step beside this step's weights.
-        auto step32 = [&](f32x16 &x, f32x16 &next, int t0, uint32_t k_next, uint32_t v_before) INLINE {
+        auto step32 = [&](auto all_seen, f32x16 &x, f32x16 &next, int t0, uint32_t k_base, int k_next, uint32_t v_base, int v_before) INLINE {
             if constexpr (CAP) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] = score<true>(a, x[r]);
             }
-            if (t0 < wave_lo || t0 + 32 > wave_hi) {
+            if (!all_seen && (t0 < wave_lo || t0 + 32 > wave_hi)) {
                 const int before = t0 + 4 * renewed(half), lo = see_lo - before, hi = see_hi - before;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -215,7 +226,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             }
             __builtin_amdgcn_s_setprio(1);
             float top = -INFINITY;
-            add(v_before, [&](int i) INLINE {
+            add(v_base, v_before, [&](int i) INLINE {
                 constexpr int N = 8 / DT;
 #pragma unroll
                 for (int y = i * N; y < i * N + N; ++y) top = fmaxf(top, x[y]);
@@ -238,7 +249,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             // product are of one, as over 16 bits.
             float even = 0;
             u32x4 packed[2];
-            multiply(k_next, next, [&](int i) INLINE {
+            multiply(k_base, k_next, next, [&](int i) INLINE {
                 constexpr int N = 16 / KK;
 #pragma unroll
                 for (int r = i * N; r < i * N + N; ++r) {
@@ -257,26 +268,54 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         __syncthreads();                       // the previous rows' products have read their buffers
         fetch(first - 1);
         fetch_ids(first);
-        make(first - 1);                       // keys of the first tile, zeros as the values before it
+        make(1);                               // keys of the first tile, some values as those before it
         fetch(first);
         fetch_ids(first + 1);
-        make(first);
+        make(0);
         fetch(first + 1);
         fetch_ids(first + 2);
         __syncthreads();
-        if (active) multiply(k_at, s0, nothing);
-        for (int step = first; step < last; ++step) {
-            const int now = ((step - first) & 1) * TILE, other = TILE - now;
-            if (active) {
-                step32(s0, s1, step * BN, k_at + now + 32 * ROW, v_at + other + 32 * ROW);
+        if (active) multiply(k_at, 0, s0, nothing);
+        for (int step = first; step < last;) {
+            if constexpr (DP < 256) {
+                // Two tiles whose tokens every row of the tile sees, in places that are
+                // constants.
+                const int t0 = step * BN;
+                if (((step - first) & 1) == 0 && step + 2 <= last && t0 >= tile_lo && t0 + 2 * BN <= tile_hi) {
+                    auto turn = [&](auto r_) INLINE {
+                        constexpr int R = decltype(r_)::value, O = 1 - R;
+                        if (active) step32(std::true_type(), s0, s1, 0, k_at, R * TILE + 32 * ROW, v_at, O * TILE + 32 * ROW);
+                        __syncthreads();
+                        make(O);
+                        fetch(step + R + 2);
+                        fetch_ids(step + R + 3);
+                        if (active) step32(std::true_type(), s1, s0, 0, k_at, O * TILE, v_at, R * TILE);
+                    };
+                    turn(std::integral_constant<int, 0>());
+                    turn(std::integral_constant<int, 1>());
+                    step += 2;
+                    continue;
+                }
             }
-            __syncthreads();
-            make(step + 1);
-            fetch(step + 2);
-            fetch_ids(step + 3);
-            if (active) step32(s1, s0, step * BN + 32, k_at + other, v_at + now);
+            const int odd = (step - first) & 1, now = odd * TILE, other = TILE - now;
+            // its two halves by one piece of code: a call with few steps waits for its
+            // instructions more than for anything else
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                if (active) {
+                    step32(std::false_type(), s0, s1, step * BN + 32 * h, k_at + (h ? other : now + 32 * ROW), 0,
+                           v_at + (h ? now : other + 32 * ROW), 0);
+                    s0 = s1;
+                }
+                if (h) break;
+                __syncthreads();
+                make(!odd);
+                fetch(step + 2);
+                fetch_ids(step + 3);
+            }
+            ++step;
         }
-        if (active) add(v_at + ((last - 1 - first) & 1) * TILE + 32 * ROW, nothing);
+        if (active) add(v_at + ((last - 1 - first) & 1) * TILE + 32 * ROW, 0, nothing);
 
         float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (from == 0)) * (M * (DP + 2)) + wave * 32 * DP;
         const float sum = l + __shfl_xor(l, 32);
@@ -320,7 +359,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             const bool whole = starts && ends, f32 = !whole || a.out_f32;
             const int size = f32 ? 4 : 2;
             if (active)
-                nan_values<T>(a, table, shift, veh, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
+                nan_values<T>(a, table, shift, a.ve + head * a.ve_head, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
                               r0 < rows ? sum : NAN, whole, 4 * half, 8,
                               whole ? a.out + size * ((int64_t)(q0 + j0) * a.out_token + ((int64_t)head * a.group + rr - j0 * a.group) * a.out_head + 4 * half)
                                     : (char *)(sums + lane * 4),
