@@ -8,15 +8,19 @@ computed (its keys and values appended, its queries attended over the whole
 prefix), so the tokens computed are the layout's trie cost (Eq. 1), which
 ``mpt_layout_cost`` bills. Nodes that no request ends at are freed once their
 children exist, unless the prefill is told to keep their depth; their pages live
-on in the children. It is a demonstration of the cache's calls: one layer, and a
+on in the children. Keys and queries can be rotated to their positions in the
+request (a node's tokens have the same ones in all requests below it), and the
+cache can be of 4 bits. It is a demonstration of the cache's calls: one layer, and a
 decode step whose tokens are not appended.
 
 ``python -m paper_2609_13692_amd.serve`` runs a small retrieval-shaped instance
 through the exact solver, the cache and a decode step in which each first
-chunk's tokens are read once for all requests below it.
+chunk's tokens are read once for all requests below it; ``--rotate`` rotates keys
+and queries, ``--bits 4`` holds the cache in 4 bits.
 """
 from __future__ import annotations
 
+import argparse
 import dataclasses
 
 import numpy as np
@@ -63,17 +67,22 @@ class LayoutServer:
     """A cache of one layer that holds the prompts of a layout.
 
     ``project(chunk)`` returns the queries [tokens, heads, dim], keys and
-    values [tokens, kv_heads, dim] of a chunk's tokens on the device.
+    values [tokens, kv_heads, dim] of a chunk's tokens on the device. With
+    ``freq`` (float32 [pairs] on the device, see :meth:`.kv.KvCache.append_rotated`)
+    queries and keys are rotated to their tokens' positions; ``bits`` are the
+    cache's (16 or 4).
     """
 
-    def __init__(self, trie: Trie, project, heads, kv_heads, dim, page_size=16, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, trie: Trie, project, heads, kv_heads, dim, page_size=16, dtype=torch.bfloat16, device="cuda",
+                 freq=None, interleaved=False, bits=16):
+        self.freq, self.interleaved = freq, interleaved
         self.trie, self.project, self.heads, self.device = trie, project, heads, torch.device(device)
         tokens = trie.length - np.where(trie.parent < 0, 0, trie.length[trie.parent])
         self.new_tokens = tokens
         # a node's own pages: its tokens, and its parent's last page once more
         pages = int((-(-(tokens + page_size - 1) // page_size)).sum())
         self.cache = kv.KvCache.create(1, max(1, pages), page_size, kv_heads, dim, max(1, len(tokens)),
-                                       int(trie.length.max(initial=1)) + page_size, dtype, device)
+                                       int(trie.length.max(initial=1)) + page_size, dtype, device, bits=bits)
         self.outputs = {}                      # attention outputs of each node's tokens
         self.held = np.zeros(len(tokens), dtype=bool)   # nodes whose slots hold their prefix
 
@@ -94,7 +103,11 @@ class LayoutServer:
             self.cache.fork(self._ints(parent), self._ints(level), self._ints(keep), self._ints(t.length[level]), check=True)
             q, k, v = (torch.cat(x) for x in zip(*(self.project(int(t.chunk[i])) for i in level)))
             off = np.concatenate([[0], np.cumsum(self.new_tokens[level])])
-            self.cache.append(0, k, v, self._ints(off), self._ints(level))
+            if self.freq is None:
+                self.cache.append(0, k, v, self._ints(off), self._ints(level))
+            else:
+                self.cache.append_rotated(0, k, v, self._ints(off), self._ints(level), self.freq, q=q, q_out=q,
+                                          interleaved=self.interleaved)
             out, _ = self.cache.attend(0, q, self._ints(off), self._ints(level))
             self.held[level] = True
             for i, a, b in zip(level, off, off[1:]):
@@ -110,7 +123,7 @@ class LayoutServer:
 
     def decode(self, q, shared_depth=1):
         """Attention of one query per request (q [requests, heads, dim], not
-        appended) over its prompt. Nodes are read once for all requests below
+        appended, rotated to the position after the prompt) over its prompt. Nodes are read once for all requests below
         them: of each request the deepest up to shared_depth whose slot prefill
         kept (keep_depth); a request without one reads its whole prompt."""
         t, requests = self.trie, len(self.trie.leaf)
@@ -127,6 +140,9 @@ class LayoutServer:
         groups, counts = np.unique(first[order[:shared]], return_counts=True)
         pick = torch.as_tensor(order, device=self.device)
         sorted_q = q[pick].contiguous()
+        if self.freq is not None:
+            self.cache.append_rotated(0, None, None, None, None, self.freq, q=sorted_q, q_out=sorted_q,
+                                      interleaved=self.interleaved, positions=self._ints(t.length[t.leaf[order]]))
         each = np.arange(len(order) + 1)
         begin = np.append(t.length, 0)[first[order]]
         out, lse = self.cache.attend(0, sorted_q, self._ints(each), self._ints(t.leaf[order]), causal=False,
@@ -157,11 +173,17 @@ def random_projection(inst, heads, kv_heads, dim, dtype, seed, device="cuda"):
     return project
 
 
-def main() -> None:
+def main(argv=None) -> None:
+    args = argparse.ArgumentParser(prog="python -m paper_2609_13692_amd.serve", description=__doc__.splitlines()[0])
+    args.add_argument("--rotate", action="store_true", help="rotate keys and queries to their positions")
+    args.add_argument("--bits", type=int, choices=(16, 4), default=16, help="of the cache's elements")
+    args = args.parse_args(argv)
+    freq = 10000.0 ** (torch.arange(64, device="cuda") / -64) if args.rotate else None
     inst = wl.gen_retrieval(m=12, u=200, topics=6, k=6, seed=1)
     orders = mpt.solve(inst)["orders"]
     trie = trie_of(inst.req_off, orders, inst.weights)
-    server = LayoutServer(trie, random_projection(inst, 8, 2, 128, torch.bfloat16, 0), 8, 2, 128)
+    server = LayoutServer(trie, random_projection(inst, 8, 2, 128, torch.bfloat16, 0), 8, 2, 128,
+                          freq=freq, bits=args.bits)
     computed = server.prefill(keep_depth=1)
     total = int(sum(inst.weights[c] for c in orders))
     print(f"{inst.name}: {computed} of {total} prompt tokens computed, {len(trie.parent)} trie nodes, "
