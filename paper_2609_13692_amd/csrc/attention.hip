@@ -50,13 +50,19 @@ struct Choice {
 //   dim 256, 32 entries: 16 rows 65/217; 48 rows 174/218 and 34/34; 64 rows
 //   226/220 and 43/35
 // More workers than the card holds, and fewer, cost up to a third (512 of heads of
-// 128: 105 us of 128 entries, 256 139, 768 137).
+// 128: 105 us of 128 entries, 256 139, 768 137). But single tiles of a few key heads
+// come to an end sooner with 256, whose partial sums are fewer to join: 8 heads of
+// 128 over 1800 tokens of 8 entries 17 us (512: 20), over 16000 of one 19 (23), over
+// 8000 of eight 26 (26), over 16000 of sixteen 67 (54); of 64 15 (768: 22), 21 (20), 48
+// (35) over the last three.
 static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
     const bool few = (int64_t)n * c.n_heads <= 256, own_cu = dim == 128 && few;
-    if (rows <= (is_mx4(c) ? (few && dim != 256 ? 64 : 48) : dim == 128 ? 32 : 16))
-        return {0, dim == 256 ? 256 : dim == 128 ? 512 : 768, 16};
+    if (rows <= (is_mx4(c) ? (few && dim != 256 ? 64 : 48) : dim == 128 ? 32 : 16)) {
+        if (dim == 256 || (is_mx4(c) && rows <= 16 && (int64_t)n * c.n_heads <= 64)) return {0, 256, 16};
+        return {0, dim == 128 ? 512 : 768, 16};
+    }
     if ((rows <= 128 && !own_cu) || dim == 256) return {4, dim == 256 ? 256 : 512, 128};
     return {8, 256, 256};
 }
