@@ -18,34 +18,41 @@ namespace mptkv {
 
 template <int DP, int WAVES>
 struct Wide4 {
-    static constexpr int kThreads = 64 * WAVES, BN = 64, KK = DP / 16, DT = DP / 32, ROW = 2 * DP;
+    static constexpr bool kSmall = DP == 256;                                  // products of 16 rows
+    static constexpr int kThreads = 64 * WAVES, BN = 64, ROW = 2 * DP, R = kSmall ? 16 : 32, M = R * WAVES;
+    static constexpr int KK = DP * R / 512, DT = DP / R;                       // operands of a row, and of an output row
+    static constexpr int S = R / 2;                                            // scores a lane of 32 tokens
+    typedef float Scores __attribute__((ext_vector_type(S)));
+    typedef float Sums __attribute__((ext_vector_type(R == 16 ? 4 : 16)));
     static constexpr int kTile = BN * ROW, CP = DP / 32, kPieces = BN * CP;   // bytes in 16 bits; pieces of a row, of a tile
     static constexpr int L = (2 * kPieces + kThreads - 1) / kThreads;          // pieces of keys and values per thread
     static constexpr int C = 8;                                                // a tile's cost besides its steps, in steps
-    static constexpr int kAhead = DP == 256 ? 3 : 2;                           // operands read from LDS ahead of their products
+    static constexpr int kAhead = DP == 256 ? 4 : 2;                           // operands read from LDS ahead of their products
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight tokens'
-    // pieces, values so that four tokens' 64 bytes, fall on all banks, and so do
-    // the first (second, ...) quarters of 16 threads' elements, which are written at
-    // a time; equal for tokens 8 apart (values) and 32 (keys).
-    __device__ static int k_swizzle(int t) { return DP == 64 ? (t >> 1) & 7 : DP == 128 ? t & 15 : t & 7; }
-    __device__ static int v_swizzle(int t) { return DP == 64 ? 5 * ((t >> 1) & 1) + 2 * ((t >> 2) & 1) : 5 * (t & 3); }
+    // pieces (wide heads: 16 tokens'), values so that four tokens' 64 bytes (32), fall
+    // on all banks, and so do the first (second, ...) quarters of the elements that 16
+    // threads (eight) write at a time; equal for tokens 8 apart (values) and 32 (keys; 16).
+    __host__ __device__ static constexpr int fold(int u) { return kSmall ? u ^ ((u >> 3) & 3) : u; }
+    __device__ static int k_swizzle(int t) { return DP == 64 ? (t >> 1) & 7 : t & 15; }
+    __device__ static int v_swizzle(int t) { return DP == 64 ? 5 * ((t >> 1) & 1) + 2 * ((t >> 2) & 1) : DP == 128 ? 5 * (t & 3) : 2 * (t & 7); }
 };
 
 template <class T, int DP, int WAVES, bool CAP>
-__global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(Attn4 a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void k_kv_wide_mx4(Attn4 a) {
     using W = Wide4<DP, WAVES>;
-    constexpr int M = 32 * WAVES, THREADS = W::kThreads, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, L = W::L, TILE = W::kTile;
-    constexpr int C = W::C, AHEAD = W::kAhead, CP = W::CP;
+    constexpr int M = W::M, THREADS = W::kThreads, BN = W::BN, KK = W::KK, DT = W::DT, ROW = W::ROW, L = W::L, TILE = W::kTile, R = W::R;
+    constexpr int C = W::C, AHEAD = W::kAhead, CP = W::CP, S = W::S;
+    constexpr bool SMALL = W::kSmall;
     __shared__ Entries ent;
     __shared__ __attribute__((aligned(1024))) char keys[2 * TILE], values[2 * TILE];
     const mpt_kv_cache &c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & (R - 1), part = lane / R;   // part: half, or quarter, of the wave
     const int shift = 31 - __clz(c.page_size), pieces = a.units / 4;
-    // Where a lane reads its operands: rows of 32 tokens of keys, 8 of values.
-    const uint32_t k_at = lds_address(keys) + col * ROW + 16 * (half ^ W::k_swizzle(col));
-    const int v_of = 4 * half + (lane & 15) / 4;
-    const uint32_t v_at = lds_address(values) + v_of * ROW + (lane & 1) * 8 + 16 * ((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ W::v_swizzle(v_of));
+    // Where a lane reads its operands: rows of 32 tokens of keys (16), 8 of values (16).
+    const uint32_t k_at = lds_address(keys) + col * ROW + 16 * (part ^ W::k_swizzle(col));
+    const int v_of = (SMALL ? 4 * part : 4 * (lane >> 5)) + (lane & 15) / 4, v_piece = (SMALL ? 0 : ((lane >> 4) & 1) * 2) + (lane & 3) / 2;
+    const uint32_t v_at = lds_address(values) + v_of * ROW + (lane & 1) * 8 + 16 * (v_piece ^ W::v_swizzle(v_of));
     bool lost = false;                         // a page id outside the pool
     // A thread's pieces, and where their elements go: the first quarter of each.
     auto is_key = [&](int i) INLINE { return i * THREADS + wave * 64 < W::kPieces; };
@@ -56,7 +63,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
 #pragma unroll
     for (int i = 0; i < L; ++i) {
         const int t = token_of_piece(i), swizzle = is_key(i) ? W::k_swizzle(t) : W::v_swizzle(t);
-        put_at[i] = lds_address(is_key(i) ? keys : values) + t * ROW + ((4 * piece_of(i) ^ swizzle) << 4);
+        put_at[i] = lds_address(is_key(i) ? keys : values) + t * ROW + ((W::fold(4 * piece_of(i)) ^ swizzle) << 4);
     }
 
     Walk<M, BN, C> walk;
@@ -73,7 +80,7 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             break;
         }
         const int first = range.first + from, last = range.first + to;
-        const int rows = n * a.group, row_base = tile * M + wave * 32;
+        const int rows = n * a.group, row_base = tile * M + wave * R;
         const int32_t *table = c.table + (int64_t)uniform(ent.slot[e]) * c.max_pages;
         const bool active = row_base < rows;
 
@@ -150,97 +157,113 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         const char *q = a.q + 2 * ((int64_t)(q0 + j0) * a.q_token + ((int64_t)head * a.group + rr - j0 * a.group) * a.q_head);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-            const int piece = 2 * kk + half;
+            const int piece = 64 / R * kk + part;
             u32x4 x = mptkv::load<u32x4>(or_zeros(r0 < rows && piece < a.units, q + 16 * piece));
             if (a.flip) x ^= 0x80008000u;
             qf[kk] = __builtin_bit_cast(s16x8, x);
-            // wide heads: in the registers that only products read, where they stay
-            if constexpr (DP == 256) asm volatile("" : "+a"(qf[kk]));
         }
         // tokens that all rows of the wave, and of the tile, see
         int wave_lo, wave_hi, tile_lo, tile_hi;
-        seen_by_all(a, n, len, begin, min(row_base, rows - 1), min(row_base + 31, rows - 1), wave_lo, wave_hi);
+        seen_by_all(a, n, len, begin, min(row_base, rows - 1), min(row_base + R - 1, rows - 1), wave_lo, wave_hi);
         seen_by_all(a, n, len, begin, tile * M, min(tile * M + M, rows) - 1, tile_lo, tile_hi);
 
-        f32x16 o[DT], s0, s1;
-        s16x8 pf[2];
+        typename W::Sums o[DT];
+        typename W::Scores s0, s1;
+        s16x8 pf[S / 8];
         float m = -INFINITY, l = 0;
-        pf[0] = pf[1] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+        for (int x = 0; x < S / 8; ++x) pf[x] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[dt][r] = 0;
+        for (int dt = 0; dt < DT; ++dt) o[dt] = 0;
 
         // The products of a step, in groups that the compiler keeps in order:
         // an operand from LDS (read some groups ahead), its product, and beside
         // it a share of the step's other work.
         // S' = K Q' of 32 tokens (base: where the lane's first operand lies; kb, vb: bytes
         // from there, constants)
-        auto multiply = [&](uint32_t base, int kb, f32x16 &s, auto beside) INLINE {
+        constexpr int KG = SMALL ? 2 * KK : KK, VG = SMALL ? DT : 2 * DT;       // products of 32 tokens
+        auto multiply = [&](uint32_t base, int kb, typename W::Scores &s, auto beside) INLINE {
             s16x8 kf[AHEAD + 1];
-            auto read = [&](int kk) INLINE { kf[kk % (AHEAD + 1)] = from_lds<s16x8>((base ^ 32 * kk) + kb); };
+            auto read = [&](int i) INLINE {
+                const int kk = i % KK;
+                kf[i % (AHEAD + 1)] = from_lds<s16x8>((base ^ 16 * W::fold(64 / R * kk)) + i / KK * 16 * ROW + kb);
+            };
+            f32x4 two[2];
 #pragma unroll
-            for (int kk = 0; kk < AHEAD; ++kk) read(kk);
+            for (int i = 0; i < AHEAD; ++i) read(i);
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                if (kk + AHEAD < KK) read(kk + AHEAD);
-                s = Type<T>::mfma32(kf[kk % (AHEAD + 1)], qf[kk], kk ? s : f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
-                beside(kk);
+            for (int i = 0; i < KG; ++i) {
+                if (i + AHEAD < KG) read(i + AHEAD);
+                const s16x8 x = kf[i % (AHEAD + 1)];
+                if constexpr (SMALL)
+                    two[i / KK] = Type<T>::mfma16(x, qf[i % KK], i % KK ? two[i / KK] : f32x4{0, 0, 0, 0});
+                else
+                    s = Type<T>::mfma32(x, qf[i], i ? s : f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
+                beside(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if constexpr (SMALL) s = __builtin_shufflevector(two[0], two[1], 0, 1, 2, 3, 4, 5, 6, 7);
         };
         // O' += V' P' of 32 tokens
         auto add = [&](uint32_t base, int vb, auto beside) INLINE {
             s16x8 vf[AHEAD + 1];
             auto read = [&](int i) INLINE {
-                const uint32_t x = (base ^ 64 * (i % DT)) + vb + (i / DT) * 16 * ROW;
-                const s16x4 y = read_column4(x), z = read_column4(x + 8 * ROW);
+                const uint32_t x = (base ^ 16 * W::fold(R / 8 * (i % DT))) + vb + (i / DT) * 16 * ROW;
+                const s16x4 y = read_column4(x), z = read_column4(x + (SMALL ? 16 : 8) * ROW);
                 vf[i % (AHEAD + 1)] = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
             };
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) read(i);
 #pragma unroll
-            for (int i = 0; i < 2 * DT; ++i) {
-                if (i + AHEAD < 2 * DT) read(i + AHEAD);
-                o[i % DT] = Type<T>::mfma32(vf[i % (AHEAD + 1)], pf[i / DT], o[i % DT]);
+            for (int i = 0; i < VG; ++i) {
+                if (i + AHEAD < VG) read(i + AHEAD);
+                const s16x8 x = vf[i % (AHEAD + 1)];
+                if constexpr (SMALL)
+                    o[i] = Type<T>::mfma16(x, pf[0], o[i]);
+                else
+                    o[i % DT] = Type<T>::mfma32(x, pf[i / DT], o[i % DT]);
                 beside(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
         auto nothing = [](int) INLINE {};
+        // the largest of what a row's lanes have
+        auto over_row = [&](float x, auto f) INLINE {
+            x = f(x, __shfl_xor(x, 32));
+            return SMALL ? f(x, __shfl_xor(x, 16)) : x;
+        };
+        const auto larger = [](float x, float y) INLINE { return fmaxf(x, y); };
+        const auto sum_of = [](float x, float y) INLINE { return x + y; };
         // One step of 32 tokens from t0 with scores x: products with the values
         // of the step before beside this step's maximum, scores of the next
         // step beside this step's weights.
-        auto step32 = [&](auto all_seen, f32x16 &x, f32x16 &next, int t0, uint32_t k_base, int k_next, uint32_t v_base, int v_before) INLINE {
+        auto step32 = [&](auto all_seen, typename W::Scores &x, typename W::Scores &next, int t0, uint32_t k_base, int k_next, uint32_t v_base, int v_before) INLINE {
             if constexpr (CAP) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[r] = score<true>(a, x[r]);
+                for (int r = 0; r < S; ++r) x[r] = score<true>(a, x[r]);
             }
             if (!all_seen && (t0 < wave_lo || t0 + 32 > wave_hi)) {
-                const int before = t0 + 4 * renewed(half), lo = see_lo - before, hi = see_hi - before;
+                const int before = t0 + 4 * renewed(part), lo = see_lo - before, hi = see_hi - before;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int t = 8 * (r / 4) + r % 4;
+                for (int r = 0; r < S; ++r) {
+                    const int t = (SMALL ? 16 : 8) * (r / 4) + r % 4;
                     if (!(t >= lo && t < hi)) x[r] = -INFINITY;
                 }
             }
             __builtin_amdgcn_s_setprio(1);
             float top = -INFINITY;
             add(v_base, v_before, [&](int i) INLINE {
-                constexpr int N = 8 / DT;
 #pragma unroll
-                for (int y = i * N; y < i * N + N; ++y) top = fmaxf(top, x[y]);
+                for (int y = i * S / VG; y < (i + 1) * S / VG; ++y) top = fmaxf(top, x[y]);
             });
             if constexpr (!CAP) top *= a.factor;
             if (__any(top > m + 8.0f)) {
-                const float now = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                const float now = fmaxf(m, over_row(top, larger));
                 const float keep = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
                 if (!__all(m == -INFINITY)) {                         // else the sums are zeros
                     l *= keep;
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[dt][r] *= keep;
+                    for (int dt = 0; dt < DT; ++dt) o[dt] *= keep;
                 }
                 m = now;
             }
@@ -248,11 +271,10 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
             // Weights are rounded to the 16-bit type, so that both operands of the
             // product are of one, as over 16 bits.
             float even = 0;
-            u32x4 packed[2];
+            u32x4 packed[S / 8];
             multiply(k_base, k_next, next, [&](int i) INLINE {
-                constexpr int N = 16 / KK;
 #pragma unroll
-                for (int r = i * N; r < i * N + N; ++r) {
+                for (int r = i * S / KG; r < (i + 1) * S / KG; ++r) {
                     const float w = __builtin_amdgcn_exp2f(CAP ? x[r] - base : __builtin_fmaf(x[r], a.factor, -base));
                     l += w;
                     if (r % 2)
@@ -261,7 +283,8 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
                         even = w;
                 }
             });
-            pf[0] = __builtin_bit_cast(s16x8, packed[0]), pf[1] = __builtin_bit_cast(s16x8, packed[1]);
+#pragma unroll
+            for (int y = 0; y < S / 8; ++y) pf[y] = __builtin_bit_cast(s16x8, packed[y]);
             __builtin_amdgcn_s_setprio(0);
         };
 
@@ -317,38 +340,54 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         }
         if (active) add(v_at + ((last - 1 - first) & 1) * TILE + 32 * ROW, 0, nothing);
 
-        float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (from == 0)) * (M * (DP + 2)) + wave * 32 * DP;
-        const float sum = l + __shfl_xor(l, 32);
+        // sums of 32 rows, as the join reads them: rows in products of 32, dimensions 4 at a time
+        float *sums = a.sums + ((int64_t)uniform(walk.worker) * 2 + (from == 0)) * (M * (DP + 2)) + wave * R / 32 * 32 * DP;
+        const int at_lane = SMALL ? (part / 2) * 64 + (part & 1) * 32 + (wave & 1) * 16 + col : lane;
+        const float sum = over_row(l, sum_of);
         if (starts && ends) {
             const int r = row_base + renewed(col);
             if (r < rows) {
                 const float scale = sum == 0 ? 0.0f : 1.0f / sum;
                 const int j = token_of(a, r);
                 const int64_t token = q0 + j, hq = (int64_t)head * a.group + r - j * a.group;
-                if (a.lse && half == 0)
+                if (a.lse && part == 0)
                     a.lse[token * a.heads + hq] = sum == 0 ? -INFINITY : 0.693147180559945f * (m + __builtin_amdgcn_logf(sum));
-                const int64_t to = token * a.out_token + hq * a.out_head + 4 * half;
+                const int64_t to = token * a.out_token + hq * a.out_head + 4 * part;
                 auto store = [&](auto f32) INLINE {
                     char *row = a.out + (f32 ? 4 : 2) * to;
+                    if constexpr (SMALL) {
 #pragma unroll
-                    for (int x = 0; x < DT * 4; ++x) {
-                        if (x >= a.units) break;
-                        const f32x16 &y = o[x / 4];
-                        const int i = x % 4 * 4;
-                        put4<T, f32>(row, 8 * x, f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]} * scale);
+                        for (int x = 0; x < DT; ++x) {
+                            if (2 * x >= a.units) break;
+                            put4<T, f32>(row, 16 * x, o[x] * scale);
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < DT * 4; ++x) {
+                            if (x >= a.units) break;
+                            const f32x16 &y = o[x / 4];
+                            const int i = x % 4 * 4;
+                            put4<T, f32>(row, 8 * x, f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]} * scale);
+                        }
                     }
                 };
                 a.out_f32 ? store(std::true_type()) : store(std::false_type());
             }
         } else {
-            // unnormalised sums, in the order of the registers
-            if (active) {
+            // unnormalised sums, also those of rows behind the last beside others
+            if (row_base / 32 * 32 < rows) {
+                if constexpr (SMALL) {
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
+                    for (int x = 0; x < DT; ++x) *(f32x4 *)(sums + (2 * x * 64 + at_lane) * 4) = o[x];
+                } else {
 #pragma unroll
-                    for (int r = 0; r < 16; r += 4)
-                        *(f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4) = f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]};
-                (sums - wave * 32 * DP + M * DP + wave * 64)[lane] = half ? sum : m;
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int r = 0; r < 16; r += 4)
+                            *(f32x4 *)(sums + ((dt * 4 + r / 4) * 64 + lane) * 4) = f32x4{o[dt][r], o[dt][r + 1], o[dt][r + 2], o[dt][r + 3]};
+                }
+                float *stats = sums - wave * R / 32 * 32 * DP + M * DP + wave * R / 32 * 64;
+                if (part < 2) stats[SMALL ? part * 32 + (wave & 1) * 16 + col : lane] = part ? sum : m;
             }
             if (!starts && tid == 0) {
                 const int workers = walk.second_of(range.count);
@@ -358,12 +397,13 @@ __global__ __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) void k_kv_wide_mx4(A
         if (__builtin_expect(__syncthreads_or(met), 0)) {
             const bool whole = starts && ends, f32 = !whole || a.out_f32;
             const int size = f32 ? 4 : 2;
+            constexpr int STEP = SMALL ? 16 : 8;             // dimensions from one of a lane's four to the next
             if (active)
                 nan_values<T>(a, table, shift, a.ve + head * a.ve_head, max(range.lo, first * BN), min(range.hi, last * BN), see_lo, see_hi,
-                              r0 < rows ? sum : NAN, whole, 4 * half, 8,
-                              whole ? a.out + size * ((int64_t)(q0 + j0) * a.out_token + ((int64_t)head * a.group + rr - j0 * a.group) * a.out_head + 4 * half)
-                                    : (char *)(sums + lane * 4),
-                              whole ? 8 * size : 64 * 16, f32);
+                              r0 < rows ? sum : NAN, whole, 4 * part, STEP,
+                              whole ? a.out + size * ((int64_t)(q0 + j0) * a.out_token + ((int64_t)head * a.group + rr - j0 * a.group) * a.out_head + 4 * part)
+                                    : (char *)(sums + at_lane * 4),
+                              whole ? STEP * size : STEP * 128, f32);
         }
         if (ends && walk.at < walk.end) walk.next(a, ent);
     }
@@ -387,7 +427,7 @@ static void launch_dim(const Attn4 &a, int waves, hipStream_t s) {
     else if (dim == 128)
         waves == 8 ? launch<T, 128, 8>(a, s) : launch<T, 128, 4>(a, s);
     else
-        launch<T, 256, 4>(a, s);
+        launch<T, 256, 8>(a, s);
 }
 
 void launch_wide_mx4(const Attn4 &a, int waves, hipStream_t s) {
