@@ -26,8 +26,8 @@ struct Wide4 {
     typedef float Sums __attribute__((ext_vector_type(R == 16 ? 4 : 16)));
     static constexpr int kTile = BN * ROW, CP = DP / 32, kPieces = BN * CP;   // bytes in 16 bits; pieces of a row, of a tile
     static constexpr int L = (2 * kPieces + kThreads - 1) / kThreads;          // pieces of keys and values per thread
-    static constexpr int C = 8;                                                // a tile's cost besides its steps, in steps
-    static constexpr int kAhead = DP == 256 ? 4 : 2;                           // operands read from LDS ahead of their products
+    static constexpr int C = DP == 256 ? 4 : 8;                                                // a tile's cost besides its steps, in steps
+    static constexpr int kAhead = DP == 256 ? 3 : 2;                           // operands read from LDS ahead of their products
 
     // Where the 16-byte pieces of a token's row lie: keys so that eight tokens'
     // pieces (wide heads: 16 tokens'), values so that four tokens' 64 bytes (32), fall
@@ -56,7 +56,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv_wide_mx4(Attn4 a) {
     bool lost = false;                         // a page id outside the pool
     // A thread's pieces, and where their elements go: the first quarter of each.
     auto is_key = [&](int i) INLINE { return i * THREADS + wave * 64 < W::kPieces; };
-    auto has_piece = [&](int i) INLINE { return i * THREADS + wave * 64 < 2 * W::kPieces; };
+    // (waves without a piece load another's: what is on its way is the same on all ways,
+    // or the compiler would wait for it as soon as it is asked for)
+    auto has_piece = [&](int i) INLINE { return L * THREADS == 2 * W::kPieces || i * THREADS + wave * 64 < 2 * W::kPieces; };
     auto piece_of = [&](int i) INLINE { return (i * THREADS + renewed(tid)) & (CP - 1); };
     auto token_of_piece = [&](int i) INLINE { return (int)((uint32_t)((i * THREADS + renewed(tid)) & (W::kPieces - 1)) / CP); };
     uint32_t put_at[L];
@@ -117,7 +119,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv_wide_mx4(Attn4 a) {
         auto fetch = [&](int j) INLINE {
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                if (!has_piece(i)) break;
                 const bool key = is_key(i);
                 const uint32_t id = min((uint32_t)ids[i], (uint32_t)c.n_pages - 1);
                 lost |= id != (uint32_t)ids[i] && range.hi > 0;
@@ -321,21 +322,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv_wide_mx4(Attn4 a) {
                 }
             }
             const int odd = (step - first) & 1, now = odd * TILE, other = TILE - now;
-            // its two halves by one piece of code: a call with few steps waits for its
-            // instructions more than for anything else
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                if (active) {
-                    step32(std::false_type(), s0, s1, step * BN + 32 * h, k_at + (h ? other : now + 32 * ROW), 0,
-                           v_at + (h ? now : other + 32 * ROW), 0);
-                    s0 = s1;
-                }
-                if (h) break;
-                __syncthreads();
-                make(!odd);
-                fetch(step + 2);
-                fetch_ids(step + 3);
-            }
+            if (active) step32(std::false_type(), s0, s1, step * BN, k_at + now + 32 * ROW, 0, v_at + other + 32 * ROW, 0);
+            __syncthreads();
+            make(!odd);
+            fetch(step + 2);
+            fetch_ids(step + 3);
+            if (active) step32(std::false_type(), s1, s0, step * BN + 32, k_at + other, 0, v_at + now, 0);
             ++step;
         }
         if (active) add(v_at + ((last - 1 - first) & 1) * TILE + 32 * ROW, 0, nothing);
