@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv_wide_mx4(Attn4 a) {
     const uint32_t k_at = lds_address(keys) + col * ROW + 16 * (part ^ W::k_swizzle(col));
     const int v_of = (SMALL ? 4 * part : 4 * (lane >> 5)) + (lane & 15) / 4, v_piece = (SMALL ? 0 : ((lane >> 4) & 1) * 2) + (lane & 3) / 2;
     const uint32_t v_at = lds_address(values) + v_of * ROW + (lane & 1) * 8 + 16 * (v_piece ^ W::v_swizzle(v_of));
-    bool lost = false;                         // a page id outside the pool
+    int lost = 0;                              // a page id outside the pool
     // A thread's pieces, and where their elements go: the first quarter of each.
     auto is_key = [&](int i) INLINE { return i * THREADS + wave * 64 < W::kPieces; };
     // (waves without a piece load another's: what is on its way is the same on all ways,
@@ -122,6 +122,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_kv_wide_mx4(Attn4 a) {
                 const bool key = is_key(i);
                 const uint32_t id = min((uint32_t)ids[i], (uint32_t)c.n_pages - 1);
                 lost |= id != (uint32_t)ids[i] && range.hi > 0;
+                // at this place: the old id and the one that is loaded next then have one register
+                asm volatile("" : "+v"(lost));
                 const uint64_t slot = (uint32_t)((j + key) * BN) & (c.page_size - 1);
                 codes[i] = mptkv::load<u32x4>(at(from_codes_of[i], id, key ? a.k_page : a.v_page) + slot * (key ? a.k_slot : a.v_slot));
                 scale[i] = mptkv::load<uint8_t>(at(from_scales_of[i], id, key ? a.ke_page : a.ve_page) + slot * (key ? a.ke_slot : a.ve_slot));
