@@ -36,19 +36,19 @@ struct Choice {
 // The limit of 32 rows for heads of 128 was drawn when 4 waves took 164 us where
 // they now take 131 and 52 where they take 44: at 17 to 32 rows narrow tiles no
 // longer gain.
-// Over 4 bits, whose codes every tile turns into 16 bits again, narrow tiles gain
-// for longer (measured the same way, over 4000 and over 300 tokens):
-//   dim 128, 128 entries: 16 rows 110/232/380 and 21/38/53; 32 rows 205/236/380
-//   and 35/41/54; 48 rows 291/275/391 and 49/47/57; 64 rows 392/281/393 and
-//   60/48/58; 128 rows 752/331/403 and 113/64/73; 256 rows 1464/680/612 and
-//   236/108/108. 32 entries: 48 rows 77/92/97 and 24/25/19; 64 rows 89/93/97 and
-//   20/25/20; 128 rows 169/106/100 and 34/33/24. 8 over 4000: 64 rows 36/49/42,
-//   128 rows 50/66/49
-//   dim 64, 128 entries: 16 rows 68/175/320 and 20/26/41; 48 rows 159/194/330 and
-//   32/30/45; 64 rows 215/195/330 and 44/30/46; 192 rows 579/379/366. 32 entries:
-//   64 rows 61/64/82 and 21/18/16
-//   dim 256, 32 entries: 16 rows 65/217; 48 rows 174/218 and 34/34; 64 rows
-//   226/220 and 43/35
+// Over 4 bits, whose codes every tile turns into 16 bits again (measured the same
+// way, over 4000 tokens and over 300):
+//   dim 128, 128 entries: 16 rows 109/222/312 and 23/37/49; 32 rows 207/212/311
+//   and 35/37/50; 48 rows 312/266/318 and 48/42/52; 128 rows 801/327/376 and
+//   113/60/70; 256 rows 1511/661/590 and 239/101/104. 32 entries: 32 rows 50/70/81
+//   and 14/21/17; 48 rows 77/87/85 and 24/23/18; 64 rows 90/88/84 and 20/23/18; 128
+//   rows 171/104/91 and 33/30/23. 8 over 4000: 48 rows 32/47/38, 128 rows 49/64/46
+//   dim 64, 128 entries: 32 rows 116/140/265 and 27/25/40; 48 rows 165/176/277 and
+//   32/29/43; 64 rows 219/180/280 and 44/29/44; 128 rows 419/202/287 and 74/38/54. 32
+//   entries: 48 rows 44/61/75 and 13/17/16; 64 rows 61/62/75 and 20/18/16
+//   dim 256 (eight waves of 16 rows), 128 entries: 16 rows 255/445 and 46/64; 32 rows
+//   483/451 and 81/68; 48 rows 698/458 and 115/71. 32 entries: 16 rows 61/114 and
+//   17/23; 32 rows 120/118 and 24/23; 8 over 4000: 32 rows 42/48, 64 rows 62/55
 // More workers than the card holds, and fewer, cost up to a third (512 of heads of
 // 128: 105 us of 128 entries, 256 139, 768 137). But single tiles of a few key heads
 // come to an end sooner with 256, whose partial sums are fewer to join: 8 heads of
@@ -59,7 +59,8 @@ static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_hea
     const int64_t rows = (n_tokens + (n > 0 ? n : 1) - 1) / (n > 0 ? n : 1) * (n_q_heads / c.n_heads);
     const int dim = pad_dim(c.head_dim);
     const bool few = (int64_t)n * c.n_heads <= 256, own_cu = dim == 128 && few;
-    if (rows <= (is_mx4(c) ? (few && dim != 256 ? 64 : 48) : dim == 128 ? 32 : 16)) {
+    const int narrow = dim == 256 ? 16 : !is_mx4(c) ? (dim == 128 ? 32 : 16) : dim == 64 || few ? 48 : 32;
+    if (rows <= narrow) {
         if (dim == 256 || (is_mx4(c) && rows <= 16 && (int64_t)n * c.n_heads <= 64)) return {0, 256, 16};
         return {0, dim == 128 ? 512 : 768, 16};
     }
