@@ -485,11 +485,11 @@ int mpt_pinned_assemble(int m, int64_t nnz, const int64_t *req_off, const int32_
  *
  * Errors in device data: a call that finds one ORs MPT_KV_* bits into *status,
  * where they stay until mpt_kv_status reads them. The page calls (forks to
- * copies below) then change nothing in tables and pages, appends write the
- * tokens that are in order. The page calls take a nullable HOST output; with
+ * copies below) then change nothing in tables and pages, appends write and
+ * reads return the tokens that are in order. The page calls take a nullable HOST output; with
  * it they synchronise `stream` and return the error of this call
  * (MPT_E_RANGE, MPT_E_DUP, MPT_E_STATE or MPT_E_PAGES). Without it, and in
- * mpt_kv_append, mpt_kv_attention and mpt_kv_merge, nothing synchronises, and
+ * appends, reads, mpt_kv_attention and mpt_kv_merge, nothing synchronises, and
  * the calls can be captured into a graph. Page ids outside [0, n_pages) and
  * slots outside [0, max_seqs) are never followed. The page calls look at every
  * page that they share, copy from, drop or (compaction) move, not at those
@@ -720,7 +720,8 @@ size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_
  * lse = minus infinity. What lies in tokens that a row does not see, NaN and
  * infinities included, has no effect on it. An infinite value that a row does
  * see makes its output infinite however small its weight (NaN beside a NaN or the
- * other infinity). The sums are formed with weights of up to 2^8, in 32 bits:
+ * other infinity). In 4 bits a byte E of NaN makes its 32 elements of the outputs
+ * NaN in the rows that see it as a value, and the score NaN that sees it as a key. The sums are formed with weights of up to 2^8, in 32 bits:
  * they overflow where weights times values pass 2^128. Bad slots count as empty,
  * tokens on bad pages as zeros or as some tokens of the pool, and tokens of no
  * entry get no output. Decoding is a chunk of one token;
@@ -735,6 +736,8 @@ size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_
  *   lse            device out, nullable: float [n_tokens * n_q_heads],
  *                  natural logarithms
  *   kv_begin [n]   device, nullable (0): first visible token
+ * The slots of a page, and the stride of pages, span less than 64 GiB of keys and
+ * of values (4 GiB of codes, and of bytes E).
  * Scores, statistics and sums are held in 32 bits; the weights exp(s_t - max)
  * are rounded to the cache's (16-bit) type for the product with the values.
  */

@@ -12,7 +12,7 @@
 // Two tiles of keys and two of values are there at a time.
 //
 // What bounds it: the matrix units and what their clock is under load (chunks of
-// 1024 tokens over 16k, 32 heads on 8 of 128: 1.00 to 1.06 ms, 1.0 to 1.06 PFLOP/s,
+// 1024 tokens over 16k, 32 heads on 8 of 128: 0.97 to 1.06 ms, 1.0 to 1.1 PFLOP/s,
 // where a library product of 8192^3 reaches 1.24), then vector instructions: scores
 // and weights as over 16 bits, and 16 conversions and 4 stores a piece.
 

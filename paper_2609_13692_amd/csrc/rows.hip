@@ -6,6 +6,13 @@
 // one token where there are few. Of each it forms the angles, in 64 bits (an angle
 // of position 10^6 in 32 bits would be off by 0.06), and hands them out through LDS;
 // its keys, values and queries go 64 units of 8 or 16 elements at a time.
+//
+// What bounds them is memory, where there is something to move: 25 chunks of 60 to
+// 600 tokens (32 heads and 8 key heads of 128), rotated into 16 bits with their
+// queries, 43 to 47 us (203 MB, 4.3 to 4.7 TB/s; a large copy reaches 5.0), 25 of 60 to
+// 1201 into 4 bits 76, 261 MB of codes read out as 983 MB 239 (5.2 TB/s). Few tokens are a launch. Angles formed once for the waves of a workgroup
+// instead of once for a wave's token took 55 to 120 us of the first, workgroups for
+// keys, values and queries apart as long.
 
 #include "kv.h"
 
@@ -19,7 +26,7 @@ using mptlib::fail;
 struct Append {
     mpt_kv_cache c;
     Scales e;
-    int layer, n, n_tokens, heads, run, parts;       // run: tokens of a wave; parts: waves that share them
+    int layer, n, n_tokens, heads, run, parts_log;   // run: tokens of a wave; 2^parts_log waves share them
     const int32_t *seqs, *q_off, *position;
     const char *k, *v, *q;
     char *q_out;
@@ -293,8 +300,8 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
     const int of_run = FOUR ? a.run : 1;             // tokens whose angles are there at a time
     Turn32 *t32 = (Turn32 *)(tables + (FOUR ? 4 * of_run * a.pairs * sizeof(Turn64) : 0)) + wave * of_run * a.pairs;
     Turn64 *t64 = (Turn64 *)tables + wave * of_run * a.pairs;
-    const int64_t at = wave_number(), group = a.parts == 1 ? at : at / a.parts;
-    const int part = (int)(at - group * a.parts);
+    const int64_t at = wave_number(), group = at >> a.parts_log;
+    const int parts = 1 << a.parts_log, part = (int)at & (parts - 1);
     if (group * a.run >= a.n_tokens) return;
     const int x0 = (int)(group * a.run), count = min(a.run, a.n_tokens - x0);
     Place place = locate(c, a.n, a.seqs, a.q_off, nullptr, x0, count);
@@ -326,7 +333,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
     // all roles' chunks in turn over the parts
     int before = 0;
     auto first_of = [&](int chunks) {
-        const int x = a.parts == 1 ? 0 : (int)((uint32_t)(part + a.parts * 65536 - before) % (uint32_t)a.parts);
+        const int x = (part - before) & (parts - 1);
         before += chunks;
         return x;
     };
@@ -351,18 +358,18 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
             *(uint4 *)((char *)(KEY ? c.k : c.v) + (a.layer * st[0] + page * st[1] + slot * st[2] + h * st[3]) + 16 * b) = codes;
             *(uint8_t *)((KEY ? a.e.k : a.e.v) + (a.layer * es[0] + page * es[1] + slot * es[2] + h * es[3]) + b) = (uint8_t)scale;
         };
-        for (int j = first_of(chunks); j < chunks; j += a.parts) put(std::integral_constant<int, kKeys>(), j * 64 + lane);
-        for (int j = first_of(chunks); j < chunks; j += a.parts) put(std::integral_constant<int, kValues>(), j * 64 + lane);
+        for (int j = first_of(chunks); j < chunks; j += parts) put(std::integral_constant<int, kKeys>(), j * 64 + lane);
+        for (int j = first_of(chunks); j < chunks; j += parts) put(std::integral_constant<int, kValues>(), j * 64 + lane);
         const int q0 = first_of(0);
         for (int x = 0; x < count; ++x) {
             if (!__builtin_amdgcn_readlane(place.known, x)) continue;
-            for (int j = q0; j < queries.chunks; j += 2 * a.parts) {
+            for (int j = q0; j < queries.chunks; j += 2 * parts) {
                 uint4 one[2], two[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) queries.load(x0 + x, (j + i * a.parts) * 64 + lane, one[i], two[i]);
+                for (int i = 0; i < 2; ++i) queries.load(x0 + x, (j + i * parts) * 64 + lane, one[i], two[i]);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    queries.put(x0 + x, 0, 0, (j + i * a.parts) * 64 + lane, one[i], two[i], t32 + x * a.pairs);
+                    queries.put(x0 + x, 0, 0, (j + i * parts) * 64 + lane, one[i], two[i], t32 + x * a.pairs);
             }
         }
     } else {
@@ -374,7 +381,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
             uint4 k1, k2, q1[2], q2[2], none;
             auto load_queries = [&](int j) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) queries.load(token, (j + i * a.parts) * 64 + lane, q1[i], q2[i]);
+                for (int i = 0; i < 2; ++i) queries.load(token, (j + i * parts) * 64 + lane, q1[i], q2[i]);
             };
             if (k0 < keys.chunks) keys.load(token, k0 * 64 + lane, k1, k2);
             if (q0 < queries.chunks) load_queries(q0);
@@ -386,21 +393,21 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
             if (page >= 0) {
                 for (int j = k0; j < keys.chunks;) {
                     keys.put(token, page, slot, j * 64 + lane, k1, k2, t32);
-                    if ((j += a.parts) < keys.chunks) keys.load(token, j * 64 + lane, k1, k2);
+                    if ((j += parts) < keys.chunks) keys.load(token, j * 64 + lane, k1, k2);
                 }
-                for (int j = v0; j < values.chunks; j += 2 * a.parts) {
+                for (int j = v0; j < values.chunks; j += 2 * parts) {
                     uint4 v[2];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) values.load(token, (j + i * a.parts) * 64 + lane, v[i], none);
+                    for (int i = 0; i < 2; ++i) values.load(token, (j + i * parts) * 64 + lane, v[i], none);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) values.put(token, page, slot, (j + i * a.parts) * 64 + lane, v[i], none, t32);
+                    for (int i = 0; i < 2; ++i) values.put(token, page, slot, (j + i * parts) * 64 + lane, v[i], none, t32);
                 }
             }
             if (known)
                 for (int j = q0; j < queries.chunks;) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) queries.put(token, 0, 0, (j + i * a.parts) * 64 + lane, q1[i], q2[i], t32);
-                    if ((j += 2 * a.parts) < queries.chunks) load_queries(j);
+                    for (int i = 0; i < 2; ++i) queries.put(token, 0, 0, (j + i * parts) * 64 + lane, q1[i], q2[i], t32);
+                    if ((j += 2 * parts) < queries.chunks) load_queries(j);
                 }
         }
     }
@@ -510,8 +517,14 @@ static void launch_append(Append &a, bool neighbours, hipStream_t s) {
     a.copy_mul = reciprocal(mx4 ? a.dim / 32 : a.dim / 8);
     a.e_min = bf16 ? -125 : -23, a.e_max = bf16 ? 125 : 13;
     const int lanes = c.n_heads * (a.dim / 32);          // of a token's keys, in 4 bits
+    // Tokens of a wave: as many as leave enough waves. In 4 bits a lane has 32 elements of a
+    // token's keys, and several tokens fill a wave where heads are few.
+    // Waves share tokens where there are few: 8 key heads of 128 and 32 query heads, in
+    // microseconds a launch with 1 / 2 / 4 waves, 256 tokens 8.0 / 6.9 / 6.0 (into 4 bits
+    // 9.4 / 8.1 / 7.7), 1024 tokens 9.3 / 8.9 / 9.4 (10.5 / 9.9 / 10.6), 2048 13.5 / 12.9 /
+    // 16.9 (14.9 / 14.6 / 19.7), 4096 20.3 / 23.3 / 28.1 (21.5 / 24.6 / 33.3).
     a.run = mx4 ? run_of(a.n_tokens, 4096, lanes >= 64 ? 1 : lanes >= 32 ? 2 : kRun4) : run_of(a.n_tokens, 16384, 16);
-    a.parts = a.n_tokens <= 1024 ? 4 : 1;
+    a.parts_log = a.n_tokens <= 512 ? 2 : a.n_tokens <= 2048 ? 1 : 0;
     using Kernel = void (*)(Append);
     static constexpr Kernel wide[2][2] = {
         {k_kv_append_rotated<__bf16, false, kApart>, k_kv_append_rotated<__bf16, false, kNeighbours>},
@@ -523,7 +536,7 @@ static void launch_append(Append &a, bool neighbours, hipStream_t s) {
          k_kv_append_rotated<_Float16, true, kApart>}};
     const Kernel kernel = mx4 ? four[!bf16][a.pairs == 0 ? kWhole : neighbours ? kNeighbours : kApart] : wide[!bf16][neighbours];
     const size_t lds = 4 * (size_t)a.pairs * (mx4 ? a.run * (sizeof(Turn32) + sizeof(Turn64)) : sizeof(Turn32));
-    const int64_t waves = ((int64_t)a.n_tokens + a.run - 1) / a.run * a.parts;
+    const int64_t waves = ((int64_t)a.n_tokens + a.run - 1) / a.run << a.parts_log;
     mptlib::LaunchScope scope("k_kv_append_rotated", (double)a.n_tokens, s);
     kernel<<<grid_of(waves), 256, lds, s>>>(a);
 }
