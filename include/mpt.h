@@ -662,7 +662,8 @@ typedef struct mpt_kv_rotation {
  * mpt_kv_append with the new keys rotated on the way, and the queries of the
  * same tokens rotated beside them: row (token, head) of q to that of q_out.
  * In a cache of 16 bits the sums above are formed in 32 bits and rounded to its
- * type, as q_out is; in one of 4 bits keys are rotated in 64 bits and rounded once.
+ * type, as q_out is; in one of 4 bits keys are rotated in 64 bits and rounded once
+ * (and count as infinite from 2^128 on).
  * Queries of tokens that are not written are rotated all the same, at
  * length - (q_off[i+1] - q_off[i]) + j, which may be negative; where there is no
  * such place (bad slots, tokens of no entry) and no position is given, q_out is

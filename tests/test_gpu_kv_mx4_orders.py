@@ -208,3 +208,22 @@ def test_the_whole_range_of_lengths_in_one_call():
     c, slots, ks, vs = filled(lengths, 16, 1, 64, torch.float16, 16)
     check(c, slots, ks, vs, [1, 1, 0, 1, 0, 1, 1, 1], 4, 17, torch.float16)
     check(c, slots, ks, vs, [1, 300, 0, 2, 0, 17, 33, 1], 4, 18, torch.float16)
+
+
+def test_rotations_past_the_range():
+    """Rotated keys that 32 bits do not hold are infinite, and so NaN in 4 bits; those
+    that the 16-bit type alone does not hold are as large as codes get."""
+    freq = torch.full((16,), np.pi / 4, device="cuda")
+    for dtype, big in ((torch.bfloat16, 3.0e38), (torch.float16, 60000.0)):
+        c = kv.KvCache.create(1, 4, 16, 1, 32, 1, 16, dtype, bits=4)
+        c.fork(ints([-1]), ints([0]), ints([0]), ints([2]), check=True)
+        k = torch.full((2, 1, 32), big, dtype=dtype, device="cuda")
+        k[1] = 1.0
+        c.append_rotated(0, k, k, ints([0, 2]), ints([0]), freq, positions=ints([1, 1]))
+        got, v = c.read(0, ints([0, 2]), ints([0]), 2)
+        if dtype is torch.bfloat16:
+            assert torch.isnan(got[0]).all()
+        else:
+            assert (got[0, 0, :16] == 0).all() and (got[0, 0, 16:] == 6 * 2.0 ** 13).all()
+        assert torch.isfinite(got[1]).all() and torch.isfinite(v).all()
+    assert c.take_status() == []
