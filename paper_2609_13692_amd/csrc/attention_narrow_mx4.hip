@@ -10,12 +10,13 @@
 // a step's keys and values are one load of a row a lane, and its page ids another;
 // lanes ask each other for them.
 //
-// What bounds it is a step's own instructions and the LDS it fills (8 KiB of 16-bit
-// values for 2 KiB of codes), not memory: with three workgroups to a CU instead of two
-// it is no faster, and with registers put into memory to make room for them slower
-// (64 contexts of 700 to 9000, 32 heads on 8 of 128: 79 us, 88 with 5 of them in
-// memory). Steps loaded two ahead instead of one, without a wait that the other order
-// would not have, take 86 us where one takes 84.
+// What bounds it is memory, where a worker has one tile: 64 contexts of 4000 tokens,
+// 32 heads on 8 of 128, 50 us (5.5 TB/s). Ragged contexts cost the starts and ends of
+// the tiles that a worker's part of the line cuts: 64 of 700 to 9000 tokens 82 us (4.1
+// TB/s) with a start counted as 3 steps, 84.5 as one, and 37 short ones of 64 19.9,
+// 21.3. Nothing else moved it: steps loaded two ahead instead of one (86), three
+// workgroups to a CU instead of two (79 to 88, with registers put into memory), cheaper
+// instructions in forming addresses.
 
 #include "attention_mx4.h"
 
@@ -30,7 +31,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <int DP>
 struct Narrow4 {
     static constexpr int M = 16, BN = 128, KK = DP / 32, DT = DP / 16, ROW = 2 * DP, CH = DP / 8;
-    static constexpr int C = 1;                                        // a tile's cost besides its steps, in steps
+    static constexpr int C = 3;                                        // a tile's cost besides its steps, in steps
     static constexpr int CODES = DP / 2, CP = CODES / 16, L = CP / 2;  // bytes and pieces of a row of codes; loads of 1 KiB
     static constexpr int E = DP == 256 ? 2 : 1;                        // bytes E of a quarter of a row
     static constexpr int kKeys = 32 * CODES, kValues = 32 * ROW;       // of a wave
