@@ -3,8 +3,9 @@
 // tokens read back.
 //
 // A wave takes a run of tokens, whose places its lanes find together, or a part of
-// one token where there are few. Of each it forms the angles, in 64 bits (an angle
-// of position 10^6 in 32 bits would be off by 0.06), and hands them out through LDS;
+// one token where there are few. It forms their angles, in 64 bits (an angle of
+// position 10^6 in 32 bits would be off by 0.06), of several tokens at a time where
+// 64 lanes do, and hands them out through LDS;
 // its keys, values and queries go 64 units of 8 or 16 elements at a time.
 //
 // What bounds them is memory, where there is something to move: 25 chunks of 60 to
@@ -34,7 +35,8 @@ struct Append {
     const float *freq;
     float factor;
     int pairs, dim, e_min, e_max;                    // rotated pairs of a row; head_dim
-    uint32_t turn_mul, copy_mul;                     // of divisions by a row's units
+    int batch;                                       // tokens of a wave whose angles are there at a time
+    uint32_t turn_mul, copy_mul, pair_mul;           // of divisions by a row's units, and by its pairs
 };
 
 // Where a token goes: lane l knows it of the l-th of the wave's tokens.
@@ -297,9 +299,8 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
     const Units<T, NEIGHBOURS, kKeys> keys(a, !FOUR && a.k);
     const Units<T, NEIGHBOURS, kValues> values(a, !FOUR && a.k);
     const Units<T, NEIGHBOURS, kQueries> queries(a, a.q);
-    const int of_run = FOUR ? a.run : 1;             // tokens whose angles are there at a time
-    Turn32 *t32 = (Turn32 *)(tables + (FOUR ? 4 * of_run * a.pairs * sizeof(Turn64) : 0)) + wave * of_run * a.pairs;
-    Turn64 *t64 = (Turn64 *)tables + wave * of_run * a.pairs;
+    Turn32 *t32 = (Turn32 *)(tables + (FOUR ? 4 * a.batch * a.pairs * sizeof(Turn64) : 0)) + wave * a.batch * a.pairs;
+    Turn64 *t64 = (Turn64 *)tables + wave * a.batch * a.pairs;
     const int64_t at = wave_number(), group = at >> a.parts_log;
     const int parts = 1 << a.parts_log, part = (int)at & (parts - 1);
     if (group * a.run >= a.n_tokens) return;
@@ -315,14 +316,16 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
     }
     if (part == 0 && place.bad) flag(c, place.bad);
     if (a.position && lane < count) place.pos = a.position[x0 + lane], place.known = true;
-    auto turn = [&](int x, Turn32 *to32, Turn64 *to64) {
-        const double pos = __builtin_amdgcn_readlane(place.pos, x);
-        for (int p = lane; p < a.pairs; p += 64) {
+    // angles of tokens x .. x + n - 1, a pair a lane
+    auto turn = [&](int x, int n) {
+        for (int y0 = 0; y0 < n * a.pairs; y0 += 64) {
+            const int y = min(y0 + lane, n * a.pairs - 1), z = divided(y, a.pair_mul), p = y - z * a.pairs;
+            const double pos = __shfl(place.pos, x + z);
             double s, co;
             sincos(pos * (double)a.freq[p], &s, &co);
             co *= a.factor, s *= a.factor;
-            if (FOUR) to64[p] = Turn64{co, s};
-            to32[p] = Turn32{(float)co, (float)s};
+            if (FOUR) t64[y] = Turn64{co, s};
+            t32[y] = Turn32{(float)co, (float)s};
         }
     };
     auto handed_out = [&]() {
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
         return x;
     };
     if constexpr (FOUR) {
-        for (int x = 0; x < count; ++x) turn(x, t32 + x * a.pairs, t64 + x * a.pairs);
+        turn(0, count);
         handed_out();
         const int blocks = a.dim / 32, units = c.n_heads * blocks, all = a.k ? count * units : 0, chunks = (all + 63) / 64;
         auto put = [&](auto role, int y) {
@@ -374,7 +377,7 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
         }
     } else {
         const int k0 = first_of(keys.chunks), v0 = first_of(values.chunks), q0 = first_of(0);
-        for (int x = 0; x < count; ++x) {
+        for (int x = 0, first = 0; x < count; ++x) {         // first: of those whose angles are there
             const int64_t token = x0 + x;
             const int page = __builtin_amdgcn_readlane(place.page, x), slot = __builtin_amdgcn_readlane(place.slot, x);
             const bool known = __builtin_amdgcn_readlane(place.known, x);
@@ -385,14 +388,16 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
             };
             if (k0 < keys.chunks) keys.load(token, k0 * 64 + lane, k1, k2);
             if (q0 < queries.chunks) load_queries(q0);
-            if (known) {
-                __builtin_amdgcn_wave_barrier();             // the last token's are read
-                turn(x, t32, nullptr);
+            if (x == 0 || x == first + a.batch) {
+                first = x;
+                __builtin_amdgcn_wave_barrier();             // the last tokens' are read
+                turn(x, min(a.batch, count - x));
                 handed_out();
             }
+            const Turn32 *turns = t32 + (x - first) * a.pairs;
             if (page >= 0) {
                 for (int j = k0; j < keys.chunks;) {
-                    keys.put(token, page, slot, j * 64 + lane, k1, k2, t32);
+                    keys.put(token, page, slot, j * 64 + lane, k1, k2, turns);
                     if ((j += parts) < keys.chunks) keys.load(token, j * 64 + lane, k1, k2);
                 }
                 for (int j = v0; j < values.chunks; j += 2 * parts) {
@@ -400,13 +405,13 @@ __global__ __launch_bounds__(256, 4) void k_kv_append_rotated(Append a) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) values.load(token, (j + i * parts) * 64 + lane, v[i], none);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) values.put(token, page, slot, (j + i * parts) * 64 + lane, v[i], none, t32);
+                    for (int i = 0; i < 2; ++i) values.put(token, page, slot, (j + i * parts) * 64 + lane, v[i], none, turns);
                 }
             }
             if (known)
                 for (int j = q0; j < queries.chunks;) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) queries.put(token, 0, 0, (j + i * parts) * 64 + lane, q1[i], q2[i], t32);
+                    for (int i = 0; i < 2; ++i) queries.put(token, 0, 0, (j + i * parts) * 64 + lane, q1[i], q2[i], turns);
                     if ((j += 2 * parts) < queries.chunks) load_queries(j);
                 }
         }
@@ -557,7 +562,11 @@ static void launch_append(Append &a, bool neighbours, hipStream_t s) {
         {k_kv_append_rotated<_Float16, true, kWhole>, k_kv_append_rotated<_Float16, true, kNeighbours>,
          k_kv_append_rotated<_Float16, true, kApart>}};
     const Kernel kernel = mx4 ? four[!bf16][a.pairs == 0 ? kWhole : neighbours ? kNeighbours : kApart] : wide[!bf16][neighbours];
-    const size_t lds = 4 * (size_t)a.pairs * (mx4 ? a.run * (sizeof(Turn32) + sizeof(Turn64)) : sizeof(Turn32));
+    // 64000 tokens of 4 query heads and 2 key heads of 64, 32 elements rotated: 63 us with four
+    // tokens' angles formed at a time, 72 with one's
+    a.batch = mx4 ? a.run : a.pairs < 64 ? 64 / a.pairs : 1;
+    a.pair_mul = reciprocal(a.pairs ? a.pairs : 1);
+    const size_t lds = 4 * (size_t)a.pairs * a.batch * (mx4 ? sizeof(Turn32) + sizeof(Turn64) : sizeof(Turn32));
     const int64_t waves = ((int64_t)a.n_tokens + a.run - 1) / a.run << a.parts_log;
     mptlib::LaunchScope scope("k_kv_append_rotated", (double)a.n_tokens, s);
     kernel<<<grid_of(waves), 256, lds, s>>>(a);
