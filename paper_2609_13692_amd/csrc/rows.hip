@@ -56,7 +56,7 @@ __device__ inline Place locate(const mpt_kv_cache &c, int n, const int32_t *seqs
     int i = n > 0 ? wave_find(off, n, x0) : -1;
     if (lane >= count) return p;
     const int x = x0 + lane;
-    if (i >= 0 && i < n && x >= off[i + 1]) {            // a later entry's
+    if (n > 0 && i < n && x >= off[i + 1]) {             // a later entry's than x0's (-1: before the first)
         int lo = i + 1, hi = n;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
