@@ -634,8 +634,9 @@ int mpt_kv_copy(const mpt_kv_cache *cache, int n, const int32_t *src, const int3
  *   k_new, v_new         device, the cache's type (of one in 4 bits its 16-bit
  *                        type), [n_tokens, n_heads, head_dim]; strides in
  *                        elements, multiples of 8; 16-byte aligned
- * Tokens before position 0, in bad slots or pages, or in pages that other
- * sequences refer to are not written (and set status bits).
+ * Tokens before position 0 or past the table's last (of a length above max_pages *
+ * page_size), in bad slots or pages, or in pages that other sequences refer to are
+ * not written (and set status bits).
  */
 int mpt_kv_append(const mpt_kv_cache *cache, int layer, int n, const int32_t *seqs,
                   const int32_t *q_off, int64_t n_tokens, const void *k_new,
@@ -686,7 +687,8 @@ int mpt_kv_append_rotated(const mpt_kv_cache *cache, int layer, int n, const int
  * Reads tokens of one layer out in the cache's 16-bit type: entry i < n has the
  * rows off[i] .. off[i+1] - 1 of k_out and v_out, for the tokens from first[i] on
  * of the sequence in slot seqs[i] (first NULL: its newest). Rows of tokens that
- * are not there (before the first, past the last, on bad pages, in bad slots)
+ * are not there (before the first, past the last or the table's last, on bad pages,
+ * in bad slots)
  * are zeros, and set status bits; rows of no entry are left as they were.
  *   seqs [n]        device; a slot may be listed several times
  *   off [n+1]       device; off[0] = 0, non-decreasing, off[n] = n_tokens

@@ -70,11 +70,13 @@ __device__ inline Place locate(const mpt_kv_cache &c, int n, const int32_t *seqs
     p.bad = MPT_KV_BAD_SLOT;
     if (i < 0 || i >= n || !slot_ok(c, seqs[i])) return p;
     const int s = seqs[i];
-    const int length = max(0, (int)min((int64_t)c.length[s], (int64_t)c.max_pages << shift));
-    p.pos = first ? (int)min((int64_t)first[i] + (x - off[i]), (int64_t)INT32_MAX) : length - (off[i + 1] - x);
+    const int length = c.length[s];
+    // in 64 bits: a length may be any number (a place below -2^31 counts as that)
+    const int64_t pos = first ? (int64_t)first[i] + (x - off[i]) : (int64_t)length - off[i + 1] + x;
+    p.pos = (int)max((int64_t)INT32_MIN, min(pos, (int64_t)INT32_MAX));
     p.known = true;
     p.bad = MPT_KV_BAD_LENGTH;
-    if (p.pos < 0 || p.pos >= length) return p;
+    if (pos < 0 || pos >= length || (pos >> shift) >= c.max_pages) return p;
     p.bad = MPT_KV_BAD_PAGE;
     const int page = c.table[(int64_t)s * c.max_pages + (p.pos >> shift)];
     if (!page_ok(c, page)) return p;
