@@ -511,8 +511,9 @@ __global__ __launch_bounds__(256) void k_kv_read(Read a) {
         }
     } else {
         for (int z0 = 0; z0 < pieces; z0 += 64) {
-            const int z = z0 + lane, h = divided(z, a.copy_mul), u = z - h * units;
-            if (z >= pieces) break;
+            // lanes past the last piece read that one: all stay to the end, for any may be
+            // asked for a token's place
+            const int z = min(z0 + lane, pieces - 1), h = divided(z, a.copy_mul), u = z - h * units;
             for (int x = 0; x < count; x += U) {
                 Got g[U];
 #pragma unroll
@@ -522,7 +523,7 @@ __global__ __launch_bounds__(256) void k_kv_read(Read a) {
                 }
 #pragma unroll
                 for (int i = 0; i < U; ++i)
-                    if (x + i < count) store(g[i], x0 + x + i, h, u);
+                    if (x + i < count && z0 + lane < pieces) store(g[i], x0 + x + i, h, u);
             }
         }
     }
