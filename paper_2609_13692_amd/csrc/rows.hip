@@ -167,12 +167,14 @@ __device__ inline void turn_unit(int pairs, uint4 a, uint4 b, char *out, int u, 
     *(uint4 *)(out + first) = narrow<T>(y);
 }
 
-// y rounded to 24 bits so that a later rounding to fewer gives what y itself
-// would: what is cut off leaves the last bit set.
+// y rounded to 23 bits so that a later rounding to fewer gives what y itself
+// would: what is cut off leaves the last bit set. Of 24 bits the last would be lost
+// in numbers of 32 bits below 2^-126, which are 2^-149 apart: between 2^-127, the
+// smallest border of codes (half of 2^-126), and 2^-126 those have 23.
 __device__ inline float to_odd(double y) {
     const uint64_t b = __builtin_bit_cast(uint64_t, y);
-    const uint32_t lo = (uint32_t)b, cut = (lo & 0x1fffffffu) + 0x1fffffffu;    // bit 29: something is cut off
-    const uint32_t kept = (lo | (cut & 0x20000000u)) & 0xe0000000u;
+    const uint32_t lo = (uint32_t)b, cut = (lo & 0x3fffffffu) + 0x3fffffffu;    // bit 30: something is cut off
+    const uint32_t kept = (lo | (cut & 0x40000000u)) & 0xc0000000u;
     return (float)__builtin_bit_cast(double, (b & 0xffffffff00000000ull) | kept);
 }
 
