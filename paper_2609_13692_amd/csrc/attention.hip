@@ -68,9 +68,11 @@ static Choice choose(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_hea
     return {8, 256, 256};
 }
 
+// Of the kernels of many rows, which keep as many sums, all calls need the same: a
+// cache that holds a workspace for each size then holds these 65 MiB once.
 static size_t attention_bytes(const mpt_kv_cache &c, int n, int64_t n_tokens, int n_q_heads) {
     const Choice ch = choose(c, n, n_tokens, n_q_heads);
-    return mptlib::align256(sizeof(Part) * ch.workers) +
+    return mptlib::align256(sizeof(Part) * (ch.waves ? 512 : ch.workers)) +
            mptlib::align256(sizeof(float) * 2 * ch.workers * ch.rows * (size_t)(pad_dim(c.head_dim) + 2));
 }
 
