@@ -724,10 +724,12 @@ size_t mpt_kv_attention_workspace_bytes(const mpt_kv_cache *cache, int n, int64_
  * infinities included, has no effect on it. An infinite value that a row does
  * see makes its output infinite however small its weight (NaN beside a NaN or the
  * other infinity). In 4 bits a byte E of NaN makes its 32 elements of the outputs
- * NaN in the rows that see it as a value, and the score NaN that sees it as a key. The sums are formed with weights of up to 2^8, in 32 bits:
- * they overflow where weights times values pass 2^128. Bad slots count as empty,
- * tokens on bad pages as zeros or as some tokens of the pool, and tokens of no
- * entry get no output. Decoding is a chunk of one token;
+ * NaN in the rows that see it as a value, and the score NaN that sees it as a key.
+ * The sums are formed with weights of up to 2^8, in 32 bits: they overflow where
+ * weights times values pass 2^128; finite scores are to stay below 2^25 in size. Bad
+ * slots count as empty, a length above max_pages * page_size as that many tokens,
+ * tokens on bad pages as zeros or as some tokens of the pool, and tokens of no entry
+ * get no output. Decoding is a chunk of one token;
  * a prefix that several sequences share is one slot with all of their queries
  * and causal = 0, joined with their own parts (kv_begin) by mpt_kv_merge.
  *   seqs [n]       device; a slot may be listed several times

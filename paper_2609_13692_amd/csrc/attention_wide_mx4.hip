@@ -12,9 +12,17 @@
 // Two tiles of keys and two of values are there at a time.
 //
 // What bounds it: the matrix units and what their clock is under load (chunks of
-// 1024 tokens over 16k, 32 heads on 8 of 128: 0.97 to 1.06 ms, 1.0 to 1.1 PFLOP/s,
+// 1024 tokens over 16k, 32 heads on 8 of 128: 0.95 to 1.06 ms, 1.0 to 1.1 PFLOP/s,
 // where a library product of 8192^3 reaches 1.24), then vector instructions: scores
-// and weights as over 16 bits, and 16 conversions and 4 stores a piece.
+// and weights as over 16 bits, and 16 conversions and 4 stores a piece. Where a
+// workgroup has few steps, it is what surrounds them. The numbers that a tile starts
+// from do not fit the scalar registers beside the loop's: eight waves and heads of 128
+// keep 108 of them and 6 vector registers elsewhere (of 256, 167 and 16), and a
+// start takes 106 lane moves and 5 reads of memory for them (162 and 8), a step none
+// (2 moves).
+// And a tile that is cut goes through memory: 9 chunks of heads of 256 with a window
+// are 140 tiles over 256 workgroups, of which 127 are cut into 313 parts of 132 KB, 41
+// MB written and read again beside the 27 MB of the case itself (59 us in all).
 
 #include "attention_mx4.h"
 

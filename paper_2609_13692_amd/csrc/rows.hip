@@ -11,9 +11,11 @@
 // What bounds them is memory, where there is something to move: 25 chunks of 60 to
 // 600 tokens (32 heads and 8 key heads of 128), rotated into 16 bits with their
 // queries, 43 to 47 us (203 MB, 4.3 to 4.7 TB/s; a large copy reaches 5.0), 25 of 60 to
-// 1201 into 4 bits 76, 261 MB of codes read out as 983 MB 239 (5.2 TB/s). Few tokens are a launch. Angles formed once for the waves of a workgroup
-// instead of once for a wave's token took 55 to 120 us of the first, workgroups for
-// keys, values and queries apart as long.
+// 1201 into 4 bits 76, 261 MB of codes read out as 983 MB 239 (5.2 TB/s). Few tokens
+// are a launch. Angles formed once for the waves of a workgroup instead of once for a
+// wave's token took 55 to 120 us of the first, workgroups for keys, values and queries
+// apart as long. Of few heads it is a chain of reads a token: 64000 tokens of 4 query
+// heads and 2 key heads of 64, 63 us (2.1 TB/s).
 
 #include "kv.h"
 

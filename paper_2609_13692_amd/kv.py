@@ -261,9 +261,11 @@ class KvCache:
         rotated to their positions: pair i of a row by position * freq[i], its
         first 2 len(freq) elements in all (see mpt_kv_append_rotated). Returns
         the rotated queries, in q_out (which may be q) or a new tensor; None
-        without any. positions [tokens] int32 in the place of the tokens' own in
-        their sequences; with k_new and v_new None nothing is written, and then,
-        with positions, q_off and seqs may be None."""
+        without any. Queries without a place (of bad slots, no positions given)
+        are not written: their rows of a new tensor hold anything. positions
+        [tokens] int32 in the place of the tokens' own in their sequences; with
+        k_new and v_new None nothing is written, and then, with positions, q_off
+        and seqs may be None."""
         index = self._index
         at, under = _on(stream, index)
         if freq.dtype is not torch.float32 or freq.get_device() != index or freq.dim() != 1 or not freq.is_contiguous():
